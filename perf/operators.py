@@ -1,0 +1,542 @@
+"""What the performance of the package's operators is judged by: calls of the
+attention with a sliding window, sinks and a relative position bias, and of
+the AdamW step over many tensors, over the sizes, types and masks that a
+training program gives them.
+
+Beside each call stands its plain form: the operator's formulas in elementary
+torch operations, in 32 bits whatever the tensors' type (in 64 where a moment
+is rounded to 8 bits), rounded once at the end.
+
+Attention.  Token j of a sequence is visible to token i when it lies within the
+sequence's length, does not follow i (causal), and is one of the first `sinks`
+tokens or less than `window` away (window 0: no window).  Scores are
+scale q.k plus, with buckets, a learned value of the head and of the bucket
+that holds the distance j - i.
+
+AdamW.  The moments are fp32, or 8-bit codes: blocks of 128 elements of a
+tensor share a power of two per moment; the first moment is held in e4m3, the
+second in an unsigned format of five exponent and three fraction bits.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+LR, BETA1, BETA2, EPS, DECAY, STEP, SCALE = 1e-4, 0.9, 0.95, 1e-8, 0.1, 7, 0.25
+BLOCK = 128           # elements that share a power of two
+M_BIAS, V_BIAS = 127, 160  # a unit of 2^(byte - bias) per block
+
+
+def _attn(name, batch, seq, heads, dim, kv_heads=None, dtype="bf16", causal=True, window=0, sinks=0,
+          buckets=0, max_distance=0, cut=0, train=True):
+    return dict(name=name, kind="attention", batch=batch, seq=seq, heads=heads, kv_heads=kv_heads or heads,
+                dim=dim, dtype=dtype, causal=causal, window=window, sinks=sinks, buckets=buckets,
+                max_distance=max_distance, cut=cut, train=train)
+
+
+def _adamw(name, bits, layers, hidden, ffn, ragged=0, grads="f32", copies=True):
+    return dict(name=name, kind="adamw", bits=bits, layers=layers, hidden=hidden, ffn=ffn, ragged=ragged,
+                grads=grads, copies=copies)
+
+
+def listed():
+    return [
+        # The smallest workload's attention (fp32, 128 tokens) under a window:
+        # a functional run, where a launch is all there is.
+        _attn("window_tiny_fwd", 1, 128, 4, 64, dtype="f32", window=32, sinks=4, train=False),
+        # 1.3B layer, two sequences of 2048, a window of a quarter of them.
+        _attn("window_1.3b", 2, 2048, 16, 128, window=512, sinks=4),
+        # One long sequence with 8 key heads for 32 query heads: what a window is for.
+        _attn("window_long", 1, 8192, 32, 128, kv_heads=8, window=1024, sinks=4),
+        # Bidirectional, heads of 80, a padded batch of ragged sequences.
+        _attn("window_ragged", 4, 1000, 32, 80, causal=False, window=100, sinks=1, cut=311),
+        # Forward only (evaluation) of a very long sequence, heads of 64, a narrow window.
+        _attn("window_eval", 1, 16384, 16, 64, window=256, sinks=16, train=False),
+        # An encoder's layer: bidirectional, short padded sequences, the usual 32 buckets.
+        _attn("bias_encoder", 8, 512, 16, 64, causal=False, buckets=32, max_distance=128, cut=37),
+        # 6.7B layer, causal, a bias instead of learned positions.
+        _attn("bias_6.7b", 1, 2048, 32, 128, buckets=32, max_distance=128),
+        # fp32 validation of the same at a small odd size.
+        _attn("bias_f32", 2, 136, 3, 64, dtype="f32", buckets=32, max_distance=128),
+        # 13B layer's heads with everything: window, sinks and a far-reaching bias.
+        _attn("bias_window_13b", 1, 4096, 40, 128, window=2048, sinks=4, buckets=64, max_distance=512),
+        # A 1.3B stage's parameters, fp32 moments.
+        _adamw("adamw32_1.3b", 32, 3, 2048, 8192),
+        # Two layers of the 6.7B stage, 8-bit moments.
+        _adamw("adamw8_6.7b", 8, 2, 4096, 16384, grads="bf16"),
+        # Many small odd tensors: norms, biases, tables.
+        _adamw("adamw8_small", 8, 3, 256, 1024, ragged=24, copies=False),
+    ]
+
+
+def _log(rng, low, high):
+    """A whole number between low and high, spread over its logarithm."""
+    return max(low, min(high, int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))))
+
+
+def draw(rng):
+    if rng.random() < 0.3:
+        bits, hidden = rng.choice((8, 32)), 8 * _log(rng, 8, 640)
+        ffn = 8 * _log(rng, 8, 2048)
+        per_layer = 4 * hidden * hidden + 2 * hidden * ffn
+        layers = max(1, min(6, int(3e8 / per_layer), _log(rng, 1, 6)))
+        case = _adamw("", bits, layers, hidden, ffn, ragged=rng.randint(0, 24), grads=rng.choice(("f32", "bf16")),
+                      copies=rng.random() < 0.6)
+    else:
+        dtype = "f32" if rng.random() < 0.2 else "bf16"
+        seq = _log(rng, 1, 2048 if dtype == "f32" else 8192)
+        group = rng.choice((1, 1, 2, 4))
+        room = int((5e8 if dtype == "bf16" else 6e7) / (seq * seq)) + 1   # scores of the plain form
+        heads = group * max(1, min(_log(rng, 1, 40), room) // group)
+        batch = max(1, min(rng.randint(1, 8), room // heads))
+        dim = 8 * rng.choice((2, 4, 5, 8, 8, 10, 12, 13, 16, 16, 16))
+        causal = rng.random() < 0.6
+        what = rng.choice(("window", "bias", "both"))
+        window = 0 if what == "bias" else _log(rng, 1, max(1, seq))
+        sinks = rng.choice((0, 1, 4, 16, 64, 100)) if window else 0
+        buckets = 0 if what == "window" else rng.choice((8, 32, 32, 64))
+        case = _attn("", batch, seq, heads, dim, kv_heads=heads // group, dtype=dtype, causal=causal, window=window,
+                     sinks=sinks, buckets=buckets, max_distance=rng.choice((64, 128, 128, 512)) if buckets else 0,
+                     cut=rng.choice((0, 0, _log(rng, 1, max(1, seq // 2)))), train=rng.random() < 0.75)
+    del case["name"]
+    return case
+
+
+# -- what a program has before the call ------------------------------------------
+
+
+def _lengths(case):
+    """Tokens of each sequence: the first one is whole, each further one `cut` shorter."""
+    return [max(0, case["seq"] - b * case["cut"]) for b in range(case["batch"])]
+
+
+def _tensors(case):
+    """(elements, decays and keeps a bf16 copy) of every tensor: a stage's layers, then ragged ones."""
+    h, f, got = case["hidden"], case["ffn"], []
+    for _ in range(case["layers"]):
+        got += [(3 * h * h, True), (h * h, True), (h * f, True), (f * h, True)]
+        got += [(h, False)] * 6 + [(3 * h, False), (f, False)]
+    return got + [(1 + (i * i * 37) % 4099, False) for i in range(case["ragged"])]
+
+
+def _places(case):
+    """Each tensor's first element in flat buffers that pad every tensor to whole blocks, and their size."""
+    at, places = 0, []
+    for n, _ in _tensors(case):
+        places.append(at)
+        at += -(-n // BLOCK) * BLOCK
+    return places, at
+
+
+def prepare(case, seed):
+    gen = torch.Generator("cuda").manual_seed(seed)
+
+    def normal(*shape, std=1.0):
+        return torch.randn(*shape, device="cuda", generator=gen).mul_(std)
+
+    if case["kind"] == "attention":
+        kind = torch.float32 if case["dtype"] == "f32" else torch.bfloat16
+        b, s, h, kv, d = (case[k] for k in ("batch", "seq", "heads", "kv_heads", "dim"))
+        st = {"case": case, "q": normal(b, s, h, d).to(kind), "k": normal(b, s, kv, d).to(kind),
+              "v": (normal(b, s, kv, d) + 0.3).to(kind), "do": normal(b, s, h, d, std=0.1).to(kind), "bias": None,
+              "lengths": None}
+        if case["buckets"]:
+            st["bias"] = normal(h, case["buckets"]).to(kind)
+        if case["cut"]:
+            st["lengths"] = torch.tensor(_lengths(case), dtype=torch.int32, device="cuda")
+        return st
+    places, n = _places(case)
+    real = torch.zeros(n, device="cuda")
+    decay = torch.zeros(n, dtype=torch.bool, device="cuda")
+    for (count, matrix), at in zip(_tensors(case), places):
+        real[at:at + count] = 1.0
+        decay[at:at + count] = matrix
+    # gradients of a few sizes over a tensor, as rows of a matrix have them
+    size = torch.exp(normal(n // BLOCK, 1).expand(-1, BLOCK).reshape(-1)).mul_(1e-3)
+    g = normal(n).mul_(size).mul_(real)
+    m = normal(n, std=0.4).mul_(size).mul_(real)
+    v = normal(n).mul_(size).square_().add_(size.square().mul_(0.1)).mul_(real)
+    st = {"case": case, "p": normal(n, std=0.02).mul_(real), "decay": decay,
+          "g": g.to(torch.bfloat16) if case["grads"] == "bf16" else g,
+          "copy": torch.zeros(n, dtype=torch.bfloat16, device="cuda") if case["copies"] else None}
+    if case["bits"] == 32:
+        return {**st, "m": m, "v": v}
+    st["m"], st["m_exp"] = _encode_m(m.double())
+    st["v"], st["v_exp"] = _encode_v(v.double())
+    return st
+
+
+# -- the plain forms --------------------------------------------------------------
+
+
+def _borders(buckets, max_distance, causal):
+    """Smallest distance of each bucket after the first, of one direction: whole numbers, so that no
+    rounding of a logarithm decides."""
+    nb = buckets if causal else buckets // 2
+    exact = nb // 2
+    k = nb - exact
+    far, n = [], exact
+    for step in range(1, k):
+        while n ** k < exact ** (k - step) * max_distance ** step:
+            n += 1
+        far.append(n)
+    return list(range(1, exact + 1)) + far
+
+
+def _bucket_of(case):
+    """The bucket of every distance j - i from -(seq - 1) to seq - 1."""
+    far = torch.arange(-(case["seq"] - 1), case["seq"], device="cuda")
+    edges = torch.tensor(_borders(case["buckets"], case["max_distance"], case["causal"]), device="cuda")
+    n = (-far).clamp(min=0) if case["causal"] else far.abs()
+    of = torch.bucketize(n, edges, right=True)
+    return of if case["causal"] else of + (far > 0) * (case["buckets"] // 2)
+
+
+def _visible(case, lengths):
+    s = case["seq"]
+    i, j = torch.arange(s, device="cuda")[:, None], torch.arange(s, device="cuda")[None, :]
+    see = torch.ones(s, s, dtype=torch.bool, device="cuda")
+    if case["causal"]:
+        see &= j <= i
+    if case["window"]:
+        see &= ((i - j).abs() < case["window"]) | (j < case["sinks"])
+    if lengths is None:
+        return see
+    n = lengths[:, None, None, None]
+    return see & (j < n) & (i < n)
+
+
+def _plain_attention(st):
+    c = st["case"]
+    b, s, h, kv, d = (c[k] for k in ("batch", "seq", "heads", "kv_heads", "dim"))
+    kind, group = st["q"].dtype, h // kv
+    q, do = st["q"].float().transpose(1, 2), st["do"].float().transpose(1, 2)
+    k = st["k"].float().transpose(1, 2).repeat_interleave(group, 1)
+    v = st["v"].float().transpose(1, 2).repeat_interleave(group, 1)
+    scale = 1.0 / math.sqrt(d)
+    x = torch.matmul(q, k.transpose(2, 3)).mul_(scale)
+    if c["buckets"]:
+        i = torch.arange(s, device="cuda")
+        of = _bucket_of(c)
+        x += st["bias"].float()[:, of][:, i[None, :] - i[:, None] + s - 1]
+    see = _visible(c, st["lengths"])
+    x = x.masked_fill_(~see, -math.inf)
+    top = x.amax(-1, keepdim=True)
+    p = torch.exp(x.sub_(torch.where(top == -math.inf, 0.0, top)))
+    total = p.sum(-1, keepdim=True)
+    p /= torch.where(total == 0, 1.0, total)
+    out = {"o": torch.matmul(p, v).transpose(1, 2).to(kind)}
+    if not c["train"]:
+        return out
+    dv = torch.matmul(p.transpose(2, 3), do)
+    dp = torch.matmul(do, v.transpose(2, 3))
+    ds = (dp - (dp * p).sum(-1, keepdim=True)).mul_(p)
+    dq = torch.matmul(ds, k).mul_(scale)
+    dk = torch.matmul(ds.transpose(2, 3), q).mul_(scale)
+    out["dq"] = dq.transpose(1, 2).to(kind)
+    out["dk"] = dk.view(b, kv, group, s, d).sum(2).transpose(1, 2).to(kind)
+    out["dv"] = dv.view(b, kv, group, s, d).sum(2).transpose(1, 2).to(kind)
+    if c["buckets"]:
+        # a row's entries moved so that equal distances share a column, then summed in 64 bits
+        by = torch.nn.functional.pad(ds.sum(0), (s - 1, 0)).view(h, -1)
+        by = torch.nn.functional.pad(by, (0, s)).view(h, s, 2 * s).sum(1, dtype=torch.float64)[:, :-1]
+        at = torch.nn.functional.one_hot(of, c["buckets"]).double()
+        out["dbias"] = torch.matmul(by, at).to(kind)
+    return out
+
+
+def _unit(byte, bias):
+    return torch.exp2((byte.to(torch.int32) - bias).double()).repeat_interleave(BLOCK)
+
+
+def _exponent(x, most, bias):
+    """Per block: the byte of the smallest power of two with |x| <= 1.75 * 2^most of its units."""
+    top = x.abs().view(-1, BLOCK).amax(1)
+    f, e = torch.frexp(top)
+    e = e - 1 - most + (f > 0.875)
+    return torch.where(top > 0, e + bias, 0).clamp(0, 255).to(torch.uint8)
+
+
+def _encode_m(m):
+    exp = _exponent(m, 8, M_BIAS)
+    x = m / _unit(exp, M_BIAS)
+    _, e = torch.frexp(x)
+    grid = torch.exp2((e - 1).clamp(min=-6).double() - 3)
+    return (torch.round(x / grid) * grid).to(torch.float8_e4m3fn).view(torch.uint8), exp
+
+
+def _decode_m(code, exp):
+    return code.view(torch.float8_e4m3fn).double() * _unit(exp, M_BIAS)
+
+
+def _encode_v(v):
+    exp = _exponent(v, 33, V_BIAS)
+    x = v / _unit(exp, V_BIAS)
+    _, e = torch.frexp(x)
+    e = (e - 1).clamp(min=3)                     # below 8 units the format is evenly spaced
+    n = torch.round(x / torch.exp2(e.double() - 3))   # 8 .. 16 (0 .. 8 in the lowest range)
+    code = n + 8 * (e - 3)
+    return torch.where((v > 0) & (code == 0), 1.0, code.double()).to(torch.uint8), exp
+
+
+def _decode_v(code, exp):
+    c = code.to(torch.int32)
+    e, f = c >> 3, c & 7
+    return torch.where(e == 0, f, 8 + f).double() * torch.exp2((e - 1).clamp(min=0).double()) * _unit(exp, V_BIAS)
+
+
+def _f32(x):
+    """A hyperparameter as the 32-bit number that the call takes."""
+    return float(np.float32(x))
+
+
+def _plain_adamw(st):
+    c, eight = st["case"], st["case"]["bits"] == 8
+    b1, b2, lr, eps, wd = (_f32(x) for x in (BETA1, BETA2, LR, EPS, DECAY))
+    wide = torch.float64 if eight else torch.float32
+    g = st["g"].to(wide) * SCALE
+    m = (_decode_m(st["m"], st["m_exp"]) if eight else st["m"]) * b1 + g * (1 - b1)
+    v = (_decode_v(st["v"], st["v_exp"]) if eight else st["v"]) * b2 + g.square() * (1 - b2)
+    p = torch.where(st["decay"], st["p"] * (1 - lr * wd), st["p"])
+    p = p - (m / (torch.sqrt(v / (1 - b2 ** STEP)) + eps) * (lr / (1 - b1 ** STEP))).float()
+    st["p"].copy_(p)
+    if eight:
+        for name, (code, exp) in (("m", _encode_m(m)), ("v", _encode_v(v))):
+            st[name].copy_(code)
+            st[name + "_exp"].copy_(exp)
+    else:
+        st["m"].copy_(m)
+        st["v"].copy_(v)
+    if st["copy"] is not None:
+        st["copy"].copy_(torch.where(st["decay"], p.to(torch.bfloat16), st["copy"]))
+    return _adamw_outputs(st)
+
+
+def _adamw_outputs(st):
+    """Parameters and copies, and the moments as the values that they stand for."""
+    out = {"p": st["p"]}
+    if st["copy"] is not None:
+        out["copy"] = st["copy"]
+    if st["case"]["bits"] == 32:
+        return {**out, "m": st["m"], "v": st["v"]}
+    m = st["m"].view(torch.float8_e4m3fn).float().view(-1, BLOCK) * torch.exp2(st["m_exp"].float() - M_BIAS)[:, None]
+    e, f = st["v"] >> 3, st["v"] & 7
+    v = (torch.where(e == 0, f, 8 + f).float() * torch.exp2((e.float() - 1).clamp(min=0))).view(-1, BLOCK)
+    # the power of two in two factors, each of which 32 bits hold
+    half = torch.exp2(torch.floor((st["v_exp"].float() - V_BIAS) / 2))[:, None]
+    rest = torch.exp2(torch.ceil((st["v_exp"].float() - V_BIAS) / 2))[:, None]
+    return {**out, "m": m.view(-1), "v": (v * half * rest).view(-1)}
+
+
+def run(state):
+    case = state["case"]
+    if case["kind"] == "attention":
+        return _own_attention(state) if own else _plain_attention(state)
+    return _own_adamw(state) if own else _plain_adamw(state)
+
+
+# -- the package's calls ------------------------------------------------------------
+
+
+def _own_attention(st):
+    from paper_2405_14009_amd import attention_backward, attention_forward
+    c = st["case"]
+    how = dict(causal=c["causal"], window=c["window"], sinks=c["sinks"], rel_bias=st["bias"],
+               max_distance=c["max_distance"], lengths=st["lengths"])
+    if not c["train"]:
+        return {"o": attention_forward(st["q"], st["k"], st["v"], save=False, **how)[0]}
+    o, saved = attention_forward(st["q"], st["k"], st["v"], **how)
+    dq, dk, dv, dbias = attention_backward(st["do"], st["q"], st["k"], st["v"], o, saved, **how)
+    out = {"o": o, "dq": dq, "dk": dk, "dv": dv}
+    if dbias is not None:
+        out["dbias"] = dbias
+    return out
+
+
+def _own_adamw(st):
+    from paper_2405_14009_amd import AdamW
+    c = st["case"]
+    if "step" not in st:
+        places, _ = _places(c)
+        tensors = _tensors(c)
+
+        def parts(flat):
+            return [flat[at:at + n] for (n, _), at in zip(tensors, places)]
+
+        def blocks(flat):
+            return [flat[at // BLOCK:at // BLOCK - (-n // BLOCK)] for (n, _), at in zip(tensors, places)]
+
+        eight = c["bits"] == 8
+        copies = None
+        if st["copy"] is not None:
+            copies = [x if matrix else None for x, (_, matrix) in zip(parts(st["copy"]), tensors)]
+        st["step"] = AdamW(parts(st["p"]), parts(st["g"]), decay=[matrix for _, matrix in tensors], copies=copies,
+                           exp_avg=parts(st["m"]), exp_avg_sq=parts(st["v"]),
+                           exp_avg_scale=blocks(st["m_exp"]) if eight else None,
+                           exp_avg_sq_scale=blocks(st["v_exp"]) if eight else None,
+                           lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY)
+    st["step"].step(SCALE, step=STEP)
+    return _adamw_outputs(st)
+
+
+# -- work and exact results -----------------------------------------------------------
+
+
+def _pairs(case):
+    """Visible (i, j) of all sequences of one head."""
+    total = 0
+    for n in _lengths(case):
+        i = np.arange(n, dtype=np.int64)
+        if not case["window"]:
+            total += int((i + 1).sum()) if case["causal"] else n * n
+            continue
+        low, high = np.maximum(i - case["window"] + 1, 0), np.minimum(i + case["window"], n)
+        if case["causal"]:
+            high = i + 1
+        total += int((high - low + np.minimum(low, case["sinks"])).sum())
+        if not case["causal"]:
+            total += int(np.maximum(min(case["sinks"], n) - high, 0).sum())
+    return total
+
+
+def work(case):
+    if case["kind"] == "attention":
+        size = 4 if case["dtype"] == "f32" else 2
+        tokens, d = sum(_lengths(case)), case["dim"]
+        q, kv = tokens * case["heads"] * d * size, tokens * case["kv_heads"] * d * size
+        pairs = _pairs(case) * case["heads"]
+        table = case["heads"] * case["buckets"] * size
+        if not case["train"]:
+            return {"bytes": 2 * q + 2 * kv + table, "flops": 4.0 * d * pairs}
+        # forward: q, k, v to o; backward: q, k, v, o, do to dq, dk, dv
+        return {"bytes": 6 * q + 6 * kv + 3 * table, "flops": 14.0 * d * pairs}
+    each = 8 + (4 if case["grads"] == "f32" else 2) + (16 if case["bits"] == 32 else 4 + 4 / BLOCK)
+    tensors = _tensors(case)
+    copies = 2 * sum(n for n, matrix in tensors if matrix) if case["copies"] else 0
+    n = sum(n for n, _ in tensors)
+    return {"bytes": each * n + copies, "flops": 15.0 * n}
+
+
+def _exact_attention(case, st):
+    b, s, h, kv, d = (case[k] for k in ("batch", "seq", "heads", "kv_heads", "dim"))
+    if 14.0 * d * b * h * s * s > 1.5e13:
+        return None
+    group, lens = h // kv, _lengths(case)
+    names = ("o", "dq", "dk", "dv") if case["train"] else ("o",)
+    full = {"o": h, "dq": h, "dk": kv, "dv": kv}
+    out = {n: torch.zeros(b, s, full[n], d, dtype=torch.float64, device="cuda") for n in names}
+    if case["buckets"]:
+        one = case["buckets"] if case["causal"] else case["buckets"] // 2
+        exact = one // 2
+        table = []
+        for n in range(s):   # the bucket of a distance n, by its definition
+            at = n
+            if n >= exact:
+                at = exact
+                while at + 1 < one and n ** (one - exact) >= (
+                        exact ** (one - at - 1) * case["max_distance"] ** (at + 1 - exact)):
+                    at += 1
+            table.append(at)
+        back = torch.tensor(table, device="cuda")
+        ahead = torch.zeros_like(back) if case["causal"] else back + one
+        if case["train"]:
+            out["dbias"] = torch.zeros(h, case["buckets"], dtype=torch.float64, device="cuda")
+    for at in range(b):
+        n = lens[at]
+        if n == 0:
+            continue
+        i = torch.arange(n, device="cuda").view(-1, 1)
+        j = torch.arange(n, device="cuda").view(1, -1)
+        hide = torch.zeros(n, n, dtype=torch.bool, device="cuda")
+        if case["window"]:
+            hide = (j >= case["sinks"]) & ((i - j >= case["window"]) | (j - i >= case["window"]))
+        if case["causal"]:
+            hide = hide | (j > i)
+        if case["buckets"]:
+            of = torch.where(j > i, ahead[(j - i).clamp(min=0)], back[(i - j).clamp(min=0)])
+        for head in range(h):
+            q, do = st["q"][at, :n, head].double(), st["do"][at, :n, head].double()
+            k, v = st["k"][at, :n, head // group].double(), st["v"][at, :n, head // group].double()
+            x = q @ k.T / math.sqrt(d)
+            if case["buckets"]:
+                x = x + st["bias"][head].double()[of]
+            p = torch.softmax(torch.where(hide, -math.inf, x), 1)
+            o = p @ v
+            out["o"][at, :n, head] = o
+            if not case["train"]:
+                continue
+            dp = do @ v.T
+            ds = p * (dp - (dp * p).sum(1, keepdim=True))   # exactly zero where one token is visible
+            out["dq"][at, :n, head] = ds @ k / math.sqrt(d)
+            out["dk"][at, :n, head // group] += ds.T @ q / math.sqrt(d)
+            out["dv"][at, :n, head // group] += p.T @ do
+            if case["buckets"]:
+                # whole diagonals first, then the few sums by their buckets
+                for side, sign in ((back, -1), (ahead, 1)):
+                    x = ds.tril() if sign < 0 else ds.triu(1)
+                    x = torch.cat((x, torch.zeros(n, n - 1, dtype=x.dtype, device="cuda")), 1).view(-1)
+                    x = torch.cat((x, x.new_zeros(n))).view(n, 2 * n).sum(0)   # column c: j - i = c, or c - 2n
+                    per = x[:n] if sign > 0 else torch.cat((x[:1], x.flip(0)[:n - 1]))
+                    out["dbias"][head].index_put_((side[:n],), per, accumulate=True)
+    return out
+
+
+def _nearest(x, values):
+    """Index of the value nearest to each x (ties: the even index) in an ascending table."""
+    high = torch.searchsorted(values, x.contiguous()).clamp(1, values.numel() - 1)
+    low = high - 1
+    down, up = x - values[low], values[high] - x
+    return torch.where((down < up) | ((down == up) & (low % 2 == 0)), low, high)
+
+
+def _exact_adamw(case, st):
+    eight = case["bits"] == 8
+    tm = [(k & 7) / 512 if k < 8 else (8 + (k & 7)) * 2.0 ** ((k >> 3) - 10) for k in range(127)]
+    tv = [float(k) if k < 8 else (8.0 + (k & 7)) * 2.0 ** ((k >> 3) - 1) for k in range(255)]
+    tm, tv = (torch.tensor(t, dtype=torch.float64, device="cuda") for t in (tm, tv))
+    b1, b2, lr, eps, wd = (_f32(x) for x in (BETA1, BETA2, LR, EPS, DECAY))
+    n = st["p"].numel()
+    out = {k: torch.empty(n, dtype=torch.float64, device="cuda") for k in ("p", "m", "v")}
+    if st["copy"] is not None:
+        out["copy"] = torch.zeros(n, dtype=torch.float64, device="cuda")
+
+    def rounded(x, table, bias):
+        rows = x.view(-1, BLOCK)
+        e = torch.ceil(torch.log2(rows.abs().amax(1) / table[-1])).nan_to_num(neginf=-bias)
+        e = torch.where(rows.abs().amax(1) > table[-1] * torch.exp2(e), e + 1, e)
+        e = torch.where(rows.abs().amax(1) <= table[-1] * torch.exp2(e - 1), e - 1, e).clamp(-bias, 255 - bias)
+        unit = torch.exp2(e)[:, None]
+        code = _nearest(rows.abs() / unit, table)
+        if bias == V_BIAS:
+            code = torch.where((rows > 0) & (code == 0), 1, code)
+        return (table[code] * torch.sign(rows) * unit).view(-1)
+
+    many = 1 << 25
+    for at in range(0, n, many):
+        to = slice(at, min(n, at + many))
+        rows = slice(at // BLOCK, min(n, at + many) // BLOCK)
+        m, v, g = st["m"][to], st["v"][to], st["g"][to].double() * SCALE
+        if eight:
+            sign = torch.where(m >= 128, -1.0, 1.0).double()
+            m = (tm[(m & 127).long()] * sign).view(-1, BLOCK) * 2.0 ** (st["m_exp"][rows].double() - M_BIAS)[:, None]
+            v = tv[v.long()].view(-1, BLOCK) * 2.0 ** (st["v_exp"][rows].double() - V_BIAS)[:, None]
+        m = b1 * m.double().view(-1) + (1 - b1) * g
+        v = b2 * v.double().view(-1) + (1 - b2) * g * g
+        p = st["p"][to].double()
+        p = torch.where(st["decay"][to], p - lr * wd * p, p)
+        p = p - lr * (m / (1 - b1 ** STEP)) / ((v / (1 - b2 ** STEP)).sqrt() + eps)
+        out["p"][to] = p
+        out["m"][to] = rounded(m, tm, M_BIAS) if eight else m
+        out["v"][to] = rounded(v, tv, V_BIAS) if eight else v
+        if "copy" in out:
+            out["copy"][to] = torch.where(st["decay"][to], p, 0.0)
+    return out
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    return (_exact_attention if case["kind"] == "attention" else _exact_adamw)(case, st)
