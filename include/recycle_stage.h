@@ -370,6 +370,115 @@ rc_status rc_stage_synchronize(rc_stage* st);
 /* Message for the last non-OK status on the calling thread ("" if none). */
 const char* rc_last_error(void);
 
+/* ---- Operators on the caller's tensors ---------------------------------- */
+
+/* What a stage computes inside, and what a program around it needs on tensors
+ * of its own (other layers' attention, embeddings, final norms and heads).
+ * The calls enqueue kernels on hip_stream (a hipStream_t, NULL = the null
+ * stream of the current device) and return; they allocate nothing, keep
+ * nothing and may be captured into a graph.  All memory is the caller's, on
+ * the device of the stream, and has to stay valid until the stream has
+ * passed the call.  Two calls may run at once if they share no output, saved
+ * or work memory. */
+
+/* A [batch, token, head, head_dim] tensor: strides in elements, head_dim
+ * contiguous.  data and all strides are multiples of 16 bytes. */
+typedef struct rc_view {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} rc_view;
+
+/* Attention of batch sequences over themselves.  Token j is visible to token
+ * i of the same sequence when
+ *   j < length  and  i < length  (length of the sequence: below),
+ *   causal:  j <= i,  and
+ *   window:  |i - j| < window, or j < sinks  (window 0: no such condition).
+ * o_i = sum_j P_ij v_j, P_ij = softmax over the visible j of
+ *   scale q_i.k_j + bias[head, bucket(j - i)].
+ * Tokens at or behind their sequence's length have o = 0 and gradients of 0, and
+ * nothing of theirs is read.
+ *
+ * Query head h reads key / value head h / (heads / kv_heads).
+ *
+ * buckets > 0: a learned relative position bias [heads, buckets].  With n =
+ * i - j (causal) or |i - j| and B = buckets (causal) or buckets / 2, of which
+ * the second half is for j > i: distances below E = B / 2 have a bucket each,
+ * the others share E + floor((B - E) log(n / E) / log(max_distance / E)), at
+ * most B - 1 (decided in whole numbers, without rounding).
+ *
+ * Requirements (otherwise RC_ERR_UNSUPPORTED): head_dim a multiple of 8, at
+ * most 128; buckets at most 128, max_distance at most 1024; seq_len at most
+ * 2^24; bf16: a head's tokens span less than 2^31 bytes in every tensor. */
+typedef struct rc_attention {
+  int32_t dtype;        /* rc_dtype of q, k, v, o and their gradients */
+  int32_t batch, seq_len, heads, kv_heads, head_dim;
+  int32_t causal, window, sinks;
+  int32_t buckets, max_distance;  /* 0, 0: no bias */
+  int32_t bias_dtype;   /* rc_dtype of the bias and its gradient */
+  float scale;          /* of the products, above zero */
+} rc_attention;
+
+/* Bytes of `saved` (written by the forward for the backward: row statistics
+ * and, bf16, what the rounding of o drops) and of the backward's `work`; both
+ * are 256-byte aligned.  Host only.  Errors: RC_ERR_INVALID_ARG, RC_ERR_UNSUPPORTED. */
+rc_status rc_attention_memory(const rc_attention* a, size_t* saved_bytes, size_t* work_bytes);
+
+/* o = attention(q, k, v).  bias: device [heads, buckets] (NULL without).
+ * lengths: device int32 [batch], or NULL when every sequence has seq_len
+ * tokens; values outside 0 .. seq_len are taken as the nearer end.  saved: NULL
+ * when no backward follows.  o overlaps no input.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_UNSUPPORTED, RC_ERR_HIP. */
+rc_status rc_attention_forward(const rc_attention* a, const rc_view* q, const rc_view* k,
+                               const rc_view* v, const void* bias, const int32_t* lengths,
+                               const rc_view* o, void* saved, void* hip_stream);
+
+/* Gradients of sum(dout o): dq, dk, dv (all of their elements are written) and,
+ * with a bias, dbias [heads, buckets], from the forward's o and saved.  Every sum
+ * has a fixed order: results are bitwise reproducible.  No output overlaps
+ * another tensor of the call.
+ * Errors: as rc_attention_forward. */
+rc_status rc_attention_backward(const rc_attention* a, const rc_view* q, const rc_view* k,
+                                const rc_view* v, const void* bias, const int32_t* lengths,
+                                const rc_view* o, const void* saved, const rc_view* dout,
+                                const rc_view* dq, const rc_view* dk, const rc_view* dv,
+                                void* dbias, void* work, void* hip_stream);
+
+/* One tensor of an AdamW step.  Its arrays are contiguous and have `count`
+ * elements; pointers need only the alignment of their elements (aligned to 16
+ * bytes they are read faster).
+ * 32-bit moments: exp_avg and exp_avg_sq are fp32, both scales NULL.
+ * 8-bit moments: one byte an element, and a byte for each 128 consecutive
+ * elements (the last block may be shorter) in the scales:
+ *   exp_avg     e4m3 codes in units of 2^(scale - 127);
+ *   exp_avg_sq  unsigned codes in units of 2^(scale - 160): code c stands for c
+ *               below 8, for (8 + c % 8) 2^(c / 8 - 1) up to 254, for NaN at 255.
+ * All zeros is the state before the first step, in both forms. */
+typedef struct rc_adamw_tensor {
+  float* param;
+  const void* grad;
+  void* exp_avg;
+  void* exp_avg_sq;
+  uint8_t* exp_avg_scale;
+  uint8_t* exp_avg_sq_scale;
+  void* copy;           /* bf16 copy of the updated parameter, or NULL */
+  int64_t count;
+  int32_t grad_dtype;   /* rc_dtype */
+  int32_t decay;        /* whether weight decay applies */
+} rc_adamw_tensor;
+
+/* AdamW step number `step` (1 for the first) over n tensors in as few launches
+ * as their descriptors take, as rc_stage_optimizer_step does it over a stage's
+ * parameters.  tensors: host array, read before the call returns.  No array of
+ * a tensor overlaps another array of the call.  state_bits: 32 or 8.  With 8
+ * the moments are formed in 64 bits from their codes, the update uses them
+ * unrounded, and then they are rounded to codes again: to nearest, ties to
+ * even, a second moment above zero to no code below 1, one that fp32 does not
+ * hold to NaN; a block takes the smallest power of two that its other moments
+ * fit.  Tensors without elements are skipped.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_HIP. */
+rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam_config* adam,
+                        int32_t state_bits, int64_t step, float grad_scale, void* hip_stream);
+
 /* ---- Schedule side (host only, no device work) ------------------------- */
 
 /* Failure Normalization (section 4.2.1, Algorithm 1): assign `failures`

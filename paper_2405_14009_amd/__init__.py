@@ -10,4 +10,5 @@ from ._lib import (  # noqa: F401
     RC_READ_ADAM_V, RC_READ_GRAD,
     RC_READ_PARAM, LIB_PATH, load,
 )
+from .operators import AdamW, attention_backward, attention_forward  # noqa: F401
 from .stage import PARAM_NAMES, Stage, param_shape  # noqa: F401

@@ -29,6 +29,7 @@ EXPORTED = (
     "rc_stage_stash_usage", "rc_stage_set_stream", "rc_stage_attention_kernels",
     "rc_stage_synchronize", "rc_stage_profile_enable", "rc_stage_profile_read", "rc_last_error",
     "rc_failure_normalization", "rc_schedule_simulate",
+    "rc_attention_memory", "rc_attention_forward", "rc_attention_backward", "rc_adamw_step",
 )
 
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "layernorm",
@@ -68,6 +69,26 @@ class RcKernelStat(ctypes.Structure):
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
 
 
+class RcView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class RcAttention(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("seq_len", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32),
+                ("bias_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class RcAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p),
+                ("exp_avg_sq", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p),
+                ("exp_avg_sq_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("count", ctypes.c_int64), ("grad_dtype", ctypes.c_int32), ("decay", ctypes.c_int32)]
+
+
 class RcError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"[{_NAMES.get(status, status)}] {msg}")
@@ -102,6 +123,7 @@ def load() -> ctypes.CDLL:
     P, I32, F32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
     cfgp = ctypes.POINTER(RcStageConfig)
     sz = ctypes.POINTER(ctypes.c_size_t)
+    view = ctypes.POINTER(RcView)
     sig = {
         "rc_stage_memory_requirements": [cfgp, sz, sz, sz],
         "rc_stage_create": [cfgp, ctypes.POINTER(RcAdamConfig), I32, I32, P, P, P, P,
@@ -131,6 +153,12 @@ def load() -> ctypes.CDLL:
         "rc_stage_profile_read": [P, ctypes.POINTER(RcKernelStat)],
         "rc_failure_normalization": [I32, I32, I32, I32, ctypes.POINTER(I32), ctypes.POINTER(ctypes.c_int64)],
         "rc_schedule_simulate": [P, P, P, I32, ctypes.POINTER(I32)],
+        "rc_attention_memory": [ctypes.POINTER(RcAttention), sz, sz],
+        "rc_attention_forward": [ctypes.POINTER(RcAttention), view, view, view, P, P, view, P, P],
+        "rc_attention_backward": [ctypes.POINTER(RcAttention), view, view, view, P, P, view, P, view,
+                                  view, view, view, P, P, P],
+        "rc_adamw_step": [ctypes.POINTER(RcAdamwTensor), I32, ctypes.POINTER(RcAdamConfig), I32,
+                          ctypes.c_int64, F32, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)

@@ -1,0 +1,62 @@
+// Attention with a sliding window, sinks and a relative position bias: the
+// arguments of its kernels and their launchers.  See attn_op_kernels.h.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+// Distances in tokens at which the last bucket of a side has to begin at the latest.
+constexpr int ATTN_OP_MAX_FAR = 1024;
+constexpr int ATTN_OP_MAX_BUCKETS = 128;
+
+// [batch, token, head, head_dim] in elements; the head_dim elements are contiguous.
+struct AttnOpView {
+  void* p;
+  long b, t, h;
+};
+
+struct AttnOpArgs {
+  AttnOpView q, k, v, o, dout, dq, dk, dv;
+  const int* lengths;  // tokens of each sequence, or null: all s
+  int batch, s, spad, heads, kv_heads, group, d;
+  // token j is in the window of token i iff -left <= j - i <= right
+  int causal, left, right, sinks;
+  float scale, sl2;  // of the products, and with log2(e)
+  // relative position bias [heads, buckets]; distances of `far` or more share
+  // the last bucket of their side
+  const void* bias;
+  int bias_f32, buckets, far;
+  // row statistics [batch, heads, spad]: reference score and log2 of the sum of
+  // exponentials relative to it (base 2), and (bf16) what the rounding of o drops
+  float *m, *l;
+  void* rest;
+  float* drow;   // [batch, heads, spad] rowsum(dO o O)
+  float* bpart;  // [batch * heads * query blocks, buckets] shares of the bias gradient
+  void* dbias;
+  // key blocks that hold sinks are seen by every query: their queries are
+  // split into chunks, whose shares of dK and dV are added up afterwards
+  float* spart;
+  int sink_blocks, chunks, chunk_len;
+  unsigned short first[ATTN_OP_MAX_BUCKETS];  // first distance of each bucket of a side
+  unsigned char bucket[ATTN_OP_MAX_FAR];      // of distances below `far`, one side
+};
+
+#define ATTN_OP_DECL(NAME)                                        \
+  hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st); \
+  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st);
+ATTN_OP_DECL(bf16_32)
+ATTN_OP_DECL(bf16_64)
+ATTN_OP_DECL(bf16_96)
+ATTN_OP_DECL(bf16_128)
+ATTN_OP_DECL(f32_64)
+ATTN_OP_DECL(f32_128)
+#undef ATTN_OP_DECL
+
+// What one attention needs, in bytes, and its launches.  The arguments' scratch
+// pointers are set from `saved` (null: nothing is kept for a backward pass) and
+// `work`.
+size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt);
+size_t attn_op_work_bytes(const AttnOpArgs& a, int elt);
+void attn_op_plan(AttnOpArgs& a, int window, int max_distance);
+hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st);
+hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work, hipStream_t st);

@@ -1,0 +1,163 @@
+// Host side of the attention operator: scratch memory, buckets, launches; and
+// the sum of the bias gradient's shares.
+#include <cmath>
+#include <cstring>
+#include <vector>
+
+#include "attn_op.h"
+#include "common.h"
+
+namespace {
+
+// x^n as 32-bit words, lowest first.
+std::vector<uint32_t> power(uint32_t x, int n, std::vector<uint32_t> r = {1}) {
+  for (; n > 0; --n) {
+    uint64_t carry = 0;
+    for (uint32_t& w : r) {
+      carry += (uint64_t)w * x;
+      w = (uint32_t)carry;
+      carry >>= 32;
+    }
+    if (carry) r.push_back((uint32_t)carry);
+  }
+  return r;
+}
+
+bool at_least(const std::vector<uint32_t>& a, const std::vector<uint32_t>& b) {
+  if (a.size() != b.size()) return a.size() > b.size();
+  for (size_t i = a.size(); i-- > 0;)
+    if (a[i] != b[i]) return a[i] > b[i];
+  return true;
+}
+
+// First distance of bucket exact + step, of k logarithmic buckets that start at
+// `exact` and reach max_distance: the smallest n with
+//   n^k >= exact^(k - step) max_distance^step,
+// estimated by logarithms, which decide unless n is at the border to their rounding.
+int border(int exact, int k, int max_distance, int step) {
+  const double t = std::log((double)exact) + (double)step / k * std::log((double)max_distance / exact);
+  const double x = std::exp(t);
+  const int near = (int)std::lround(x);
+  if (std::fabs(x - near) > 1e-6 * x) return (int)std::ceil(x);
+  const auto want = power((uint32_t)max_distance, step, power((uint32_t)exact, k - step));
+  return at_least(power((uint32_t)near, k), want) ? near : near + 1;
+}
+
+// dbias[h, c] = sum of the shares of head h in the order of (sequence, query
+// block): sixteen or fewer groups of threads take every g-th share, then add up.
+template <class E>
+__global__ __launch_bounds__(256) void attn_op_dbias_k(const float* part, E* out, int batch, int heads, int nqb,
+                                                       int buckets) {
+  __shared__ float red[256];
+  const int h = blockIdx.x, groups = 256 / buckets, g = threadIdx.x / buckets, c = threadIdx.x % buckets;
+  float t = 0.f;
+  if (g < groups)
+    for (int i = g; i < batch * nqb; i += groups)
+      t += part[(((long)(i / nqb) * heads + h) * nqb + i % nqb) * buckets + c];
+  red[threadIdx.x] = t;
+  __syncthreads();
+  if (g != 0) return;
+  for (int k = 1; k < groups; ++k) t += red[k * buckets + c];
+  out[(long)h * buckets + c] = (E)t;
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+int columns(int elt, int d) { return elt == 2 && d <= 32 ? 32 : d <= 64 ? 64 : elt == 2 && d <= 96 ? 96 : 128; }
+
+size_t rows(const AttnOpArgs& a) { return (size_t)a.batch * a.heads * a.spad; }
+
+}  // namespace
+
+// Fills what follows from the sizes: the window, buckets and the chunks of sink blocks.
+void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
+  const int far = 1 << 30;
+  a.spad = (a.s + 63) / 64 * 64;
+  a.group = a.heads / a.kv_heads;
+  a.sl2 = a.scale * 1.4426950408889634f;
+  if (window >= a.s) window = 0;
+  a.left = window ? window - 1 : far;
+  a.right = a.causal ? 0 : a.left;
+  if (!window) a.sinks = 0;
+  a.sinks = a.sinks < a.s ? a.sinks : a.s;
+  if (a.buckets) {
+    const int side = a.causal ? a.buckets : a.buckets / 2, exact = side / 2, k = side - exact;
+    for (int c = 0; c < side; ++c)
+      a.first[c] = (unsigned short)(c <= exact ? c : border(exact, k, max_distance, c - exact));
+    a.far = a.first[side - 1];
+    for (int n = 0, c = 0; n < a.far; ++n) {
+      while (c + 1 < side && a.first[c + 1] <= n) ++c;
+      a.bucket[n] = (unsigned char)c;
+    }
+  }
+  // Every query sees the sinks: their key blocks' queries go in chunks of about
+  // what another key block sees.
+  a.sink_blocks = (a.sinks + 127) / 128;
+  a.chunk_len = (((a.causal ? 1 : 2) * window + 128 + 63) / 64) * 64;
+  if (a.chunk_len < 512) a.chunk_len = 512;
+  a.chunks = a.sink_blocks ? (a.s + a.chunk_len - 1) / a.chunk_len : 1;
+}
+
+size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
+  return 2 * align256(4 * rows(a)) + (elt == 2 ? align256(2 * (size_t)a.batch * a.s * a.heads * a.d) : 0);
+}
+
+size_t attn_op_work_bytes(const AttnOpArgs& a, int elt) {
+  size_t n = align256(4 * rows(a));
+  if (a.buckets) n += align256(4 * (size_t)a.batch * a.heads * ((a.s + 127) / 128) * a.buckets);
+  if (a.chunks > 1)
+    n += align256(4 * (size_t)a.batch * a.kv_heads * a.sink_blocks * a.chunks * 2 * 128 * columns(elt, a.d));
+  return n;
+}
+
+namespace {
+
+void set_saved(AttnOpArgs& a, const void* saved) {
+  char* p = (char*)saved;
+  a.m = a.l = nullptr;
+  a.rest = nullptr;
+  if (!p) return;
+  a.m = (float*)p;
+  a.l = (float*)(p + align256(4 * rows(a)));
+  a.rest = p + 2 * align256(4 * rows(a));
+}
+
+}  // namespace
+
+hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st) {
+  set_saved(a, saved);
+  const int c = columns(elt, a.d);
+  if (elt == 4) return c == 64 ? attn_op_fwd_f32_64(a, st) : attn_op_fwd_f32_128(a, st);
+  return c == 32   ? attn_op_fwd_bf16_32(a, st)
+         : c == 64 ? attn_op_fwd_bf16_64(a, st)
+         : c == 96 ? attn_op_fwd_bf16_96(a, st)
+                   : attn_op_fwd_bf16_128(a, st);
+}
+
+hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work, hipStream_t st) {
+  set_saved(a, saved);
+  const int nqb = (a.s + 127) / 128;
+  char* w = (char*)work;
+  a.drow = (float*)w;
+  w += align256(4 * rows(a));
+  a.bpart = (float*)w;
+  if (a.buckets) w += align256(4 * (size_t)a.batch * a.heads * nqb * a.buckets);
+  a.spart = (float*)w;
+  const int c = columns(elt, a.d);
+  hipError_t e;
+  if (elt == 4)
+    e = c == 64 ? attn_op_bwd_f32_64(a, st) : attn_op_bwd_f32_128(a, st);
+  else
+    e = c == 32   ? attn_op_bwd_bf16_32(a, st)
+        : c == 64 ? attn_op_bwd_bf16_64(a, st)
+        : c == 96 ? attn_op_bwd_bf16_96(a, st)
+                  : attn_op_bwd_bf16_128(a, st);
+  if (e != hipSuccess || !a.bias) return e;
+  if (a.bias_f32)
+    hipLaunchKernelGGL(attn_op_dbias_k<float>, dim3(a.heads), dim3(256), 0, st, a.bpart, (float*)a.dbias, a.batch,
+                       a.heads, nqb, a.buckets);
+  else
+    hipLaunchKernelGGL(attn_op_dbias_k<bf16>, dim3(a.heads), dim3(256), 0, st, a.bpart, (bf16*)a.dbias, a.batch,
+                       a.heads, nqb, a.buckets);
+  return hipGetLastError();
+}

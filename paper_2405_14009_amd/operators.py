@@ -1,0 +1,252 @@
+"""Operators on the caller's tensors (see include/recycle_stage.h): attention
+with a sliding window, sinks and a relative position bias, and an AdamW step
+over many tensors.
+
+Argument marshalling only: every step runs in the HIP library.  The calls
+enqueue on PyTorch's current stream of the tensors' device and take their
+outputs and scratch memory from PyTorch, so they may be captured into a graph.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import math
+from typing import Optional, Sequence
+
+from . import _lib as L
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _kind(t, name):
+    """The library's dtype of a tensor."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype == torch.bfloat16:
+        return L.RC_BF16
+    if t.dtype == torch.float32:
+        return L.RC_FP32
+    raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+
+
+def _same(t, name, like, shape):
+    """Checks a tensor that goes with `like`; a view of it."""
+    if _kind(t, name) != _kind(like, "q") or t.device != like.device:
+        raise ValueError(f"{name} must have the type and device of q")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    return _view(t, name)
+
+
+def _view(t, name):
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be [batch, tokens, heads, head_dim]")
+    b, s, h, d = t.stride()
+    if d != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the elements of a head must be contiguous")
+    # the stride of a dimension of one element says nothing: any will do
+    b, s, h = (x if n > 1 else 0 for x, n in zip((b, s, h), t.shape))
+    return L.RcView(t.data_ptr(), b, s, h)
+
+
+def _on(device):
+    """The device as PyTorch's current one, and its stream."""
+    torch = _torch()
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext(), torch.cuda.current_stream(device)
+    return torch.cuda.device(device), torch.cuda.current_stream(device)
+
+
+class _Call:
+    """What a forward and a backward call have in common."""
+
+    def __init__(self, q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale):
+        torch = _torch()
+        kind = _kind(q, "q")
+        if q.dim() != 4:
+            raise ValueError("q must be [batch, tokens, heads, head_dim]")
+        batch, seq, heads, d = q.shape
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("k must be [batch, tokens, kv_heads, head_dim]")
+        kv = k.shape[2]
+        self.shape, self.kv_shape = (batch, seq, heads, d), (batch, seq, kv, d)
+        self.q, self.k, self.v = _view(q, "q"), _same(k, "k", q, self.kv_shape), _same(v, "v", q, self.kv_shape)
+        self.bias = self.lengths = None
+        buckets, bias_kind = 0, L.RC_FP32
+        if rel_bias is not None:
+            bias_kind = _kind(rel_bias, "rel_bias")
+            if rel_bias.dim() != 2 or rel_bias.shape[0] != heads or rel_bias.shape[1] < 1:
+                raise ValueError(f"rel_bias must be [{heads}, buckets]")
+            if not rel_bias.is_contiguous() or rel_bias.device != q.device:
+                raise ValueError("rel_bias must be contiguous and on the device of q")
+            buckets = rel_bias.shape[1]
+            self.bias = ctypes.c_void_p(rel_bias.data_ptr())
+        if lengths is not None:
+            if not isinstance(lengths, torch.Tensor) or lengths.device != q.device:
+                raise TypeError("lengths must be a tensor on the device of q")
+            if lengths.dtype != torch.int32 or tuple(lengths.shape) != (batch,) or not lengths.is_contiguous():
+                raise ValueError(f"lengths must be a contiguous int32 tensor of {batch}")
+            self.lengths = ctypes.c_void_p(lengths.data_ptr())
+        if scale is None:
+            scale = 1.0 / math.sqrt(d) if d else 0.0
+        self.c = L.RcAttention(kind, batch, seq, heads, kv, d, 1 if causal else 0, int(window), int(sinks),
+                               buckets, int(max_distance) if buckets else 0, bias_kind, scale)
+        self.lib = L.load()
+        saved, work = ctypes.c_size_t(), ctypes.c_size_t()
+        L.check(self.lib.rc_attention_memory(ctypes.byref(self.c), ctypes.byref(saved), ctypes.byref(work)))
+        self.saved_bytes, self.work_bytes = saved.value, work.value
+
+
+def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: int = 0, rel_bias=None,
+                      max_distance: int = 128, lengths=None, scale: Optional[float] = None, save: bool = True,
+                      out=None):
+    """Attention of sequences over themselves: (o, saved).
+
+    q: [batch, tokens, heads, d], k and v: [batch, tokens, kv_heads, d], bf16 or
+    fp32, any strides of 16-byte multiples.  Token j is visible to token i when
+    it lies within the sequence's length (lengths: int32 [batch]), does not
+    follow i (causal), and is one of the first `sinks` tokens or less than
+    `window` away (0: no window).  rel_bias: [heads, buckets], added to the
+    scores by the bucket of the distance (the last one from about max_distance
+    on).  scale: 1 / sqrt(d) unless given.  saved: what attention_backward needs,
+    None with save=False.  out: a tensor for o."""
+    torch = _torch()
+    c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
+    ctx, stream = _on(q.device)
+    with ctx:
+        o = torch.empty(c.shape, dtype=q.dtype, device=q.device) if out is None else out
+        ov = _same(o, "out", q, c.shape)
+        saved = torch.empty(c.saved_bytes, dtype=torch.uint8, device=q.device) if save else None
+        L.check(c.lib.rc_attention_forward(
+            ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
+            ctypes.byref(ov), ctypes.c_void_p(saved.data_ptr() if save else None),
+            ctypes.c_void_p(stream.cuda_stream)))
+    return o, saved
+
+
+def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: int = 0, sinks: int = 0,
+                       rel_bias=None, max_distance: int = 128, lengths=None, scale: Optional[float] = None,
+                       dq=None, dk=None, dv=None):
+    """Gradients of sum(dout * o): (dq, dk, dv, drel_bias), the last None without
+    a bias and of its type otherwise.  o and saved are attention_forward's for the
+    same arguments; dq, dk, dv: tensors for the gradients (all of their elements
+    are written)."""
+    torch = _torch()
+    c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
+    if not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device:
+        raise ValueError("saved must be what attention_forward returned for these arguments")
+    ov, dov = _same(o, "o", q, c.shape), _same(dout, "dout", q, c.shape)
+    ctx, stream = _on(q.device)
+    with ctx:
+        def given(t, name, shape):
+            t = torch.empty(shape, dtype=q.dtype, device=q.device) if t is None else t
+            return t, _same(t, name, q, shape)
+
+        (dq, dqv), (dk, dkv), (dv, dvv) = given(dq, "dq", c.shape), given(dk, "dk", c.kv_shape), given(
+            dv, "dv", c.kv_shape)
+        dbias = None if rel_bias is None else torch.empty_like(rel_bias)
+        work = torch.empty(c.work_bytes, dtype=torch.uint8, device=q.device)
+        L.check(c.lib.rc_attention_backward(
+            ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
+            ctypes.byref(ov), ctypes.c_void_p(saved.data_ptr()), ctypes.byref(dov), ctypes.byref(dqv),
+            ctypes.byref(dkv), ctypes.byref(dvv), None if dbias is None else ctypes.c_void_p(dbias.data_ptr()),
+            ctypes.c_void_p(work.data_ptr()), ctypes.c_void_p(stream.cuda_stream)))
+    return dq, dk, dv, dbias
+
+
+class AdamW:
+    """AdamW over a fixed set of tensors, all of them in one call.
+
+    params: fp32 tensors; grads: fp32 or bf16 tensors of their sizes, read at each
+    step.  decay: whether weight decay applies, by tensor (default: all).
+    copies: bf16 tensors that receive the updated parameters, or None, by tensor.
+    The moments are exp_avg and exp_avg_sq, by tensor: fp32, or with
+    state_bits=8 bytes of codes, with exp_avg_scale and exp_avg_sq_scale a byte
+    per 128 elements.  Moments that are not given start at zero (state_bits
+    then says which form they have).  Every tensor is contiguous; all are kept
+    and updated in place."""
+
+    def __init__(self, params: Sequence, grads: Sequence, *, decay: Optional[Sequence[bool]] = None,
+                 copies: Optional[Sequence] = None, state_bits: Optional[int] = None, exp_avg=None,
+                 exp_avg_sq=None, exp_avg_scale=None, exp_avg_sq_scale=None, lr: float = 1e-4,
+                 beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8, weight_decay: float = 0.1):
+        torch = _torch()
+        self._lib = L.load()
+        self.params, self.grads = list(params), list(grads)
+        n = len(self.params)
+        if state_bits is None:
+            state_bits = 32 if exp_avg_scale is None else 8
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.state_bits, self.steps = state_bits, 0
+        given = [x is not None for x in (exp_avg, exp_avg_sq)]
+        scales = [x is not None for x in (exp_avg_scale, exp_avg_sq_scale)]
+        if given[0] != given[1] or scales[0] != scales[1] or scales[0] != (given[0] and state_bits == 8):
+            raise ValueError("moments are given with their scales (8 bits) or without (32), or not at all")
+        kind = torch.uint8 if state_bits == 8 else torch.float32
+        for i, p in enumerate(self.params):
+            if not isinstance(p, torch.Tensor) or p.device.type != "cuda":
+                raise TypeError(f"params[{i}] must be a device tensor")
+
+        def zeros(size):
+            return [torch.zeros(size(p.numel()), dtype=kind, device=p.device) for p in self.params]
+
+        def blocks(count):
+            return -(-count // 128)
+
+        self.exp_avg = list(exp_avg) if given[0] else zeros(lambda c: c)
+        self.exp_avg_sq = list(exp_avg_sq) if given[0] else zeros(lambda c: c)
+        self.exp_avg_scale = self.exp_avg_sq_scale = None
+        if state_bits == 8:
+            self.exp_avg_scale = list(exp_avg_scale) if given[0] else zeros(blocks)
+            self.exp_avg_sq_scale = list(exp_avg_sq_scale) if given[0] else zeros(blocks)
+        self.copies = [None] * n if copies is None else list(copies)
+        self.decay = [True] * n if decay is None else [bool(x) for x in decay]
+        self.adam = L.RcAdamConfig(lr, beta1, beta2, eps, weight_decay)
+        self.device = self.params[0].device if n else None
+
+        def pointer(lists, i, name, types, count):
+            if len(lists) != n:
+                raise ValueError(f"{name} must have {n} entries")
+            t = lists[i]
+            if not isinstance(t, torch.Tensor) or t.device != self.device:
+                raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
+            if t.dtype not in types or t.numel() != count or not t.is_contiguous():
+                raise ValueError(f"{name}[{i}] must be a contiguous tensor of {count} elements of "
+                                 f"{' or '.join(str(x) for x in types)}")
+            return t.data_ptr()
+
+        if len(self.decay) != n or len(self.copies) != n or len(self.grads) != n:
+            raise ValueError(f"grads, decay and copies must have {n} entries")
+        self._tensors = (L.RcAdamwTensor * max(1, n))()
+        f32, bf16 = torch.float32, torch.bfloat16
+        for i in range(n):
+            t, count = self._tensors[i], self.params[i].numel()
+            t.param = pointer(self.params, i, "params", (f32,), count)
+            t.grad = pointer(self.grads, i, "grads", (f32, bf16), count)
+            t.exp_avg = pointer(self.exp_avg, i, "exp_avg", (kind,), count)
+            t.exp_avg_sq = pointer(self.exp_avg_sq, i, "exp_avg_sq", (kind,), count)
+            if state_bits == 8:
+                t.exp_avg_scale = pointer(self.exp_avg_scale, i, "exp_avg_scale", (kind,), blocks(count))
+                t.exp_avg_sq_scale = pointer(self.exp_avg_sq_scale, i, "exp_avg_sq_scale", (kind,), blocks(count))
+            if self.copies[i] is not None:
+                t.copy = pointer(self.copies, i, "copies", (bf16,), count)
+            t.count, t.decay = count, self.decay[i]
+            t.grad_dtype = L.RC_BF16 if self.grads[i].dtype == bf16 else L.RC_FP32
+
+    def step(self, grad_scale: float = 1.0, *, step: Optional[int] = None) -> None:
+        """One step with grad_scale * grads, as step number `step` (by default one
+        more than the last).  A captured step replays its own number."""
+        number = self.steps + 1 if step is None else int(step)
+        if not self.params:
+            self.steps = number
+            return
+        ctx, stream = _on(self.device)
+        with ctx:
+            L.check(self._lib.rc_adamw_step(self._tensors, len(self.params), ctypes.byref(self.adam), self.state_bits,
+                                            number, float(grad_scale), ctypes.c_void_p(stream.cuda_stream)))
+        self.steps = number

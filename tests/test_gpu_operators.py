@@ -1,0 +1,430 @@
+"""The operators on the caller's tensors against their plain 64-bit forms, at
+the sizes, masks and layouts where they can go wrong."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from tests import operators_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no HIP device")
+
+
+def ops():
+    import paper_2405_14009_amd as pkg
+    return pkg
+
+
+def normal(seed, *shape, std=1.0, mean=0.0, kind=BF16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * std + mean).to(kind).cuda()
+
+
+def inputs(b, s, h, kv, d, kind=BF16, seed=1):
+    return dict(q=normal(seed, b, s, h, d, kind=kind), k=normal(seed + 1, b, s, kv, d, kind=kind),
+                v=normal(seed + 2, b, s, kv, d, mean=0.3, kind=kind)), normal(seed + 3, b, s, h, d, std=0.1, kind=kind)
+
+
+def run(t, do, **how):
+    o, saved = ops().attention_forward(t["q"], t["k"], t["v"], **how)
+    dq, dk, dv, dbias = ops().attention_backward(do, t["q"], t["k"], t["v"], o, saved, **how)
+    got = dict(o=o, dq=dq, dk=dk, dv=dv)
+    if dbias is not None:
+        got["dbias"] = dbias
+    return got
+
+
+def compare(t, do, got, **how):
+    bias = how.pop("rel_bias", None)
+    out, mag = ref.attention(t["q"], t["k"], t["v"], do, bias=bias, **how)
+    return ref.check_attention(got, out, mag, t["q"].dtype, None if bias is None else bias.dtype)
+
+
+# b, s, heads, kv heads, d, causal, window, sinks, buckets, max_distance, lengths
+CASES = [
+    (1, 1, 1, 1, 8, True, 0, 0, 0, 0, None),             # one token
+    (2, 1, 3, 1, 64, False, 1, 1, 8, 16, None),
+    (1, 2, 2, 2, 128, True, 1, 0, 0, 0, None),           # every token sees itself only
+    (1, 63, 4, 4, 32, True, 7, 0, 0, 0, None),
+    (1, 64, 2, 1, 128, True, 64, 3, 0, 0, None),
+    (2, 65, 4, 2, 64, True, 17, 4, 0, 0, None),
+    (1, 129, 2, 2, 128, True, 64, 0, 0, 0, None),
+    (1, 200, 2, 2, 96, False, 33, 5, 0, 0, None),
+    (2, 257, 6, 2, 80, True, 100, 70, 0, 0, None),       # sinks beyond one block of 64
+    (1, 700, 2, 1, 64, True, 40, 130, 0, 0, None),       # and of 128
+    (1, 1100, 2, 2, 128, True, 65, 4, 0, 0, None),       # sinks' gradients in chunks
+    (1, 1300, 2, 2, 40, False, 31, 200, 0, 0, None),     # bidirectional sinks on both sides
+    (1, 130, 2, 2, 128, True, 1000, 8, 0, 0, None),      # a window wider than the sequence
+    (1, 96, 2, 2, 16, True, 0, 9, 0, 0, None),           # sinks without a window
+    (3, 150, 2, 2, 64, False, 20, 3, 0, 0, (150, 0, 77)),  # an empty sequence
+    (4, 140, 4, 4, 128, True, 30, 2, 0, 0, (1, 140, 64, 128)),
+    (2, 90, 2, 2, 104, False, 0, 0, 0, 0, (-5, 1000)),   # lengths beyond their range
+    (1, 33, 2, 2, 64, True, 0, 0, 2, 2, None),           # the fewest buckets
+    (1, 150, 2, 2, 64, False, 0, 0, 4, 2, None),
+    (1, 300, 3, 3, 64, True, 0, 0, 32, 128, None),
+    (2, 333, 4, 2, 128, False, 0, 0, 32, 128, None),
+    (1, 400, 2, 2, 32, False, 0, 0, 128, 1024, None),    # the most, none of them far
+    (1, 1400, 2, 1, 128, True, 0, 0, 128, 1024, None),
+    (2, 260, 2, 1, 96, True, 90, 5, 16, 40, None),       # bias, window and sinks
+    (3, 280, 2, 2, 128, False, 70, 6, 32, 100, (280, 31, 0)),
+    (1, 900, 2, 2, 64, True, 50, 10, 64, 512, (777,)),
+]
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:10]))
+def test_attention(case, kind):
+    b, s, h, kv, d, causal, window, sinks, buckets, far, lengths = case
+    t, do = inputs(b, s, h, kv, d, kind)
+    how = dict(causal=causal, window=window, sinks=sinks, max_distance=far)
+    if buckets:
+        how["rel_bias"] = normal(9, h, buckets, kind=kind)
+    if lengths is not None:
+        how["lengths"] = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    compare(t, do, run(t, do, **how), **how)
+
+
+# -- layouts, streams, graphs ----------------------------------------------------
+
+MASKED = dict(causal=False, window=40, sinks=3, max_distance=50)
+
+
+def masked(seed=1, b=2, s=170, h=4, kv=2, d=64, kind=BF16):
+    t, do = inputs(b, s, h, kv, d, kind, seed)
+    how = dict(MASKED, rel_bias=normal(seed + 9, h, 16, kind=kind),
+               lengths=torch.tensor([s - 20 * i for i in range(b)], dtype=torch.int32, device="cuda"))
+    return t, do, how
+
+
+def test_strided_views():
+    """Heads as columns of one packed matrix, sequences inside heads, and gradients into such views."""
+    b, s, h, d = 2, 170, 4, 64
+    packed = normal(1, b, s, 3 * h * d)
+    q, k, v = (x.view(b, s, h, d) for x in packed.split(h * d, 2))
+    do = normal(4, b, h, s, d, std=0.1).transpose(1, 2)
+    t, how = dict(q=q, k=k, v=v), dict(MASKED, rel_bias=normal(9, h, 16))
+    grads = torch.full((b, s, 3 * h * d), math.nan, dtype=BF16, device="cuda")
+    dq, dk, dv = (x.view(b, s, h, d) for x in grads.split(h * d, 2))
+    o = torch.full((s, h, b, d + 8), math.nan, dtype=BF16, device="cuda")
+    ov = o[..., :d].permute(2, 0, 1, 3)
+    got_o, saved = ops().attention_forward(q, k, v, out=ov, **how)
+    assert got_o is ov
+    got = ops().attention_backward(do, q, k, v, ov, saved, dq=dq, dk=dk, dv=dv, **how)
+    assert got[0] is dq and got[1] is dk and got[2] is dv
+    compare(t, do, dict(o=ov, dq=dq, dk=dk, dv=dv, dbias=got[3]), **how)
+    assert bool(o[..., d:].isnan().all()), "columns beyond the heads were written"
+
+
+def test_broadcast_inputs():
+    """Inputs that repeat a sequence or a head (stride 0) get a gradient for each use."""
+    b, s, h, d = 3, 100, 4, 32
+    one = normal(1, 1, s, 1, d)
+    t = dict(q=normal(2, b, s, h, d), k=one.expand(b, s, 2, d), v=one.expand(b, s, 2, d))
+    do = normal(3, 1, s, 1, d, std=0.1).expand(b, s, h, d)
+    compare(t, do, run(t, do, window=30), window=30)
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+def test_results_are_reproducible(kind):
+    t, do, how = masked(kind=kind, s=700, b=1)
+    first = run(t, do, **how)
+    for _ in range(3):
+        again = run(t, do, **how)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+
+
+def test_forward_without_saved_is_the_same():
+    t, do, how = masked()
+    a = ops().attention_forward(t["q"], t["k"], t["v"], **how)[0]
+    b, saved = ops().attention_forward(t["q"], t["k"], t["v"], save=False, **how)
+    assert saved is None and torch.equal(a, b)
+
+
+def test_on_another_stream():
+    t, do, how = masked()
+    want = run(t, do, **how)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = run(t, do, **how)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+
+
+def test_two_captured_graphs():
+    """Two graphs captured and replayed in turn, with new inputs and eager work between the replays."""
+    calls = [masked(seed=1), masked(seed=30, s=260)]
+    graphs, outs = [], []
+    for t, do, how in calls:
+        run(t, do, **how)
+    torch.cuda.synchronize()
+    for t, do, how in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(run(t, do, **how))
+        graphs.append(g)
+    for turn in range(3):
+        for t, do, _ in calls:
+            for n, x in enumerate((t["q"], t["k"], t["v"], do)):
+                x.copy_(normal(100 * turn + n, *x.shape))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for (t, do, how), out in zip(calls, outs):
+            want = run(t, do, **how)
+            assert all(torch.equal(want[n], out[n]) for n in want), turn
+
+
+# -- values ------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+def test_padding_is_not_read(kind):
+    """NaN and infinities behind a sequence's length reach nothing."""
+    t, do, how = masked(kind=kind, b=3)
+    want = run(t, do, **how)
+    for i, n in enumerate(how["lengths"].tolist()):
+        for x, bad in zip((t["q"], t["k"], t["v"], do), (math.nan, math.inf, -math.inf, math.nan)):
+            x[i, n:] = bad
+    got = run(t, do, **how)
+    assert all(torch.equal(want[n], got[n]) for n in want)
+    for i, n in enumerate(how["lengths"].tolist()):
+        assert all(float(got[x][i, n:].abs().sum()) == 0.0 for x in ("o", "dq", "dk", "dv"))
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+def test_one_visible_token(kind):
+    """Where a token sees itself alone, o is its value and no gradient reaches the scores."""
+    t, do = inputs(2, 150, 4, 2, 64, kind)
+    got = run(t, do, window=1, rel_bias=normal(9, 4, 8, kind=kind), max_distance=16)
+    assert torch.equal(got["o"], t["v"].repeat_interleave(2, 2))
+    for n in ("dq", "dk", "dbias"):
+        assert float(got[n].abs().max()) == 0.0, n
+
+
+@pytest.mark.parametrize("low", [-math.inf, "lowest"])
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+def test_bias_that_hides(kind, low):
+    """A bias of -inf hides its bucket, and a row of such is empty; with the type's
+    lowest value a row of such is uniform instead, and a bucket among others hidden."""
+    t, do = inputs(1, 200, 2, 2, 64, kind)
+    low = torch.finfo(kind).min if low == "lowest" else low
+    bias = normal(9, 2, 8, kind=kind)
+    bias[0, 2:] = low
+    bias[1] = low
+    how = dict(rel_bias=bias, max_distance=16)
+    got = run(t, do, **how)
+    plain = bias.cpu().double()
+    out, mag = ref.attention(t["q"], t["k"], t["v"], do, bias=torch.where(plain < -1e38, -math.inf, plain), max_distance=16)
+    if math.isfinite(low):  # head 1: the mean over the tokens up to i, whatever the scores
+        flat, fmag = ref.attention(t["q"] * 0, t["k"] * 0, t["v"], do, causal=True)
+        for n in ("o", "dv"):
+            out[n][:, :, 1] = flat[n][:, :, 1]
+            mag[n] = tuple(torch.cat((a[:, :, :1], b[:, :, 1:]), 2) for a, b in zip(mag[n], fmag[n]))
+        got = {n: got[n] for n in ("o", "dv")}
+        out = {n: out[n] for n in ("o", "dv")}
+    ref.check_attention(got, out, mag, kind, kind)
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+def test_large_scores(kind):
+    """Scores of several thousand: probabilities of nearly one token a row."""
+    t, do = inputs(1, 200, 2, 2, 64, kind)
+    t["q"], t["k"] = t["q"] * 8, t["k"] * 8
+    how = dict(window=60, sinks=2, rel_bias=normal(9, 2, 8, std=30.0, kind=kind), max_distance=16)
+    compare(t, do, run(t, do, **how), **how)
+
+
+def test_gradients_against_differences():
+    """dq, dk, dv and dbias of a small fp32 call against central differences of
+    the 64-bit operator.  A difference of step e = 2^-10 is off by e^2 / 6 of a
+    third derivative, under 2^-20 * 2^6 of the gradient's size here."""
+    t, do = inputs(1, 20, 2, 1, 8, F32)
+    bias = normal(9, 2, 8, kind=F32)
+    how = dict(causal=False, window=6, sinks=1, max_distance=6, rel_bias=bias)
+    got = run(t, do, **how)
+    wide = {n: x.cpu().double() for n, x in (("q", t["q"]), ("k", t["k"]), ("v", t["v"]), ("rel_bias", bias))}
+    dod, e = do.cpu().double(), 2.0 ** -10
+
+    def total(x):
+        o, _ = ref.attention(x["q"], x["k"], x["v"], bias=x["rel_bias"], causal=False, window=6, sinks=1, max_distance=6)
+        return float((o["o"] * dod).sum())
+
+    rng = np.random.RandomState(0)
+    for n, g in (("q", "dq"), ("k", "dk"), ("v", "dv"), ("rel_bias", "dbias")):
+        size = float(got[g].abs().max())
+        for at in rng.permutation(wide[n].numel())[:12]:
+            flat = wide[n].view(-1)
+            was = float(flat[at])
+            flat[at] = was + e
+            up = total(wide)
+            flat[at] = was - e
+            down = total(wide)
+            flat[at] = was
+            assert abs((up - down) / (2 * e) - float(got[g].view(-1)[at])) < 2.0 ** -14 * size + 2.0 ** -20, (n, at)
+
+
+# -- AdamW ----------------------------------------------------------------------------
+
+
+def adamw_set(sizes, bits, grad_kind, seed=1, offset=0):
+    """Tensors of the given sizes, each `offset` elements into an allocation of its own."""
+    rng = np.random.RandomState(seed)
+    make = lambda x, kind: torch.cat((torch.zeros(offset), torch.from_numpy(x).float())).to(kind).cuda()[offset:]  # noqa: E731
+    p = [make(rng.randn(n) * 0.02, F32) for n in sizes]
+    g = [make(rng.randn(n) * np.exp(rng.randn()) * 1e-3, grad_kind) for n in sizes]
+    return p, g
+
+
+def check_adamw(opt, before, grads, scale, step, **hyper):
+    """Each tensor's p, m and v after a step against the 64-bit step from its state before.
+    fp32: m and v take three half-steps; p a few of p and of the update.  8 bits: the codes
+    are those of the 64-bit step."""
+    half = 2.0 ** -24
+    for i, (p0, m0, v0) in enumerate(before):
+        p, m, v = ref.adamw(p0, grads[i], m0, v0, step=step, decay=opt.decay[i], grad_scale=scale, **hyper)
+        got = opt.params[i].cpu().double().numpy()
+        bound = 4 * half * np.abs(p) + 16 * half * np.abs(p - p0) + 1e-30
+        assert np.all(np.abs(got - p) <= bound), (i, np.max(np.abs(got - p) / bound))
+        if opt.copies[i] is not None:
+            assert torch.equal(opt.copies[i], opt.params[i].to(BF16)), i
+        if opt.state_bits == 32:
+            gm, gv = opt.exp_avg[i].cpu().double().numpy(), opt.exp_avg_sq[i].cpu().double().numpy()
+            parts = 0.9 * np.abs(m0) + 0.1 * np.abs(grads[i] * scale)
+            assert np.all(np.abs(gm - m) <= 4 * half * parts + 1e-38), i
+            assert np.all(np.abs(gv - v) <= 5 * half * v + 1e-38), i
+        else:
+            for code, scales, want in ((opt.exp_avg[i], opt.exp_avg_scale[i], ref.encode_m(m)),
+                                       (opt.exp_avg_sq[i], opt.exp_avg_sq_scale[i], ref.encode_v(v))):
+                assert np.array_equal(scales.cpu().numpy(), want[1]), i
+                c, w = code.cpu().numpy(), want[0]
+                zero = (c & 127 == 0) & (w & 127 == 0) if want[0] is not None else False  # either sign of zero
+                assert np.all((c == w) | zero), (i, np.flatnonzero((c != w) & ~zero)[:5])
+
+
+def state(opt):
+    got = []
+    for i, p in enumerate(opt.params):
+        m, v = opt.exp_avg[i].cpu().numpy(), opt.exp_avg_sq[i].cpu().numpy()
+        if opt.state_bits == 8:
+            m = ref.decode_m(m, opt.exp_avg_scale[i].cpu().numpy())
+            v = ref.decode_v(v, opt.exp_avg_sq_scale[i].cpu().numpy())
+        got.append((p.cpu().double().numpy(), m.astype(np.float64), v.astype(np.float64)))
+    return got
+
+
+SIZES = [1, 2, 127, 128, 129, 4096, 4097, 1000, 8191, 0, 20000]
+
+
+@pytest.mark.parametrize("offset", [0, 1], ids=["aligned", "unaligned"])
+@pytest.mark.parametrize("grad_kind", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw(bits, grad_kind, offset):
+    p, g = adamw_set(SIZES, bits, grad_kind, offset=offset)
+    copies = [torch.zeros(n, dtype=BF16, device="cuda") if i % 2 else None for i, n in enumerate(SIZES)]
+    opt = ops().AdamW(p, g, state_bits=bits, decay=[i % 3 != 0 for i in range(len(SIZES))], copies=copies)
+    rng = np.random.RandomState(7)
+    for step in range(1, 4):
+        for x in g:
+            x.mul_(float(rng.rand()) + 0.5)
+        grads = [x.cpu().double().numpy() for x in g]
+        before = state(opt)
+        opt.step(0.5)
+        assert opt.steps == step
+        check_adamw(opt, before, grads, 0.5, step)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_more_tensors_than_a_launch_takes(bits):
+    sizes = [1 + 31 * i % 300 for i in range(131)]
+    p, g = adamw_set(sizes, bits, F32)
+    opt = ops().AdamW(p, g, state_bits=bits)
+    before, grads = state(opt), [x.cpu().double().numpy() for x in g]
+    opt.step()
+    check_adamw(opt, before, grads, 1.0, 1)
+
+
+def test_adamw_8_bit_edges():
+    """Moments from 2^-75 to 2^60 in one block, blocks of zeros, of equal values at the
+    formats' borders, and values that fp32 does not hold: their own codes are NaN, their
+    block's others are as if they were not there."""
+    g = np.zeros(128 * 8)
+    g[:128] = np.ldexp(1.0, np.linspace(-75, 60, 128).astype(int)) * np.where(np.arange(128) % 2, 1, -1)
+    g[256:384] = np.ldexp(1.75, 5)                           # both formats' largest code
+    g[384:512] = np.ldexp(1.7500002, 5)                      # just beyond: the next power of two
+    g[512:640] = np.random.RandomState(0).randn(128)
+    g[520], g[530], g[540] = np.nan, np.inf, -np.inf
+    g[640:768] = np.random.RandomState(1).randn(128) * 1e30  # squares beyond fp32
+    g[768:896] = np.random.RandomState(2).randn(128) * 1e-30
+    p = [torch.zeros(g.size, device="cuda")]
+    grads = [torch.from_numpy(g).float().cuda()]
+    opt = ops().AdamW(p, grads, state_bits=8, weight_decay=0.0)
+    before = state(opt)
+    wide = grads[0].cpu().double().numpy()
+    opt.step()
+    b1, b2 = float(np.float32(0.9)), float(np.float32(0.95))
+    with np.errstate(invalid="ignore"):
+        m, v = (1 - b1) * wide, (1 - b2) * wide * wide
+    for code, scales, want in ((opt.exp_avg[0], opt.exp_avg_scale[0], ref.encode_m(m)),
+                               (opt.exp_avg_sq[0], opt.exp_avg_sq_scale[0], ref.encode_v(v))):
+        assert np.array_equal(scales.cpu().numpy(), want[1])
+        c, w = code.cpu().numpy(), want[0]
+        assert np.all((c == w) | ((c & 127 == 0) & (w & 127 == 0)) | ((c & 127 == 127) & (w & 127 == 127))), \
+            np.flatnonzero(c != w)
+    assert before[0][0].sum() == 0 and bool(torch.isfinite(p[0][:512]).all())
+    assert int(opt.exp_avg_sq[0][:128].min()) >= 1, "a second moment above zero lost its code"
+    # a second step keeps what is not a number where it was
+    opt.step()
+    m2, v2 = state(opt)[0][1:]
+    assert np.array_equal(np.isnan(m2), ~(np.abs(m) < 3.4e38)) and np.isnan(v2[[520, 530, 540]]).all()
+
+
+def test_adamw_in_a_graph():
+    sizes = [3000, 17, 129]
+    p, g = adamw_set(sizes, 8, F32)
+    opt = ops().AdamW(p, g, state_bits=8)
+    opt.step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(0.25, step=2)
+    for turn in range(3):
+        for x in g:
+            x.copy_(normal(turn, *x.shape, std=1e-3, kind=F32))
+        before, grads = state(opt), [x.cpu().double().numpy() for x in g]
+        graph.replay()
+        torch.cuda.synchronize()
+        check_adamw(opt, before, grads, 0.25, 2)
+
+
+def test_adamw_steps_as_the_stage_does():
+    """32-bit moments: from the same state, the step of a stage's own optimizer.  Both
+    are compiled from one formula, but the compiler may join either product of a sum
+    with the addition, so each is held to the bounds of its 32-bit roundings."""
+    from paper_2405_14009_amd import RC_READ_ADAM_M, RC_READ_ADAM_V, RC_READ_GRAD, RC_READ_PARAM, Stage, param_shape
+    stage = Stage(num_layers=1, hidden=64, heads=2, ffn=128, seq_len=32, micro_batch=1, dtype="f32")
+    rng = np.random.RandomState(0)
+    stage.load_params([[rng.randn(*param_shape(i, 64, 128)) * 0.1 for i in range(12)]])
+    flat = lambda what: [torch.from_numpy(x.ravel()).cuda() for x in stage.read_all(what)[0]]  # noqa: E731
+    for step in range(1, 4):
+        stage.forward((0, 0), normal(step, 1, 32, 64, kind=F32))
+        stage.backward((0, 0), normal(step + 9, 1, 32, 64, kind=F32))
+        args = dict(decay=[i in (2, 4, 8, 10) for i in range(12)])
+        own = ops().AdamW(flat(RC_READ_PARAM), flat(RC_READ_GRAD), exp_avg=flat(RC_READ_ADAM_M),
+                          exp_avg_sq=flat(RC_READ_ADAM_V), **args)
+        before, grads = state(own), [x.cpu().double().numpy() for x in own.grads]
+        own.step(0.5, step=step)
+        check_adamw(own, before, grads, 0.5, step)
+        stage.optimizer_step(0.5)
+        theirs = ops().AdamW(flat(RC_READ_PARAM), flat(RC_READ_GRAD), exp_avg=flat(RC_READ_ADAM_M),
+                             exp_avg_sq=flat(RC_READ_ADAM_V), **args)
+        check_adamw(theirs, before, grads, 0.5, step)
