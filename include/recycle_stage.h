@@ -122,7 +122,8 @@ enum { RC_READ_PARAM = 0, RC_READ_GRAD = 1, RC_READ_ADAM_M = 2, RC_READ_ADAM_V =
 enum {
   RC_P_LN1_G = 0, RC_P_LN1_B = 1, RC_P_W_QKV = 2, RC_P_B_QKV = 3, RC_P_W_O = 4, RC_P_B_O = 5,
   RC_P_LN2_G = 6, RC_P_LN2_B = 7, RC_P_W_1 = 8, RC_P_B_1 = 9, RC_P_W_2 = 10, RC_P_B_2 = 11,
-  RC_NUM_PARAMS = 12
+  RC_NUM_PARAMS = 12,
+  RC_P_REL_BIAS = 12  /* stages with a relative position bias only: [heads, buckets] (see rc_stage_options) */
 };
 
 typedef struct rc_stage rc_stage; /* opaque, library-owned host object */
@@ -172,6 +173,48 @@ rc_status rc_stage_create(const rc_stage_config* cfg, const rc_adam_config* adam
 rc_status rc_stage_create_static(const rc_stage_config* cfg, const rc_adam_config* adam,
                                  int32_t stage_index, int32_t pipeline_id, void* state_arena,
                                  void* stash_arena, void* hip_stream, rc_stage** out);
+
+/* What a stage may have beyond rc_stage_config; all zeros: nothing.
+ *
+ * Attention.  window, sinks, buckets and max_distance are those of
+ * rc_attention below, in every layer; scores are scaled by 1 / sqrt(head_dim).
+ * buckets > 0 gives each layer the parameter RC_P_REL_BIAS [heads, buckets]
+ * (fp32, zero until loaded, no weight decay, no bf16 copy).  Its gradient is
+ * formed by B_input, which has the scores' gradients at hand, and kept in the
+ * micro-batch's stash slot; B_weight adds it up, like every other gradient.
+ * Stages with a window (shorter than seq_len) or a bias run the kernels of
+ * rc_attention_forward / _backward (RC_ATTN_OPERATOR), in either dtype.
+ *
+ * adam_state_bits = 8: the moments are 8-bit codes (see rc_adamw_tensor; 0 and
+ * 32: fp32).  The state arena then holds the moments before and after the
+ * last step, so that a step can still be rolled back (4 bytes a parameter in
+ * place of 8): rollback returns to the moments that the step read, and
+ * recomputes its update from them and the gradient.  (A step captured into a
+ * graph reads and writes the moments that it read and wrote when it was
+ * captured: capture two steps, not one, to replay them in turn.)
+ *
+ * static_work = 1: work memory as for rc_stage_create_static (work_arena is
+ * NULL, no dry run).
+ *
+ * Stash account (rc_stash_account) of stages that run RC_ATTN_OPERATOR: attn =
+ * 8 b heads s, and 2 T h more in bf16; with a bias s_w has 4 L heads buckets more. */
+typedef struct rc_stage_options {
+  int32_t window, sinks;
+  int32_t buckets, max_distance;
+  int32_t adam_state_bits;
+  int32_t static_work;
+} rc_stage_options;
+
+/* rc_stage_memory_requirements and rc_stage_create with options (NULL: none).
+ * Errors: as theirs; RC_ERR_INVALID_ARG and RC_ERR_UNSUPPORTED also for what
+ * rc_attention_memory refuses in the options. */
+rc_status rc_stage_memory_requirements_with(const rc_stage_config* cfg, const rc_stage_options* options,
+                                            size_t* state_bytes, size_t* stash_bytes,
+                                            size_t* work_bytes);
+rc_status rc_stage_create_with(const rc_stage_config* cfg, const rc_stage_options* options,
+                               const rc_adam_config* adam, int32_t stage_index, int32_t pipeline_id,
+                               void* state_arena, void* stash_arena, void* work_arena,
+                               void* hip_stream, rc_stage** out);
 
 /* Waits for the handle's stream, then frees the host object (not the arenas). */
 rc_status rc_stage_destroy(rc_stage* st);
@@ -359,9 +402,14 @@ rc_status rc_stage_profile_read(rc_stage* st, rc_kernel_stat* out);
  *                         that fill the compute units once);
  *   RC_ATTN_SPLIT         fused, one workgroup per 32 queries, whose four waves
  *                         share their keys (grids of at most one such workgroup
- *                         per compute unit, two for head_dim <= 64).
+ *                         per compute unit, two for head_dim <= 64);
+ *   RC_ATTN_OPERATOR      rc_attention_forward / _backward (stages with a
+ *                         window or a relative position bias).
  * Host only; works on dry-run handles.  Errors: RC_ERR_INVALID_ARG. */
-enum { RC_ATTN_MATERIALISED = 0, RC_ATTN_BLOCK = 1, RC_ATTN_PAIRED = 2, RC_ATTN_SPLIT = 3 };
+enum {
+  RC_ATTN_MATERIALISED = 0, RC_ATTN_BLOCK = 1, RC_ATTN_PAIRED = 2, RC_ATTN_SPLIT = 3,
+  RC_ATTN_OPERATOR = 4
+};
 rc_status rc_stage_attention_kernels(rc_stage* st, int32_t* kind);
 
 /* Wait for the handle's stream; reports any deferred device error as RC_ERR_HIP. */
@@ -478,6 +526,14 @@ typedef struct rc_adamw_tensor {
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_HIP. */
 rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam_config* adam,
                         int32_t state_bits, int64_t step, float grad_scale, void* hip_stream);
+
+/* The moments of n tensors as fp32 values (a checkpoint, a resumed run with
+ * 32-bit moments): exp_avg[i] and exp_avg_sq[i] are device arrays of
+ * tensors[i].count floats, host arrays of n pointers.  Only the moments, scales
+ * and counts of the tensors are looked at.
+ * Errors: RC_ERR_INVALID_ARG, RC_ERR_HIP. */
+rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state_bits,
+                        float* const* exp_avg, float* const* exp_avg_sq, void* hip_stream);
 
 /* ---- Schedule side (host only, no device work) ------------------------- */
 

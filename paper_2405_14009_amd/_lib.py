@@ -15,8 +15,8 @@ RC_OK, RC_ERR_INVALID_ARG, RC_ERR_BAD_STATE, RC_ERR_OUT_OF_STASH, RC_ERR_HIP, RC
 RC_FP32, RC_BF16 = 0, 1
 RC_OP_F, RC_OP_B, RC_OP_W, RC_OP_STEP, RC_OP_SKIP, RC_OP_ROLLBACK = 0, 1, 2, 3, 4, 5
 RC_READ_PARAM, RC_READ_GRAD, RC_READ_ADAM_M, RC_READ_ADAM_V = 0, 1, 2, 3
-RC_NUM_PARAMS = 12
-RC_ATTN_MATERIALISED, RC_ATTN_BLOCK, RC_ATTN_PAIRED, RC_ATTN_SPLIT = 0, 1, 2, 3
+RC_NUM_PARAMS, RC_P_REL_BIAS = 12, 12
+RC_ATTN_MATERIALISED, RC_ATTN_BLOCK, RC_ATTN_PAIRED, RC_ATTN_SPLIT, RC_ATTN_OPERATOR = 0, 1, 2, 3, 4
 RC_STATIC_WORK_BYTES = 96 * 1024 * 1024
 
 # Every symbol the header declares, for load checks.
@@ -30,6 +30,7 @@ EXPORTED = (
     "rc_stage_synchronize", "rc_stage_profile_enable", "rc_stage_profile_read", "rc_last_error",
     "rc_failure_normalization", "rc_schedule_simulate",
     "rc_attention_memory", "rc_attention_forward", "rc_attention_backward", "rc_adamw_step",
+    "rc_adamw_read", "rc_stage_memory_requirements_with", "rc_stage_create_with",
 )
 
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "layernorm",
@@ -47,6 +48,12 @@ class RcStageConfig(ctypes.Structure):
                 ("micro_batch", ctypes.c_int32), ("causal", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("ln_eps", ctypes.c_float),
                 ("max_stashed_mb", ctypes.c_int32), ("max_inflight_mb", ctypes.c_int32)]
+
+
+class RcStageOptions(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("buckets", ctypes.c_int32),
+                ("max_distance", ctypes.c_int32), ("adam_state_bits", ctypes.c_int32),
+                ("static_work", ctypes.c_int32)]
 
 
 class RcAdamConfig(ctypes.Structure):
@@ -157,6 +164,10 @@ def load() -> ctypes.CDLL:
         "rc_attention_forward": [ctypes.POINTER(RcAttention), view, view, view, P, P, view, P, P],
         "rc_attention_backward": [ctypes.POINTER(RcAttention), view, view, view, P, P, view, P, view,
                                   view, view, view, P, P, P],
+        "rc_stage_memory_requirements_with": [cfgp, ctypes.POINTER(RcStageOptions), sz, sz, sz],
+        "rc_stage_create_with": [cfgp, ctypes.POINTER(RcStageOptions), ctypes.POINTER(RcAdamConfig), I32, I32, P,
+                                 P, P, P, ctypes.POINTER(P)],
+        "rc_adamw_read": [ctypes.POINTER(RcAdamwTensor), I32, I32, ctypes.POINTER(P), ctypes.POINTER(P), P],
         "rc_adamw_step": [ctypes.POINTER(RcAdamwTensor), I32, ctypes.POINTER(RcAdamConfig), I32,
                           ctypes.c_int64, F32, P],
     }

@@ -25,6 +25,8 @@
 // HBM allows about 120 vector operations for each), so that the codes are
 // those of the formulas and do not depend on how 32-bit sums round.  The
 // update itself uses m' and v' before that rounding.
+#include <cmath>
+
 #include "adam.h"
 #include "adamw_op.h"
 #include "common.h"
@@ -47,8 +49,11 @@ struct Tensor {
 };
 enum { DECAY = 1, GRAD_BF16 = 2, WIDE = 4 };  // WIDE: every pointer is aligned to its vector accesses
 
+enum { IN_PLACE, BANKS, UNDO };  // where 8-bit moments go: where they were, `to` bytes on, nowhere
+
 struct Args {
   AdamwHyper h;
+  long to;
   int n;
   Tensor t[MAX];
 };
@@ -156,15 +161,16 @@ __device__ __forceinline__ double decode_v(int c, double unit) {
 }
 
 // A thread takes 8 elements, 16 lanes a block of 128.
-__device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long i) {
+template <int MODE>
+__device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long i, long to) {
   const long left_l = t.n - i;
   const int left = left_l < 8 ? (left_l > 0 ? (int)left_l : 0) : 8;
   const bool wide = (t.flags & WIDE) && left == 8;
   float p[8], g[8];
   load_f32<8>(p, t.p, i, left, wide);
   load_grad<8>(g, t, i, left, wide);
-  uint8_t* const mc = (uint8_t*)t.m + i;
-  uint8_t* const vc = (uint8_t*)t.v + i;
+  const uint8_t* const mc = (const uint8_t*)t.m + i;
+  const uint8_t* const vc = (const uint8_t*)t.v + i;
   uint32_t mw[2] = {0, 0}, vw[2] = {0, 0};
   if (wide) {
     *(uint2*)mw = *(const uint2*)mc;
@@ -205,11 +211,19 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long
   if (!left) return;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    if (t.flags & DECAY) p[k] *= (1.f - h.lr * h.weight_decay);
-    p[k] -= adam_update((float)m[k], (float)v[k], h.eps, h.step_size, h.inv_sqrt_bc2);
+    const float u = adam_update((float)m[k], (float)v[k], h.eps, h.step_size, h.inv_sqrt_bc2);
+    const float shrink = 1.f - h.lr * h.weight_decay;
+    if constexpr (MODE == UNDO) {
+      p[k] += u;
+      if (t.flags & DECAY) p[k] /= shrink;
+    } else {
+      if (t.flags & DECAY) p[k] *= shrink;
+      p[k] -= u;
+    }
   }
   store_f32<8>(p, t.p, i, left, wide);
   store_copy<8>(p, t, i, left, wide);
+  if constexpr (MODE == UNDO) return;
   mw[0] = mw[1] = vw[0] = vw[1] = 0;
 #pragma unroll
   for (int k = 0; k < 8; k += 2) {
@@ -221,20 +235,22 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long
     const int c1 = fits(v[k + 1]) ? encode_v(scaled_odd(v[k + 1], ev)) : 255;
     vw[k >> 2] |= (uint32_t)(c0 | c1 << 8) << (8 * (k & 3));
   }
+  uint8_t* const mo = (uint8_t*)t.m + i + (MODE == BANKS ? to : 0);
+  uint8_t* const vo = (uint8_t*)t.v + i + (MODE == BANKS ? to : 0);
   if (wide) {
-    *(uint2*)mc = *(const uint2*)mw;
-    *(uint2*)vc = *(const uint2*)vw;
+    *(uint2*)mo = *(const uint2*)mw;
+    *(uint2*)vo = *(const uint2*)vw;
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
       if (k < left) {
-        mc[k] = (uint8_t)(mw[k >> 2] >> (8 * (k & 3)));
-        vc[k] = (uint8_t)(vw[k >> 2] >> (8 * (k & 3)));
+        mo[k] = (uint8_t)(mw[k >> 2] >> (8 * (k & 3)));
+        vo[k] = (uint8_t)(vw[k >> 2] >> (8 * (k & 3)));
       }
   }
   if (i % ADAMW_BLOCK == 0) {
-    t.ms[blk] = (uint8_t)(em + 127);
-    t.vs[blk] = (uint8_t)(ev + 160);
+    t.ms[blk + (MODE == BANKS ? to : 0)] = (uint8_t)(em + 127);
+    t.vs[blk + (MODE == BANKS ? to : 0)] = (uint8_t)(ev + 160);
   }
 }
 
@@ -258,10 +274,9 @@ __device__ __forceinline__ void step32(const Tensor& t, const AdamwHyper& h, lon
   store_copy<4>(p, t, i, left, wide);
 }
 
-template <int BITS>
-__global__ __launch_bounds__(NT) void adamw_tensors_k(Args a) {
-  const int c = blockIdx.x;
-  int lo = 0, hi = a.n - 1;  // the last tensor whose first chunk is not after c
+// The tensor of chunk c: the last one whose first chunk is not after it.
+__device__ __forceinline__ const Tensor& tensor_of(const Args& a, int c) {
+  int lo = 0, hi = a.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.t[mid].first <= c)
@@ -269,48 +284,170 @@ __global__ __launch_bounds__(NT) void adamw_tensors_k(Args a) {
     else
       hi = mid - 1;
   }
-  const Tensor& t = a.t[lo];
-  const long at = (long)(c - t.first) * CHUNK;
+  return a.t[lo];
+}
+
+template <int BITS, int MODE>
+__global__ __launch_bounds__(NT) void adamw_tensors_k(Args a) {
+  const Tensor& t = tensor_of(a, blockIdx.x);
+  const long at = (long)((int)blockIdx.x - t.first) * CHUNK;
   constexpr int N = BITS == 8 ? 8 : 4;
   for (int k = 0; k < CHUNK; k += NT * N) {
     const long i = at + k + (long)threadIdx.x * N;
     if constexpr (BITS == 8)
-      step8(t, a.h, i);
+      step8<MODE>(t, a.h, i, a.to);
     else
       step32(t, a.h, i);
   }
 }
 
+// Moments as values: m and v of a tensor into p and g of its descriptor.
+template <int BITS>
+__global__ __launch_bounds__(NT) void adamw_read_k(Args a) {
+  const Tensor& t = tensor_of(a, blockIdx.x);
+  const long at = (long)((int)blockIdx.x - t.first) * CHUNK;
+  for (int k = 0; k < CHUNK; k += NT * 8) {
+    const long i = at + k + (long)threadIdx.x * 8, left_l = t.n - i;
+    if (left_l <= 0) return;
+    const int left = left_l < 8 ? (int)left_l : 8;
+    const bool wide = (t.flags & WIDE) && left == 8;
+    float m[8], v[8];
+    if constexpr (BITS == 32) {
+      load_f32<8>(m, (const float*)t.m, i, left, wide);
+      load_f32<8>(v, (const float*)t.v, i, left, wide);
+    } else {
+      uint8_t mc[8], vc[8];
+      if (wide) {
+        *(uint2*)mc = *(const uint2*)((const uint8_t*)t.m + i);
+        *(uint2*)vc = *(const uint2*)((const uint8_t*)t.v + i);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          mc[j] = j < left ? ((const uint8_t*)t.m)[i + j] : 0;
+          vc[j] = j < left ? ((const uint8_t*)t.v)[i + j] : 0;
+        }
+      }
+      const double mu = power_of_two((int)t.ms[i / ADAMW_BLOCK] - 127);
+      const double vu = power_of_two((int)t.vs[i / ADAMW_BLOCK] - 160);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = (float)((double)__builtin_amdgcn_cvt_f32_fp8(mc[j], 0) * mu);
+        v[j] = (float)decode_v(vc[j], vu);
+      }
+    }
+    store_f32<8>(m, t.p, i, left, wide);
+    store_f32<8>(v, (float*)t.g, i, left, wide);
+  }
+}
+
 bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
-}  // namespace
-
-hipError_t adamw_tensors(const rc_adamw_tensor* ts, int n, int bits, const AdamwHyper& h, hipStream_t s) {
-  Args a;
-  a.h = h;
+// launch(args, chunks) for groups of up to MAX of the tensors, whose descriptors set(tensor, i) makes.
+template <class Set, class Launch>
+hipError_t in_groups(const rc_adamw_tensor* ts, int n, Args& a, Set set, Launch launch) {
   for (int at = 0; at < n;) {
     long chunks = 0;
     a.n = 0;
     for (; at < n && a.n < MAX; ++at) {
-      const rc_adamw_tensor& x = ts[at];
-      if (x.count == 0) continue;
-      const long own = (x.count + CHUNK - 1) / CHUNK;
+      if (ts[at].count == 0) continue;
+      const long own = (ts[at].count + CHUNK - 1) / CHUNK;
       if (a.n && chunks + own > 0x7fffffffL) break;
       Tensor& t = a.t[a.n++];
-      t = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, (bf16*)x.copy, x.count, (int)chunks, 0};
-      const bool wide = aligned(x.param, 16) && aligned(x.grad, x.grad_dtype == RC_BF16 ? 8 : 16) &&
-                        aligned(x.exp_avg, bits == 8 ? 8 : 16) && aligned(x.exp_avg_sq, bits == 8 ? 8 : 16) &&
-                        aligned(x.copy, 8);
-      t.flags = (x.decay ? DECAY : 0) | (x.grad_dtype == RC_BF16 ? GRAD_BF16 : 0) | (wide ? WIDE : 0);
+      t = set(ts[at], at);
+      t.n = ts[at].count;
+      t.first = (int)chunks;
       chunks += own;
     }
     if (!a.n) break;
-    if (bits == 8)
-      hipLaunchKernelGGL(adamw_tensors_k<8>, dim3((unsigned)chunks), dim3(NT), 0, s, a);
-    else
-      hipLaunchKernelGGL(adamw_tensors_k<32>, dim3((unsigned)chunks), dim3(NT), 0, s, a);
+    launch(dim3((unsigned)chunks));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+Tensor step_tensor(const rc_adamw_tensor& x, int bits) {
+  const size_t moment = bits == 8 ? 8 : 16;
+  const bool wide = aligned(x.param, 16) && aligned(x.grad, x.grad_dtype == RC_BF16 ? 8 : 16) &&
+                    aligned(x.exp_avg, moment) && aligned(x.exp_avg_sq, moment) && aligned(x.copy, 8);
+  Tensor t = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, (bf16*)x.copy, 0, 0, 0};
+  t.flags = (x.decay ? DECAY : 0) | (x.grad_dtype == RC_BF16 ? GRAD_BF16 : 0) | (wide ? WIDE : 0);
+  return t;
+}
+
+}  // namespace
+
+AdamwHyper adamw_hyper(const rc_adam_config& a, int64_t step, float grad_scale) {
+  AdamwHyper h;
+  h.beta1 = a.beta1;
+  h.beta2 = a.beta2;
+  h.grad_scale = grad_scale;
+  h.lr = a.lr;
+  h.weight_decay = a.weight_decay;
+  h.eps = a.eps;
+  h.step_size = (float)(a.lr / (1.0 - std::pow(h.beta1, (double)step)));
+  h.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h.beta2, (double)step)));
+  return h;
+}
+
+hipError_t adamw_tensors(const rc_adamw_tensor* ts, int n, int bits, const AdamwHyper& h, hipStream_t s) {
+  Args a;
+  a.h = h;
+  a.to = 0;
+  return in_groups(
+      ts, n, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, bits); },
+      [&](dim3 grid) {
+        if (bits == 8)
+          hipLaunchKernelGGL((adamw_tensors_k<8, IN_PLACE>), grid, dim3(NT), 0, s, a);
+        else
+          hipLaunchKernelGGL((adamw_tensors_k<32, IN_PLACE>), grid, dim3(NT), 0, s, a);
+      });
+}
+
+hipError_t adamw_banks(const rc_adamw_tensor* ts, int n, const AdamwHyper& h, long to, bool undo, hipStream_t s) {
+  Args a;
+  a.h = h;
+  a.to = to;
+  return in_groups(
+      ts, n, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, 8); },
+      [&](dim3 grid) {
+        if (undo)
+          hipLaunchKernelGGL((adamw_tensors_k<8, UNDO>), grid, dim3(NT), 0, s, a);
+        else
+          hipLaunchKernelGGL((adamw_tensors_k<8, BANKS>), grid, dim3(NT), 0, s, a);
+      });
+}
+
+hipError_t adamw_read(const rc_adamw_tensor* ts, int n, int bits, float* const* m, float* const* v, hipStream_t s) {
+  Args a;
+  a.h = {};
+  a.to = 0;
+  return in_groups(
+      ts, n, a,
+      [&](const rc_adamw_tensor& x, int i) {
+        const size_t moment = bits == 8 ? 8 : 16;
+        const bool wide = aligned(m[i], 16) && aligned(v[i], 16) && aligned(x.exp_avg, moment) &&
+                          aligned(x.exp_avg_sq, moment);
+        return Tensor{m[i], v[i], x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, nullptr, 0, 0,
+                      wide ? WIDE : 0};
+      },
+      [&](dim3 grid) {
+        if (bits == 8)
+          hipLaunchKernelGGL(adamw_read_k<8>, grid, dim3(NT), 0, s, a);
+        else
+          hipLaunchKernelGGL(adamw_read_k<32>, grid, dim3(NT), 0, s, a);
+      });
+}
+
+float adamw_decode_m(int code, int scale) {
+  const int e = (code >> 3) & 15, f = code & 7;
+  if ((code & 127) == 127) return NAN;
+  const float x = e ? std::ldexp((float)(8 + f), e - 10) : std::ldexp((float)f, -9);
+  return std::ldexp(code & 128 ? -x : x, scale - 127);
+}
+
+float adamw_decode_v(int code, int scale) {
+  if (code == 255) return NAN;
+  const double x = code < 8 ? code : std::ldexp((double)(8 + (code & 7)), (code >> 3) - 1);
+  return (float)std::ldexp(x, scale - 160);
 }

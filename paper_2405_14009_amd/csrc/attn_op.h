@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "recycle_stage.h"
+
 // Distances in tokens at which the last bucket of a side has to begin at the latest.
 constexpr int ATTN_OP_MAX_FAR = 1024;
 constexpr int ATTN_OP_MAX_BUCKETS = 128;
@@ -51,6 +53,16 @@ ATTN_OP_DECL(bf16_128)
 ATTN_OP_DECL(f32_64)
 ATTN_OP_DECL(f32_128)
 #undef ATTN_OP_DECL
+
+// Checks a configuration and sets the arguments that follow from it (operators.cpp).
+rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a);
+
+// dbias (+)= the sum of n gradients of count floats, in order.
+constexpr int ATTN_OP_MAX_SHARES = 32;
+struct AttnOpShares {
+  const float* p[ATTN_OP_MAX_SHARES];
+};
+hipError_t attn_op_add_dbias(const AttnOpShares& shares, int n, long count, float* out, int accumulate, hipStream_t st);
 
 // What one attention needs, in bytes, and its launches.  The arguments' scratch
 // pointers are set from `saved` (null: nothing is kept for a backward pass) and

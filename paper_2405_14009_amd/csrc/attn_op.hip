@@ -61,6 +61,15 @@ __global__ __launch_bounds__(256) void attn_op_dbias_k(const float* part, E* out
   out[(long)h * buckets + c] = (E)t;
 }
 
+__global__ __launch_bounds__(256) void attn_op_add_dbias_k(AttnOpShares shares, int n, long count, float* out,
+                                                           int accumulate) {
+  const long i = blockIdx.x * 256L + threadIdx.x;
+  if (i >= count) return;
+  float t = accumulate ? out[i] : 0.f;
+  for (int k = 0; k < n; ++k) t += shares.p[k][i];
+  out[i] = t;
+}
+
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 int columns(int elt, int d) { return elt == 2 && d <= 32 ? 32 : d <= 64 ? 64 : elt == 2 && d <= 96 ? 96 : 128; }
@@ -159,5 +168,12 @@ hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work
   else
     hipLaunchKernelGGL(attn_op_dbias_k<bf16>, dim3(a.heads), dim3(256), 0, st, a.bpart, (bf16*)a.dbias, a.batch,
                        a.heads, nqb, a.buckets);
+  return hipGetLastError();
+}
+
+hipError_t attn_op_add_dbias(const AttnOpShares& shares, int n, long count, float* out, int accumulate, hipStream_t st) {
+  if (n < 1 || n > ATTN_OP_MAX_SHARES) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(attn_op_add_dbias_k, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, shares, n, count, out,
+                     accumulate);
   return hipGetLastError();
 }

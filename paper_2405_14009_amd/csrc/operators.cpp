@@ -13,6 +13,49 @@
 
 rc_status rc_set_error(rc_status s, const std::string& msg);
 
+rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
+  if (c.dtype != RC_FP32 && c.dtype != RC_BF16) return rc_set_error(RC_ERR_INVALID_ARG, "unknown dtype");
+  if (c.batch < 1 || c.seq_len < 1 || c.heads < 1 || c.kv_heads < 1 || c.head_dim < 1)
+    return rc_set_error(RC_ERR_INVALID_ARG, "attention sizes must be positive");
+  if (c.heads % c.kv_heads) return rc_set_error(RC_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
+  if (c.causal != 0 && c.causal != 1) return rc_set_error(RC_ERR_INVALID_ARG, "causal must be 0 or 1");
+  if (c.window < 0 || c.sinks < 0) return rc_set_error(RC_ERR_INVALID_ARG, "window and sinks must not be negative");
+  if (!(c.scale > 0.f) || !std::isfinite(c.scale))
+    return rc_set_error(RC_ERR_INVALID_ARG, "scale must be finite and above zero");
+  if (c.buckets) {
+    const int side = c.causal ? c.buckets : c.buckets / 2;
+    if (c.buckets < 0 || side < 2 || (!c.causal && c.buckets % 2))
+      return rc_set_error(RC_ERR_INVALID_ARG, "buckets: at least 2 (causal), or an even number of at least 4");
+    if (c.max_distance <= side / 2)
+      return rc_set_error(RC_ERR_INVALID_ARG, "max_distance must exceed the distances with a bucket each (" +
+                                          std::to_string(side / 2) + ")");
+    if (c.bias_dtype != RC_FP32 && c.bias_dtype != RC_BF16)
+      return rc_set_error(RC_ERR_INVALID_ARG, "unknown bias_dtype");
+    if (c.buckets > ATTN_OP_MAX_BUCKETS || c.max_distance > ATTN_OP_MAX_FAR)
+      return rc_set_error(RC_ERR_UNSUPPORTED, "at most " + std::to_string(ATTN_OP_MAX_BUCKETS) +
+                                          " buckets and a max_distance of " + std::to_string(ATTN_OP_MAX_FAR));
+  }
+  if (c.head_dim % 8 || c.head_dim > 128)
+    return rc_set_error(RC_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most 128");
+  if (c.seq_len > (1 << 24)) return rc_set_error(RC_ERR_UNSUPPORTED, "seq_len exceeds 2^24");
+  a = {};
+  a.batch = c.batch;
+  a.s = c.seq_len;
+  a.heads = c.heads;
+  a.kv_heads = c.kv_heads;
+  a.d = c.head_dim;
+  a.causal = c.causal;
+  a.sinks = c.sinks;
+  a.scale = c.scale;
+  a.buckets = c.buckets;
+  a.bias_f32 = c.bias_dtype == RC_FP32;
+  attn_op_plan(a, c.window, c.max_distance);
+  const long units = ((long)a.s + 127) / 128 + (long)a.sink_blocks * a.chunks;
+  if (units * a.batch > 0x7fffffffL / a.heads)
+    return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks of 128 tokens");
+  return RC_OK;
+}
+
 namespace {
 
 rc_status fail(rc_status s, const std::string& msg) { return rc_set_error(s, msg); }
@@ -54,46 +97,7 @@ int elt_of(int dtype) { return dtype == RC_BF16 ? 2 : 4; }
 
 rc_status attention_args(const rc_attention* c, AttnOpArgs& a) {
   if (!c) return fail(RC_ERR_INVALID_ARG, "null attention");
-  if (c->dtype != RC_FP32 && c->dtype != RC_BF16) return fail(RC_ERR_INVALID_ARG, "unknown dtype");
-  if (c->batch < 1 || c->seq_len < 1 || c->heads < 1 || c->kv_heads < 1 || c->head_dim < 1)
-    return fail(RC_ERR_INVALID_ARG, "attention sizes must be positive");
-  if (c->heads % c->kv_heads) return fail(RC_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
-  if (c->causal != 0 && c->causal != 1) return fail(RC_ERR_INVALID_ARG, "causal must be 0 or 1");
-  if (c->window < 0 || c->sinks < 0) return fail(RC_ERR_INVALID_ARG, "window and sinks must not be negative");
-  if (!(c->scale > 0.f) || !std::isfinite(c->scale))
-    return fail(RC_ERR_INVALID_ARG, "scale must be finite and above zero");
-  if (c->buckets) {
-    const int side = c->causal ? c->buckets : c->buckets / 2;
-    if (c->buckets < 0 || side < 2 || (!c->causal && c->buckets % 2))
-      return fail(RC_ERR_INVALID_ARG, "buckets: at least 2 (causal), or an even number of at least 4");
-    if (c->max_distance <= side / 2)
-      return fail(RC_ERR_INVALID_ARG, "max_distance must exceed the distances with a bucket each (" +
-                                          std::to_string(side / 2) + ")");
-    if (c->bias_dtype != RC_FP32 && c->bias_dtype != RC_BF16)
-      return fail(RC_ERR_INVALID_ARG, "unknown bias_dtype");
-    if (c->buckets > ATTN_OP_MAX_BUCKETS || c->max_distance > ATTN_OP_MAX_FAR)
-      return fail(RC_ERR_UNSUPPORTED, "at most " + std::to_string(ATTN_OP_MAX_BUCKETS) +
-                                          " buckets and a max_distance of " + std::to_string(ATTN_OP_MAX_FAR));
-  }
-  if (c->head_dim % 8 || c->head_dim > 128)
-    return fail(RC_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most 128");
-  if (c->seq_len > (1 << 24)) return fail(RC_ERR_UNSUPPORTED, "seq_len exceeds 2^24");
-  a = {};
-  a.batch = c->batch;
-  a.s = c->seq_len;
-  a.heads = c->heads;
-  a.kv_heads = c->kv_heads;
-  a.d = c->head_dim;
-  a.causal = c->causal;
-  a.sinks = c->sinks;
-  a.scale = c->scale;
-  a.buckets = c->buckets;
-  a.bias_f32 = c->bias_dtype == RC_FP32;
-  attn_op_plan(a, c->window, c->max_distance);
-  const long units = ((long)a.s + 127) / 128 + (long)a.sink_blocks * a.chunks;
-  if (units * a.batch > 0x7fffffffL / a.heads)
-    return fail(RC_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks of 128 tokens");
-  return RC_OK;
+  return attn_op_check(*c, a);
 }
 
 // A view of n heads; an output's elements must each have a place of their own.
@@ -134,6 +138,18 @@ rc_status bias_args(const rc_attention* c, const void* bias, const int32_t* leng
     return fail(RC_ERR_INVALID_ARG, "bias or lengths not aligned to their elements");
   a.bias = bias;
   a.lengths = lengths;
+  return RC_OK;
+}
+
+constexpr int64_t kMaxCount = (int64_t)1 << 42;
+
+rc_status moment_args(const rc_adamw_tensor& t, int state_bits, const std::string& name) {
+  if (!t.exp_avg || !t.exp_avg_sq) return fail(RC_ERR_INVALID_ARG, name + "null array");
+  const bool scales = t.exp_avg_scale && t.exp_avg_sq_scale, none = !t.exp_avg_scale && !t.exp_avg_sq_scale;
+  if (state_bits == 8 ? !scales : !none)
+    return fail(RC_ERR_INVALID_ARG, name + "8-bit moments have scales, 32-bit ones have none");
+  if (state_bits == 32 && ((uintptr_t)t.exp_avg | (uintptr_t)t.exp_avg_sq) % 4)
+    return fail(RC_ERR_INVALID_ARG, name + "an array is not aligned to its elements");
   return RC_OK;
 }
 
@@ -218,31 +234,40 @@ rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam
     for (int i = 0; i < n; ++i) {
       const rc_adamw_tensor& t = tensors[i];
       const std::string name = "tensor " + std::to_string(i) + ": ";
-      if (t.count < 0 || t.count > (int64_t)1 << 42) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
+      if (t.count < 0 || t.count > kMaxCount) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
       if (t.grad_dtype != RC_FP32 && t.grad_dtype != RC_BF16)
         return fail(RC_ERR_INVALID_ARG, name + "unknown grad_dtype");
       if (t.count == 0) continue;
-      if (!t.param || !t.grad || !t.exp_avg || !t.exp_avg_sq) return fail(RC_ERR_INVALID_ARG, name + "null array");
-      const bool scales = t.exp_avg_scale && t.exp_avg_sq_scale, none = !t.exp_avg_scale && !t.exp_avg_sq_scale;
-      if (state_bits == 8 ? !scales : !none)
-        return fail(RC_ERR_INVALID_ARG, name + "8-bit moments have scales, 32-bit ones have none");
-      const uintptr_t words = (uintptr_t)t.param | (t.grad_dtype == RC_BF16 ? 0 : (uintptr_t)t.grad) |
-                              (state_bits == 8 ? 0 : (uintptr_t)t.exp_avg | (uintptr_t)t.exp_avg_sq);
-      if (words % 4 || (uintptr_t)t.grad % 2 || (uintptr_t)t.copy % 2)
+      if (!t.param || !t.grad) return fail(RC_ERR_INVALID_ARG, name + "null array");
+      TRY(moment_args(t, state_bits, name));
+      if ((uintptr_t)t.param % 4 || (uintptr_t)t.grad % elt_of(t.grad_dtype) || (uintptr_t)t.copy % 2)
         return fail(RC_ERR_INVALID_ARG, name + "an array is not aligned to its elements");
     }
-    AdamwHyper h;
-    h.beta1 = adam->beta1;
-    h.beta2 = adam->beta2;
-    h.grad_scale = grad_scale;
-    h.lr = adam->lr;
-    h.weight_decay = adam->weight_decay;
-    h.eps = adam->eps;
-    h.step_size = (float)(adam->lr / (1.0 - std::pow(h.beta1, (double)step)));
-    h.inv_sqrt_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h.beta2, (double)step)));
     OnDevice on((hipStream_t)hip_stream);
     if (on.err != hipSuccess) return hip_result(on.err, "device of the stream");
-    return hip_result(adamw_tensors(tensors, n, state_bits, h, (hipStream_t)hip_stream), "AdamW step");
+    return hip_result(adamw_tensors(tensors, n, state_bits, adamw_hyper(*adam, step, grad_scale), (hipStream_t)hip_stream),
+                      "AdamW step");
+  });
+}
+
+rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state_bits, float* const* exp_avg,
+                        float* const* exp_avg_sq, void* hip_stream) {
+  return guarded([&]() -> rc_status {
+    if (n < 0 || (n > 0 && (!tensors || !exp_avg || !exp_avg_sq)))
+      return fail(RC_ERR_INVALID_ARG, "null argument or negative count");
+    if (state_bits != 32 && state_bits != 8) return fail(RC_ERR_INVALID_ARG, "state_bits must be 32 or 8");
+    for (int i = 0; i < n; ++i) {
+      const rc_adamw_tensor& t = tensors[i];
+      const std::string name = "tensor " + std::to_string(i) + ": ";
+      if (t.count < 0 || t.count > kMaxCount) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
+      if (t.count == 0) continue;
+      TRY(moment_args(t, state_bits, name));
+      if (!exp_avg[i] || !exp_avg_sq[i] || ((uintptr_t)exp_avg[i] | (uintptr_t)exp_avg_sq[i]) % 4)
+        return fail(RC_ERR_INVALID_ARG, name + "null or misaligned destination");
+    }
+    OnDevice on((hipStream_t)hip_stream);
+    if (on.err != hipSuccess) return hip_result(on.err, "device of the stream");
+    return hip_result(adamw_read(tensors, n, state_bits, exp_avg, exp_avg_sq, (hipStream_t)hip_stream), "AdamW read");
   });
 }
 

@@ -5,6 +5,8 @@
 //   state: flat fp32 master weights | fp32 gradients | Adam m | Adam v, then
 //          the bf16 copies of the weight matrices (bf16 stages).  Matrices of
 //          all layers come first, so weight decay applies to one prefix.
+//          (8-bit moments: in place of m and v two banks, each m codes | v codes |
+//          m scales | v scales, of which a step reads one and writes the other.)
 //   stash: the WeightGradStore (ReCycle, section 5): max_stashed_mb weight-pass
 //          slots (held from F to W) and max_inflight_mb forward-only slots
 //          (held from F to B), each laid out per layer.
@@ -23,6 +25,8 @@
 #include <utility>
 #include <vector>
 
+#include "adamw_op.h"
+#include "attn_op.h"
 #include "gemm.h"
 #include "kernels.h"
 #include "recycle_stage.h"
@@ -45,7 +49,7 @@ rc_status fail(rc_status s, const std::string& msg) {
 
 constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-long pad64(long n) { return (n + 63) / 64 * 64; }
+long pad_to(long n, long m) { return (n + m - 1) / m * m; }
 
 const int kMatrixIds[4] = {RC_P_W_QKV, RC_P_W_O, RC_P_W_1, RC_P_W_2};
 const int kVectorIds[8] = {RC_P_LN1_G, RC_P_LN1_B, RC_P_B_QKV, RC_P_B_O,
@@ -57,27 +61,38 @@ struct PLoc {
 
 // Byte offsets inside one layer of a weight-pass slot.
 struct WLayer {
-  size_t X, A, O, H, C, G, dY, dQKV, dH, dU, dA, dC, mu1, r1, mu2, r2, bytes;
+  // dB: gradient of the relative position bias, which B_input leaves here
+  size_t X, A, O, H, C, G, dY, dQKV, dH, dU, dA, dC, mu1, r1, mu2, r2, dB, bytes;
 };
 // Byte offsets inside one layer of a forward-only slot.
 struct FLayer {
   // Dg: gelu'(U) of the FFN, which the FC2 input gradient multiplies by (the
   // forward stores it instead of U: the same information for B_input, and the
   // derivative is formed where the fp32 U is at hand).  P: attention
-  // probabilities, or the row statistics (fused attention).  Or: what the
-  // bf16 rounding of O drops (fused attention below head dimension 128).
+  // probabilities, or the row statistics (fused attention), or what the
+  // attention operator keeps.  Or: what the bf16 rounding of O drops (fused
+  // attention below head dimension 128).
   size_t QKV, Dg, P, Or, bytes;
 };
+
+// Parameters of a layer: the twelve of rc_stage_config's layers and the relative position bias.
+constexpr int kParams = RC_NUM_PARAMS + 1;
 
 struct Layout {
   int L, h, a, d, f, s, b, elt, causal;
   long T;
   bool bf, flash;
+  bool op;          // attention by the operator's kernels (a window or a bias)
+  AttnOpArgs attn;  // its arguments but for the pointers
+  int buckets;
+  double pairs;     // visible (query, key) pairs of a head of one sequence
+  bool adam8;
   float eps;
   int wslots, fslots;
-  std::vector<std::array<PLoc, RC_NUM_PARAMS>> p;
+  std::vector<std::array<PLoc, kParams>> p;
   long n_mat, n_total;
   size_t off_master, off_grad, off_m, off_v, off_wb, state_bytes;
+  size_t off_bank, bank_bytes;  // 8-bit moments: two banks
   WLayer w;
   FLayer fl;
   size_t wslot_bytes, fslot_bytes, off_fslots, stash_bytes;
@@ -115,7 +130,48 @@ int reductions(const Layout& y, int l, float* grads, ColJob* jobs) {
   return n;
 }
 
-rc_status make_layout(const rc_stage_config* c, Layout& y) {
+// Visible (query, key) pairs of one head and sequence.
+double visible_pairs(long s, bool causal, long window, long sinks) {
+  double n = 0.0;
+  for (long i = 0; i < s; ++i) {
+    const long lo = window ? std::max(0L, i - window + 1) : 0;
+    const long hi = causal ? i + 1 : window ? std::min(s, i + window) : s;  // the window's keys [lo, hi)
+    n += hi - lo + std::min(lo, sinks) + (causal ? 0 : std::max(0L, sinks - hi));
+  }
+  return n;
+}
+
+rc_status option_layout(const rc_stage_config* c, const rc_stage_options* o, Layout& y) {
+  y.op = y.adam8 = false;
+  y.buckets = 0;
+  y.attn = {};
+  if (!o) return RC_OK;
+  if (o->adam_state_bits != 0 && o->adam_state_bits != 32 && o->adam_state_bits != 8)
+    return fail(RC_ERR_INVALID_ARG, "adam_state_bits must be 8 or 32");
+  if (o->static_work != 0 && o->static_work != 1) return fail(RC_ERR_INVALID_ARG, "static_work must be 0 or 1");
+  y.adam8 = o->adam_state_bits == 8;
+  if (o->window < 0 || o->sinks < 0 || o->buckets < 0)
+    return fail(RC_ERR_INVALID_ARG, "window, sinks and buckets must not be negative");
+  y.buckets = o->buckets;
+  y.op = o->buckets || (o->window && o->window < c->seq_len);
+  if (!y.op) return RC_OK;
+  rc_attention a = {};
+  a.dtype = c->dtype;
+  a.batch = c->micro_batch;
+  a.seq_len = c->seq_len;
+  a.heads = a.kv_heads = c->heads;
+  a.head_dim = c->hidden / c->heads;
+  a.causal = c->causal;
+  a.window = o->window;
+  a.sinks = o->sinks;
+  a.buckets = o->buckets;
+  a.max_distance = o->max_distance;
+  a.bias_dtype = RC_FP32;
+  a.scale = 1.0f / std::sqrt((float)a.head_dim);
+  return attn_op_check(a, y.attn);
+}
+
+rc_status make_layout(const rc_stage_config* c, Layout& y, const rc_stage_options* o = nullptr) {
   if (!c) return fail(RC_ERR_INVALID_ARG, "null config");
   if (c->num_layers < 1 || c->hidden < 1 || c->heads < 1 || c->ffn < 1 || c->seq_len < 1 ||
       c->micro_batch < 1)
@@ -140,10 +196,12 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
                                       "exceeds 2^31-1 bytes");
     if (2L * c->hidden * wide > cap)
       return fail(RC_ERR_UNSUPPORTED, "bf16 weight matrix [hidden, max(3*hidden, ffn)] exceeds 2^31-1 bytes");
-    if (d != 128 && 2L * c->seq_len * c->seq_len > cap)
+    if (d != 128 && !(o && (o->buckets > 0 || (o->window > 0 && o->window < c->seq_len))) && 2L * c->seq_len * c->seq_len > cap)
       return fail(RC_ERR_UNSUPPORTED, "bf16 attention probabilities [seq_len, seq_len] of one head "
                                       "exceed 2^31-1 bytes");
   }
+  const rc_status ro = option_layout(c, o, y);
+  if (ro != RC_OK) return ro;
   y.L = c->num_layers;
   y.h = c->hidden;
   y.a = c->heads;
@@ -154,42 +212,51 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
   y.T = (long)c->micro_batch * c->seq_len;
   y.bf = c->dtype == RC_BF16;
   y.elt = y.bf ? 2 : 4;
-  y.flash = attn_flash_supported(y.elt, d, c->seq_len);
+  y.flash = !y.op && attn_flash_supported(y.elt, d, c->seq_len);
+  y.pairs = !y.op ? (c->causal ? 0.5 : 1.0) * c->seq_len * c->seq_len
+                  : visible_pairs(c->seq_len, c->causal, o->window < c->seq_len ? o->window : 0, y.attn.sinks);
   y.causal = c->causal;
   y.eps = c->ln_eps;
   y.wslots = c->max_stashed_mb;
   y.fslots = c->max_inflight_mb;
   const long h = y.h, f = y.f;
-  const long msize[RC_NUM_PARAMS] = {h, h, h * 3 * h, 3 * h, h * h, h, h, h, h * f, f, f * h, h};
+  const long msize[kParams] = {h, h, h * 3 * h, 3 * h, h * h, h, h, h, h * f, f, f * h, h, (long)y.a * y.buckets};
+  const long unit = y.adam8 ? ADAMW_BLOCK : 64;  // no block of moments spans two parameters
   y.p.assign(y.L, {});
   long off = 0;
   for (int l = 0; l < y.L; ++l)
     for (int pid : kMatrixIds) {
       y.p[l][pid] = {off, msize[pid]};
-      off += pad64(msize[pid]);
+      off += pad_to(msize[pid], unit);
     }
   y.n_mat = off;
   for (int l = 0; l < y.L; ++l)
     for (int pid : kVectorIds) {
       y.p[l][pid] = {off, msize[pid]};
-      off += pad64(msize[pid]);
+      off += pad_to(msize[pid], unit);
     }
+  for (int l = 0; l < y.L; ++l) {
+    y.p[l][RC_P_REL_BIAS] = {off, msize[RC_P_REL_BIAS]};
+    off += pad_to(msize[RC_P_REL_BIAS], unit);
+  }
   y.n_total = off;
-  size_t o = 0;
+  size_t at = 0;
   auto take = [&](size_t bytes) {
-    size_t r = o;
-    o = align_up(o + bytes);
+    size_t r = at;
+    at = align_up(at + bytes);
     return r;
   };
   y.off_master = take(4 * y.n_total);
   y.off_grad = take(4 * y.n_total);
-  y.off_m = take(4 * y.n_total);
-  y.off_v = take(4 * y.n_total);
+  y.off_m = take(y.adam8 ? 0 : 4 * y.n_total);
+  y.off_v = take(y.adam8 ? 0 : 4 * y.n_total);
+  y.bank_bytes = y.adam8 ? align_up(2 * (y.n_total + y.n_total / ADAMW_BLOCK)) : 0;
+  y.off_bank = take(2 * y.bank_bytes);
   y.off_wb = take(y.bf ? 2 * y.n_mat : 0);
-  y.state_bytes = o;
+  y.state_bytes = at;
 
   const size_t E = y.elt, T = y.T;
-  o = 0;
+  at = 0;
   WLayer& w = y.w;
   w.X = take(T * h * E);
   w.A = take(T * h * E);
@@ -207,25 +274,26 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
   w.r1 = take(T * 4);
   w.mu2 = take(T * 4);
   w.r2 = take(T * 4);
-  w.bytes = o;
-  o = 0;
+  w.dB = take(4 * (size_t)y.a * y.buckets);
+  w.bytes = at;
+  at = 0;
   const size_t ss = (size_t)y.b * y.a * y.s * y.s;
   const size_t rows = (size_t)y.b * y.a * y.s;
   y.fl.QKV = take(T * 3 * h * E);
   y.fl.Dg = take(T * f * E);
   const bool narrow = y.flash && attn_flash_narrow(d);
-  y.fl.P = take(y.flash ? rows * (narrow ? 8 : 4) : ss * E);
+  y.fl.P = take(y.op ? attn_op_saved_bytes(y.attn, y.elt) : y.flash ? rows * (narrow ? 8 : 4) : ss * E);
   y.fl.Or = take(narrow ? T * h * E : 0);
-  y.fl.bytes = o;
+  y.fl.bytes = at;
   y.wslot_bytes = (size_t)y.L * w.bytes;
   y.fslot_bytes = (size_t)y.L * y.fl.bytes;
   y.off_fslots = (size_t)y.wslots * y.wslot_bytes;
   y.stash_bytes = y.off_fslots + (size_t)y.fslots * y.fslot_bytes;
-  o = 0;
-  y.off_S = take(y.flash ? 0 : ss * 4);
-  y.off_dS = take(y.flash ? 0 : ss * E);
+  at = 0;
+  y.off_S = take(y.flash || y.op ? 0 : ss * 4);
+  y.off_dS = take(y.flash || y.op ? 0 : ss * E);
   y.off_dO = take(T * h * E);
-  y.off_dv = take(y.flash ? rows * 4 : 0);
+  y.off_dv = take(y.op ? attn_op_work_bytes(y.attn, y.elt) : y.flash ? rows * 4 : 0);
   y.off_check = take(8 * GRAD_CHECK_BLOCKS);
   // Logical stash bytes per micro-batch (tensor sizes, no alignment padding):
   // from F to B_input the forward-written part of the weight-pass slot (X, A,
@@ -237,9 +305,11 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
     // Head dimensions other than 128 count the probabilities also where the
     // fused kernels keep less (row statistics and O's rest), so that limits and op lists
     // planned with these figures stay valid whichever kernels run.
-    const uint64_t attn = y.bf && d == 128 ? 4ull * rows : (uint64_t)E * ss;
+    const uint64_t attn = y.op ? 8ull * rows + (y.bf ? 2 * Th : 0)
+                          : y.bf && d == 128 ? 4ull * rows
+                                             : (uint64_t)E * ss;
     y.acct_af = (uint64_t)y.L * (E * (8 * Th + 2 * Tf) + st + attn);
-    y.acct_sw = (uint64_t)y.L * (E * (12 * Th + 2 * Tf) + st);
+    y.acct_sw = (uint64_t)y.L * (E * (12 * Th + 2 * Tf) + st + 4ull * y.a * y.buckets);
   }
   // Work memory of the products: partials of split reductions (split_floats,
   // taken where they fit) and partial bias sums of the bf16 weight-gradient
@@ -270,10 +340,10 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
   const long chunks = nw * ((y.T + 63) / 64);
   const size_t part = 8 * (chunks + (chunks + 15) / 16) * std::max(3 * h, f);
   const size_t cs = y.bf ? 4 * std::max((h + 255) / 256 * std::max(3 * h, f), (f + 255) / 256 * h) : 0;
-  const size_t need = align_up(o + part) + align_up(cs);
+  const size_t need = align_up(at + part) + align_up(cs);
   auto bias_floats = [&] { return y.cs_floats[0] + y.cs_floats[1] + y.cs_floats[2] + y.cs_floats[3]; };
   auto over = [&](long cs_bytes) {
-    return need <= RC_STATIC_WORK_BYTES && o + 4 * want_part + cs_bytes + 5 * kAlign > RC_STATIC_WORK_BYTES;
+    return need <= RC_STATIC_WORK_BYTES && at + 4 * want_part + cs_bytes + 5 * kAlign > RC_STATIC_WORK_BYTES;
   };
   if (over(4 * bias_floats())) {
     for (int i = 0; i < 4; ++i) y.cs_floats[i] = y.bf ? (shapes[i][0] + 255) / 256 * shapes[i][1] : 0;
@@ -282,13 +352,13 @@ rc_status make_layout(const rc_stage_config* c, Layout& y) {
   y.cs_shared = over(4 * bias_floats());
   y.part_floats = want_part;
   y.off_part = take(4 * want_part);
-  for (int i = 0; i < 4; ++i) y.off_cs[i] = y.cs_shared ? o : take(4 * y.cs_floats[i]);
+  for (int i = 0; i < 4; ++i) y.off_cs[i] = y.cs_shared ? at : take(4 * y.cs_floats[i]);
   if (y.cs_shared) take(4 * *std::max_element(y.cs_floats, y.cs_floats + 4));
-  y.off_split = o;
-  size_t total = std::max(need, align_up(o + 4 * want_split));
+  y.off_split = at;
+  size_t total = std::max(need, align_up(at + 4 * want_split));
   if (need <= RC_STATIC_WORK_BYTES) total = std::min(total, (size_t)RC_STATIC_WORK_BYTES);
-  total = std::max(total, o);
-  y.split_floats = std::min<long>(want_split, (total - o) / 4);
+  total = std::max(total, at);
+  y.split_floats = std::min<long>(want_split, (total - at) / 4);
   y.work_bytes = total;
   return RC_OK;
 }
@@ -312,6 +382,7 @@ struct rc_stage {
   std::vector<int> free_w, free_f;
   std::vector<rc_op_record> log;
   int64_t iter = 0, t = 0;
+  int bank = 0;  // 8-bit moments: the bank that holds the current ones
   bool grads_fresh = true;
   // Post-step validation: `closed` = the last call closed an iteration (step,
   // skip, rollback); a step can be rolled back while it is the last call.
@@ -336,7 +407,7 @@ namespace {
 
 struct WPtr {
   char *X, *A, *O, *H, *C, *G, *dY, *dQKV, *dH, *dU, *dA, *dC;
-  float *mu1, *r1, *mu2, *r2;
+  float *mu1, *r1, *mu2, *r2, *dB;
 };
 struct FPtr {
   char *QKV, *Dg, *P, *Or;
@@ -348,7 +419,7 @@ WPtr wptr(rc_stage* st, int slot, int l) {
   const WLayer& w = y.w;
   return {b + w.X, b + w.A, b + w.O, b + w.H, b + w.C, b + w.G, b + w.dY, b + w.dQKV,
           b + w.dH, b + w.dU, b + w.dA, b + w.dC, (float*)(b + w.mu1), (float*)(b + w.r1),
-          (float*)(b + w.mu2), (float*)(b + w.r2)};
+          (float*)(b + w.mu2), (float*)(b + w.r2), (float*)(b + w.dB)};
 }
 
 FPtr fptr(rc_stage* st, int slot, int l) {
@@ -456,9 +527,28 @@ void batch_heads(GemmParams& g, const Layout& y, long a_bs, long a_hs, long b_bs
   g.c_hs = c_hs;
 }
 
-rc_status attn_forward(rc_stage* st, char* QKV, char* P, char* O, char* Or) {
+// The attention operator over the heads of a packed [T, 3h] matrix: Q | K | V, or their gradients.
+AttnOpView packed_heads(const Layout& y, char* m, int block) {
+  return {el(m, (long)block * y.h, y.elt), 3L * y.h * y.s, 3L * y.h, y.d};
+}
+AttnOpArgs op_args(rc_stage* st, int l, char* QKV, char* O) {
+  const Layout& y = st->lay;
+  AttnOpArgs a = y.attn;
+  a.q = packed_heads(y, QKV, 0);
+  a.k = packed_heads(y, QKV, 1);
+  a.v = packed_heads(y, QKV, 2);
+  a.o = {O, (long)y.h * y.s, y.h, y.d};
+  if (y.buckets) a.bias = master(st, l, RC_P_REL_BIAS);
+  return a;
+}
+
+rc_status attn_forward(rc_stage* st, int l, char* QKV, char* P, char* O, char* Or) {
   const Layout& y = st->lay;
   const int E = y.elt;
+  if (y.op) {
+    HIPCHK(attn_op_forward(op_args(st, l, QKV, O), E, P, st->stream));
+    return RC_OK;
+  }
   if (y.flash) {
     HIPCHK(attn_flash_forward(QKV, O, Or, (float*)P, y.b, y.s, y.a, y.h, y.causal, st->stream));
     return RC_OK;
@@ -478,9 +568,19 @@ rc_status attn_forward(rc_stage* st, char* QKV, char* P, char* O, char* Or) {
   return RC_OK;
 }
 
-rc_status attn_backward(rc_stage* st, char* QKV, char* P, char* O, char* Or, char* dO, char* dQKV) {
+rc_status attn_backward(rc_stage* st, int l, char* QKV, char* P, char* O, char* Or, char* dO, char* dQKV, float* dB) {
   const Layout& y = st->lay;
   const int E = y.elt;
+  if (y.op) {
+    AttnOpArgs a = op_args(st, l, QKV, O);
+    a.dout = {dO, (long)y.h * y.s, y.h, y.d};
+    a.dq = packed_heads(y, dQKV, 0);
+    a.dk = packed_heads(y, dQKV, 1);
+    a.dv = packed_heads(y, dQKV, 2);
+    a.dbias = dB;
+    HIPCHK(attn_op_backward(a, E, P, st->work + y.off_dv, st->stream));
+    return RC_OK;
+  }
   if (y.flash) {
     HIPCHK(attn_flash_backward(QKV, O, Or, dO, (const float*)P, (float*)(st->work + y.off_dv), dQKV, y.b,
                                y.s, y.a, y.h, y.causal, st->stream));
@@ -519,7 +619,7 @@ rc_status run_forward(rc_stage* st, int ws, int fs, const void* x, void* yout) {
   const long T = y.T, h = y.h, f = y.f;
   hipStream_t s = st->stream;
   const double ln_f_bytes = 2.0 * T * h * E + 8.0 * T + 8.0 * h;
-  const double att = (y.causal ? 1.0 : 2.0) * y.b * (double)y.s * y.s * h;
+  const double att = 2.0 * y.b * y.pairs * h;
   for (int l = 0; l < L; ++l) {
     WPtr w = wptr(st, ws, l);
     FPtr fl = fptr(st, fs, l);
@@ -534,7 +634,7 @@ rc_status run_forward(rc_stage* st, int ws, int fs, const void* x, void* yout) {
     HIPCHK(gemm_lin(st, g, RC_K_GEMM_FWD));
     {
       Prof pa(st, RC_K_ATTN_FWD, 2.0 * att, 4.0 * T * h * E);
-      rc_status r = attn_forward(st, fl.QKV, fl.P, w.O, fl.Or);
+      rc_status r = attn_forward(st, l, fl.QKV, fl.P, w.O, fl.Or);
       if (r != RC_OK) return r;
     }
     g = gp(T, h, h, w.O, h, 1, weight(st, l, RC_P_W_O), h, 0, EPI_BIAS_RESID, w.H, h);
@@ -569,7 +669,7 @@ rc_status run_backward_input(rc_stage* st, int ws, int fs, const void* dy, void*
   hipStream_t s = st->stream;
   char* dO = st->work + y.off_dO;
   const double ln_b_bytes = 4.0 * T * h * E + 8.0 * T + 4.0 * h;
-  const double att = (y.causal ? 1.0 : 2.0) * y.b * (double)y.s * y.s * h;
+  const double att = 2.0 * y.b * y.pairs * h;
   for (int l = L - 1; l >= 0; --l) {
     WPtr w = wptr(st, ws, l);
     FPtr fl = fptr(st, fs, l);
@@ -600,7 +700,7 @@ rc_status run_backward_input(rc_stage* st, int ws, int fs, const void* dy, void*
     HIPCHK(gemm_lin(st, g, RC_K_GEMM_DGRAD));
     {
       Prof pa(st, RC_K_ATTN_BWD, 4.0 * att, 8.0 * T * h * E);
-      rc_status r = attn_backward(st, fl.QKV, fl.P, w.O, fl.Or, dO, w.dQKV);
+      rc_status r = attn_backward(st, l, fl.QKV, fl.P, w.O, fl.Or, dO, w.dQKV, w.dB);
       if (r != RC_OK) return r;
     }
     // dA = dQKV W_qkv^T
@@ -671,9 +771,39 @@ rc_status run_backward_weight(rc_stage* st, const int* ws, int n) {
     ColJob jobs[COLSUM_MAX_JOBS];
     const int njobs = reductions(y, l, grads, jobs);
     HIPCHK(colsum(E, sg, n, T, jobs, njobs, bias, nbias, acc, part, y.part_floats, s));
+    if (y.buckets) {
+      AttnOpShares sh;
+      for (int k = 0; k < n; ++k) sh.p[k] = (const float*)(sg.base + ws[k] * y.wslot_bytes + y.w.dB);
+      HIPCHK(attn_op_add_dbias(sh, n, y.p[l][RC_P_REL_BIAS].count, gradp(st, l, RC_P_REL_BIAS), acc, s));
+    }
   }
   return RC_OK;
 }
+
+// The stage's parameters as the two tensors of an 8-bit step: matrices (which
+// decay) and vectors.  The moments are those of `bank`.
+void adam8_tensors(rc_stage* st, int bank, rc_adamw_tensor* t) {
+  const Layout& y = st->lay;
+  char* b = st->state + y.off_bank + bank * y.bank_bytes;
+  const long n[2] = {y.n_mat, y.n_total - y.n_mat};
+  for (int i = 0; i < 2; ++i) {
+    const long off = i ? y.n_mat : 0;
+    t[i] = {};
+    t[i].param = (float*)(st->state + y.off_master) + off;
+    t[i].grad = (float*)(st->state + y.off_grad) + off;
+    t[i].exp_avg = b + off;
+    t[i].exp_avg_sq = b + y.n_total + off;
+    t[i].exp_avg_scale = (uint8_t*)b + 2 * y.n_total + off / ADAMW_BLOCK;
+    t[i].exp_avg_sq_scale = (uint8_t*)b + 2 * y.n_total + (y.n_total + off) / ADAMW_BLOCK;
+    t[i].copy = y.bf && !i ? st->state + y.off_wb : nullptr;
+    t[i].count = n[i];
+    t[i].grad_dtype = RC_FP32;
+    t[i].decay = !i;
+  }
+}
+
+// From the current bank of moments to the other one, in bytes.
+long other_bank(rc_stage* st) { return st->bank ? -(long)st->lay.bank_bytes : (long)st->lay.bank_bytes; }
 
 rc_status run_optimizer(rc_stage* st, float grad_scale) {
   const Layout& y = st->lay;
@@ -683,6 +813,13 @@ rc_status run_optimizer(rc_stage* st, float grad_scale) {
   float* M = (float*)(st->state + y.off_m);
   float* V = (float*)(st->state + y.off_v);
   if (st->grads_fresh) HIPCHK(fill_f32(G, y.n_total, 0.f, s));
+  if (y.adam8) {  // from the current bank to the other one
+    rc_adamw_tensor ts[2];
+    adam8_tensors(st, st->bank, ts);
+    Prof pr(st, RC_K_ADAM, 0, 16.0 * y.n_total + (y.bf ? 2.0 * y.n_mat : 0.0));
+    HIPCHK(adamw_banks(ts, 2, adamw_hyper(st->adam, st->t + 1, grad_scale), other_bank(st), false, s));
+    return RC_OK;
+  }
   const double t = (double)(st->t + 1);
   const rc_adam_config& a = st->adam;
   const double bc1 = 1.0 - std::pow((double)a.beta1, t);
@@ -698,6 +835,13 @@ rc_status run_optimizer(rc_stage* st, float grad_scale) {
 // gradient buffer: the next iteration's first weight pass overwrites them).
 rc_status run_rollback(rc_stage* st) {
   const Layout& y = st->lay;
+  if (y.adam8) {  // the other bank holds the moments that the step read
+    rc_adamw_tensor ts[2];
+    adam8_tensors(st, 1 - st->bank, ts);
+    Prof pr(st, RC_K_ADAM, 0, 14.0 * y.n_total + (y.bf ? 2.0 * y.n_mat : 0.0));
+    HIPCHK(adamw_banks(ts, 2, adamw_hyper(st->adam, st->t, st->last_scale), 0, true, st->stream));
+    return RC_OK;
+  }
   const double t = (double)st->t;
   const rc_adam_config& a = st->adam;
   const double bc1 = 1.0 - std::pow((double)a.beta1, t);
@@ -734,8 +878,30 @@ int take_min(std::vector<int>& v) {
 rc_status check_param(rc_stage* st, int layer, int pid) {
   if (!st) return fail(RC_ERR_INVALID_ARG, "null stage");
   if (layer < 0 || layer >= st->lay.L) return fail(RC_ERR_INVALID_ARG, "layer out of range");
-  if (pid < 0 || pid >= RC_NUM_PARAMS) return fail(RC_ERR_INVALID_ARG, "param_id out of range");
+  if (pid < 0 || pid >= (st->lay.buckets ? kParams : RC_NUM_PARAMS))
+    return fail(RC_ERR_INVALID_ARG, "param_id out of range");
   if (st->dry) return fail(RC_ERR_INVALID_ARG, "dry-run handle has no device memory");
+  return RC_OK;
+}
+
+// An 8-bit moment of a parameter as values on the host.
+rc_status read_moment8(rc_stage* st, int what, const PLoc& p, float* host_dst) {
+  const Layout& y = st->lay;
+  const bool second = what == RC_READ_ADAM_V;
+  const char* b = st->state + y.off_bank + st->bank * y.bank_bytes;
+  constexpr long kPiece = 1 << 20;  // elements on the host at a time
+  std::vector<uint8_t> codes(std::min(p.count, kPiece)), scales((codes.size() + ADAMW_BLOCK - 1) / ADAMW_BLOCK);
+  for (long at = 0; at < p.count; at += kPiece) {
+    const long n = std::min(p.count - at, kPiece), first = (second ? y.n_total : 0) + p.off + at;
+    HIPCHK(hipMemcpyAsync(codes.data(), b + first, n, hipMemcpyDeviceToHost, st->stream));
+    HIPCHK(hipMemcpyAsync(scales.data(), b + 2 * y.n_total + first / ADAMW_BLOCK, (n + ADAMW_BLOCK - 1) / ADAMW_BLOCK,
+                          hipMemcpyDeviceToHost, st->stream));
+    HIPCHK(hipStreamSynchronize(st->stream));
+    for (long i = 0; i < n; ++i) {
+      const int scale = scales[i / ADAMW_BLOCK];
+      host_dst[at + i] = second ? adamw_decode_v(codes[i], scale) : adamw_decode_m(codes[i], scale);
+    }
+  }
   return RC_OK;
 }
 
@@ -817,9 +983,14 @@ extern "C" {
 
 rc_status rc_stage_memory_requirements(const rc_stage_config* cfg, size_t* state_bytes,
                                        size_t* stash_bytes, size_t* work_bytes) {
+  return rc_stage_memory_requirements_with(cfg, nullptr, state_bytes, stash_bytes, work_bytes);
+}
+
+rc_status rc_stage_memory_requirements_with(const rc_stage_config* cfg, const rc_stage_options* options,
+                                            size_t* state_bytes, size_t* stash_bytes, size_t* work_bytes) {
   if (!state_bytes || !stash_bytes || !work_bytes) return fail(RC_ERR_INVALID_ARG, "null output pointer");
   Layout y;
-  rc_status r = make_layout(cfg, y);
+  rc_status r = make_layout(cfg, y, options);
   if (r != RC_OK) return r;
   *state_bytes = y.state_bytes;
   *stash_bytes = y.stash_bytes;
@@ -830,32 +1001,39 @@ rc_status rc_stage_memory_requirements(const rc_stage_config* cfg, size_t* state
 rc_status rc_stage_create(const rc_stage_config* cfg, const rc_adam_config* adam,
                           int32_t stage_index, int32_t pipeline_id, void* state_arena,
                           void* stash_arena, void* work_arena, void* hip_stream, rc_stage** out) {
-  if (!out || !adam) return fail(RC_ERR_INVALID_ARG, "null argument");
-  *out = nullptr;
-  Layout y;
-  rc_status r = make_layout(cfg, y);
-  if (r != RC_OK) return r;
-  return create_handle(y, cfg, adam, stage_index, pipeline_id, state_arena, stash_arena, work_arena,
-                       hip_stream, out);
+  return rc_stage_create_with(cfg, nullptr, adam, stage_index, pipeline_id, state_arena, stash_arena, work_arena,
+                              hip_stream, out);
 }
 
 rc_status rc_stage_create_static(const rc_stage_config* cfg, const rc_adam_config* adam,
                                  int32_t stage_index, int32_t pipeline_id, void* state_arena,
                                  void* stash_arena, void* hip_stream, rc_stage** out) {
+  rc_stage_options options = {};
+  options.static_work = 1;
+  return rc_stage_create_with(cfg, &options, adam, stage_index, pipeline_id, state_arena, stash_arena, nullptr,
+                              hip_stream, out);
+}
+
+rc_status rc_stage_create_with(const rc_stage_config* cfg, const rc_stage_options* options,
+                               const rc_adam_config* adam, int32_t stage_index, int32_t pipeline_id,
+                               void* state_arena, void* stash_arena, void* work_arena, void* hip_stream,
+                               rc_stage** out) {
   if (!out || !adam) return fail(RC_ERR_INVALID_ARG, "null argument");
   *out = nullptr;
   Layout y;
-  rc_status r = make_layout(cfg, y);
+  rc_status r = make_layout(cfg, y, options);
   if (r != RC_OK) return r;
-  if (y.work_bytes > kScratchBytes)
-    return fail(RC_ERR_UNSUPPORTED, "the configuration needs " + std::to_string(y.work_bytes) +
-                                        " bytes of work memory; the no-allocation work memory holds " +
-                                        std::to_string(kScratchBytes));
-  if (!state_arena || !stash_arena) return fail(RC_ERR_INVALID_ARG, "null state or stash arena");
-  void* work = nullptr;
-  r = scratch_address((hipStream_t)hip_stream, &work);
-  if (r != RC_OK) return r;
-  return create_handle(y, cfg, adam, stage_index, pipeline_id, state_arena, stash_arena, work, hip_stream,
+  if (options && options->static_work) {
+    if (y.work_bytes > kScratchBytes)
+      return fail(RC_ERR_UNSUPPORTED, "the configuration needs " + std::to_string(y.work_bytes) +
+                                          " bytes of work memory; the no-allocation work memory holds " +
+                                          std::to_string(kScratchBytes));
+    if (!state_arena || !stash_arena) return fail(RC_ERR_INVALID_ARG, "null state or stash arena");
+    if (work_arena) return fail(RC_ERR_INVALID_ARG, "static_work takes no work arena");
+    r = scratch_address((hipStream_t)hip_stream, &work_arena);
+    if (r != RC_OK) return r;
+  }
+  return create_handle(y, cfg, adam, stage_index, pipeline_id, state_arena, stash_arena, work_arena, hip_stream,
                        out);
 }
 
@@ -901,6 +1079,7 @@ rc_status rc_stage_read(rc_stage* st, int32_t what, int32_t layer, int32_t param
     default: return fail(RC_ERR_INVALID_ARG, "unknown read target");
   }
   const PLoc& p = st->lay.p[layer][param_id];
+  if (st->lay.adam8 && (what == RC_READ_ADAM_M || what == RC_READ_ADAM_V)) return read_moment8(st, what, p, host_dst);
   HIPCHK(hipMemcpyAsync(host_dst, (float*)(st->state + base) + p.off, 4 * p.count,
                         hipMemcpyDeviceToHost, st->stream));
   HIPCHK(hipStreamSynchronize(st->stream));
@@ -1057,6 +1236,7 @@ rc_status rc_stage_optimizer_step(rc_stage* st, float grad_scale) {
     if (r != RC_OK) return r;
   }
   st->t += 1;
+  st->bank ^= 1;
   record(st, RC_OP_STEP, -1, -1);
   st->mbs.clear();
   st->grads_fresh = true;
@@ -1094,6 +1274,7 @@ rc_status rc_stage_optimizer_rollback(rc_stage* st) {
     if (r != RC_OK) return r;
   }
   st->t -= 1;
+  st->bank ^= 1;
   record(st, RC_OP_ROLLBACK, -1, -1);
   st->log.back().iter = st->iter - 1;  // the iteration whose step is undone
   st->can_rollback = false;
@@ -1151,7 +1332,8 @@ rc_status rc_stage_attention_kernels(rc_stage* st, int32_t* kind) {
   if (!st || !kind) return fail(RC_ERR_INVALID_ARG, "null argument");
   const Layout& y = st->lay;
   const AttnForm form = attn_flash_form(y.b, y.s, y.a, y.d, y.causal);
-  *kind = !y.flash ? RC_ATTN_MATERIALISED
+  *kind = y.op       ? RC_ATTN_OPERATOR
+          : !y.flash ? RC_ATTN_MATERIALISED
           : form == ATTN_SPLIT ? RC_ATTN_SPLIT
           : form == ATTN_PAIRED ? RC_ATTN_PAIRED
                                 : RC_ATTN_BLOCK;

@@ -250,3 +250,28 @@ class AdamW:
             L.check(self._lib.rc_adamw_step(self._tensors, len(self.params), ctypes.byref(self.adam), self.state_bits,
                                             number, float(grad_scale), ctypes.c_void_p(stream.cuda_stream)))
         self.steps = number
+
+    def moments(self, out=None):
+        """The moments as fp32 values: (exp_avg, exp_avg_sq), lists of tensors, by
+        tensor.  out: two such lists to fill (contiguous fp32 tensors of the sizes)."""
+        torch = _torch()
+        if out is None:
+            out = [[torch.empty(p.numel(), dtype=torch.float32, device=p.device) for p in self.params]
+                   for _ in range(2)]
+        n = len(self.params)
+        arrays = []
+        for name, tensors in zip(("exp_avg", "exp_avg_sq"), out):
+            if len(tensors) != n:
+                raise ValueError(f"{name} must have {n} entries")
+            for i, (t, p) in enumerate(zip(tensors, self.params)):
+                if not isinstance(t, torch.Tensor) or t.device != self.device:
+                    raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
+                if t.dtype != torch.float32 or t.numel() != p.numel() or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {p.numel()} elements")
+            arrays.append((ctypes.c_void_p * max(1, n))(*[t.data_ptr() for t in tensors]))
+        if n:
+            ctx, stream = _on(self.device)
+            with ctx:
+                L.check(self._lib.rc_adamw_read(self._tensors, n, self.state_bits, *arrays,
+                                                ctypes.c_void_p(stream.cuda_stream)))
+        return out[0], out[1]

@@ -16,8 +16,12 @@ PARAM_NAMES = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o",
                "ln2_g", "ln2_b", "w_1", "b_1", "w_2", "b_2")
 
 
-def param_shape(pid: int, hidden: int, ffn: int) -> Tuple[int, ...]:
+def param_shape(pid: int, hidden: int, ffn: int, rel_bias: Tuple[int, int] = (0, 0)) -> Tuple[int, ...]:
+    """Shape of a parameter; rel_bias: (heads, buckets) of the relative position bias,
+    parameter 12 of the stages that have one."""
     h, f = hidden, ffn
+    if pid == L.RC_P_REL_BIAS and rel_bias[1]:
+        return tuple(rel_bias)
     return ((h,), (h,), (h, 3 * h), (3 * h,), (h, h), (h,),
             (h,), (h,), (h, f), (f,), (f, h), (h,))[pid]
 
@@ -35,16 +39,23 @@ class Stage:
 
     ``dry_run=True`` creates a bookkeeping-only handle (no device memory, no
     kernels): it validates op lists on the host.  ``static_work=True`` creates
-    the handle with rc_stage_create_static: its work memory is the library's
+    the handle with the work memory of rc_stage_create_static: the library's
     own per-device array, so only the state and stash arenas are allocated
-    here."""
+    here.
+
+    window, sinks: sliding-window attention whose first tokens stay visible
+    (see attention_forward).  rel_buckets: buckets of a learned relative position
+    bias [heads, rel_buckets], parameter 12 of every layer, zero until loaded.
+    adam_state_bits=8: 8-bit Adam moments (see AdamW)."""
 
     def __init__(self, *, num_layers: int, hidden: int, heads: int, ffn: int, seq_len: int,
                  micro_batch: int, causal: bool = True, dtype: str = "bf16",
                  ln_eps: float = 1e-5, max_stashed_mb: int = 1, max_inflight_mb: Optional[int] = None,
                  lr: float = 1e-4, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
                  weight_decay: float = 0.1, stage_index: int = 0, pipeline_id: int = 0,
-                 device=None, stream=None, dry_run: bool = False, static_work: bool = False):
+                 device=None, stream=None, dry_run: bool = False, static_work: bool = False,
+                 window: int = 0, sinks: int = 0, rel_buckets: int = 0, rel_max_distance: int = 128,
+                 adam_state_bits: int = 32):
         self._lib = L.load()
         self._h = None
         if dtype not in ("bf16", "f32"):
@@ -55,16 +66,18 @@ class Stage:
                                    ln_eps, max_stashed_mb,
                                    max_inflight_mb if max_inflight_mb is not None else max_stashed_mb)
         self.adam = L.RcAdamConfig(lr, beta1, beta2, eps, weight_decay)
+        self.options = L.RcStageOptions(window, sinks, rel_buckets, rel_max_distance if rel_buckets else 0,
+                                        adam_state_bits, 1 if static_work and not dry_run else 0)
+        self._rel_bias = (heads, rel_buckets)
         st, sh, wk = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
-        L.check(self._lib.rc_stage_memory_requirements(ctypes.byref(self.cfg), ctypes.byref(st),
-                                                       ctypes.byref(sh), ctypes.byref(wk)))
+        L.check(self._lib.rc_stage_memory_requirements_with(
+            ctypes.byref(self.cfg), ctypes.byref(self.options), ctypes.byref(st), ctypes.byref(sh),
+            ctypes.byref(wk)))
         self.state_bytes, self.stash_bytes, self.work_bytes = st.value, sh.value, wk.value
         self.dry_run = dry_run
         handle = ctypes.c_void_p()
         if dry_run:
-            L.check(self._lib.rc_stage_create(ctypes.byref(self.cfg), ctypes.byref(self.adam),
-                                              stage_index, pipeline_id, None, None, None, None,
-                                              ctypes.byref(handle)))
+            arenas, hip_stream = (None, None, None), None
         else:
             import torch
             if not torch.cuda.is_available():
@@ -74,11 +87,11 @@ class Stage:
             self._arenas = [torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
                             for n in sizes]
             self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
-            create = self._lib.rc_stage_create_static if static_work else self._lib.rc_stage_create
-            L.check(create(
-                ctypes.byref(self.cfg), ctypes.byref(self.adam), stage_index, pipeline_id,
-                *[ctypes.c_void_p(a.data_ptr()) for a in self._arenas],
-                ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(handle)))
+            arenas = [ctypes.c_void_p(a.data_ptr()) for a in self._arenas] + [None] * static_work
+            hip_stream = ctypes.c_void_p(self.stream.cuda_stream)
+        L.check(self._lib.rc_stage_create_with(
+            ctypes.byref(self.cfg), ctypes.byref(self.options), ctypes.byref(self.adam), stage_index,
+            pipeline_id, *arenas, hip_stream, ctypes.byref(handle)))
         self._h = handle
 
     @classmethod
@@ -199,11 +212,19 @@ class Stage:
         L.check(self._lib.rc_stage_optimizer_rollback(self._h))
 
     # -- state access -----------------------------------------------------------
+    @property
+    def num_params(self) -> int:
+        """Parameters of a layer: 12, and the relative position bias where there is one."""
+        return L.RC_NUM_PARAMS + (1 if self._rel_bias[1] else 0)
+
+    def _param_shape(self, pid: int) -> Tuple[int, ...]:
+        return param_shape(pid, self.cfg.hidden, self.cfg.ffn, self._rel_bias)
+
     def load_param(self, layer: int, pid: int, value) -> None:
         a = np.ascontiguousarray(value, dtype=np.float32)
-        if a.shape != param_shape(pid, self.cfg.hidden, self.cfg.ffn):
-            raise ValueError(f"param {PARAM_NAMES[pid]} has shape "
-                             f"{param_shape(pid, self.cfg.hidden, self.cfg.ffn)}, got {a.shape}")
+        if a.shape != self._param_shape(pid):
+            name = PARAM_NAMES[pid] if pid < L.RC_NUM_PARAMS else "rel_bias"
+            raise ValueError(f"param {name} has shape {self._param_shape(pid)}, got {a.shape}")
         L.check(self._lib.rc_stage_load_param(self._h, layer, pid, a.ctypes.data_as(ctypes.c_void_p)))
 
     def load_params(self, params: Sequence[Sequence[np.ndarray]]) -> None:
@@ -212,12 +233,12 @@ class Stage:
                 self.load_param(l, pid, v)
 
     def read(self, what: int, layer: int, pid: int) -> np.ndarray:
-        out = np.empty(param_shape(pid, self.cfg.hidden, self.cfg.ffn), dtype=np.float32)
+        out = np.empty(self._param_shape(pid), dtype=np.float32)
         L.check(self._lib.rc_stage_read(self._h, what, layer, pid, out.ctypes.data_as(ctypes.c_void_p)))
         return out
 
     def read_all(self, what: int) -> List[List[np.ndarray]]:
-        return [[self.read(what, l, p) for p in range(L.RC_NUM_PARAMS)]
+        return [[self.read(what, l, p) for p in range(self.num_params)]
                 for l in range(self.cfg.num_layers)]
 
     def op_log(self) -> List[Tuple[int, int, int, int, int, int]]:
@@ -235,11 +256,12 @@ class Stage:
 
     def attention_kernels(self) -> str:
         """Which attention kernels F and B_input run: "materialised", "block",
-        "paired" or "split" (chosen from the shape and the device's compute units)."""
+        "paired", "split" or "operator" (chosen from the shape and the device's compute units)."""
         k = ctypes.c_int32()
         L.check(self._lib.rc_stage_attention_kernels(self._h, ctypes.byref(k)))
         return {L.RC_ATTN_MATERIALISED: "materialised", L.RC_ATTN_BLOCK: "block",
-                L.RC_ATTN_PAIRED: "paired", L.RC_ATTN_SPLIT: "split"}[k.value]
+                L.RC_ATTN_PAIRED: "paired", L.RC_ATTN_SPLIT: "split",
+                L.RC_ATTN_OPERATOR: "operator"}[k.value]
 
     def set_stream(self, stream) -> None:
         self.stream = stream

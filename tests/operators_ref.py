@@ -67,7 +67,7 @@ def attention(q, k, v, do=None, *, causal=True, window=0, sinks=0, bias=None, ma
     if bias is not None:
         size = size + x.abs()
     # (what is hidden, or has a bias of -inf, is no part of any sum)
-    size = float(torch.where(x > -math.inf, size, 0.0).max())
+    size = float(torch.where(x > -math.inf, size, 0.0).detach().max())
     mag = {"score": size, "d": d, "o": (back(p @ v.abs()),)}
     if do is None:
         return out, mag

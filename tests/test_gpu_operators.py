@@ -428,3 +428,16 @@ def test_adamw_steps_as_the_stage_does():
         theirs = ops().AdamW(flat(RC_READ_PARAM), flat(RC_READ_GRAD), exp_avg=flat(RC_READ_ADAM_M),
                              exp_avg_sq=flat(RC_READ_ADAM_V), **args)
         check_adamw(theirs, before, grads, 0.5, step)
+
+
+@pytest.mark.parametrize("offset", [0, 1], ids=["aligned", "unaligned"])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_as_values(bits, offset):
+    p, g = adamw_set(SIZES, bits, F32, offset=offset)
+    opt = ops().AdamW(p, g, state_bits=bits)
+    for _ in range(2):
+        opt.step()
+    m, v = opt.moments()
+    for i, (_, wm, wv) in enumerate(state(opt)):
+        assert np.array_equal(m[i].cpu().numpy(), wm.astype(np.float32)), i
+        assert np.array_equal(v[i].cpu().numpy(), wv.astype(np.float32)), i
