@@ -379,8 +379,14 @@ def _own_adamw(st):
                            exp_avg_scale=blocks(st["m_exp"]) if eight else None,
                            exp_avg_sq_scale=blocks(st["v_exp"]) if eight else None,
                            lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY)
+        st["values"] = [torch.zeros_like(st["p"]) for _ in range(2 if eight else 0)]
+        st["parts"] = [parts(x) for x in st["values"]]
     st["step"].step(SCALE, step=STEP)
-    return _adamw_outputs(st)
+    if not st["values"]:
+        return _adamw_outputs(st)
+    st["step"].moments(out=st["parts"])   # the values that the codes stand for
+    out = {"p": st["p"], "m": st["values"][0], "v": st["values"][1]}
+    return out if st["copy"] is None else {**out, "copy": st["copy"]}
 
 
 # -- work and exact results -----------------------------------------------------------
