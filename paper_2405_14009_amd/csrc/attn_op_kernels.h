@@ -47,6 +47,7 @@ struct TileB16 {
   using A = Attn<HD_, false>;
   static constexpr int HD = HD_, TILE = A::TILE64;
   static constexpr bool ASYNC = true, REST = true;
+  static constexpr int WAVES = 2;  // a SIMD, of the kernels over queries
   using Rows = bf16x8[HD / 16];
   struct Offs {
     typename A::RowOffs ro;
@@ -105,6 +106,7 @@ struct TileF32 {
   using E = float;
   static constexpr int HD = HD_, LD = HD + 8, TILE = 64 * LD * 4;
   static constexpr bool ASYNC = false, REST = false;
+  static constexpr int WAVES = HD > 64 ? 1 : 2;
   // the halves of a wave hold half of the columns each
   using Rows = float[HD / 2];
   struct Offs {
@@ -231,6 +233,49 @@ struct AttnOp {
   static __device__ __forceinline__ void fill_table(const AttnOpArgs& p, int h, float* table) {
     for (int e = threadIdx.x; e < table_len(p); e += blockDim.x) table[e] = bias_at(p, h, e - table_off(p));
   }
+  // Adds a block (lane column = query, elements = keys) to a table by distance
+  // whose entry `to` belongs to this lane's query and key row 4 (lane / 32).
+  // With b = row_of(r) % 16, lane i of a row of 16 holds the distance that lane
+  // i - b holds at row 0, so each element is shifted by b lanes (an addition
+  // with a DPP operand) into the sum of its distance: to[0], to[16] for what
+  // leaves the row of lanes and for rows 16 and on, to[32] for both.  30
+  // additions and three LDS atomics for 16 elements; the 16 atomics without the
+  // shifts cost half of the kernel (us, dq of 13B's heads at s 4096, window
+  // 2048, 64 buckets: DIAG).
+  template <int R>
+  static __device__ __forceinline__ void shift_in(float& stays, float& leaves, const f32x16& x) {
+    constexpr int b = row_of(R) % 16;
+    const int v = __float_as_int(x[R]);
+    if constexpr (b == 0) {
+      stays += x[R];
+    } else {
+      stays += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x100 + b, 0xf, 0xf, true));         // lane i + b
+      leaves += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x110 + 16 - b, 0xf, 0xf, true));  // lane i + b - 16
+    }
+  }
+  static __device__ __forceinline__ void add_diagonals(float* to, const f32x16& x) {
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+    shift_in<0>(s0, s1, x);
+    shift_in<1>(s0, s1, x);
+    shift_in<2>(s0, s1, x);
+    shift_in<3>(s0, s1, x);
+    shift_in<4>(s0, s1, x);
+    shift_in<5>(s0, s1, x);
+    shift_in<6>(s0, s1, x);
+    shift_in<7>(s0, s1, x);
+    shift_in<8>(s1, s2, x);
+    shift_in<9>(s1, s2, x);
+    shift_in<10>(s1, s2, x);
+    shift_in<11>(s1, s2, x);
+    shift_in<12>(s1, s2, x);
+    shift_in<13>(s1, s2, x);
+    shift_in<14>(s1, s2, x);
+    shift_in<15>(s1, s2, x);
+    __hip_atomic_fetch_add(to, s0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    __hip_atomic_fetch_add(to + 16, s1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    __hip_atomic_fetch_add(to + 32, s2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+
   // x = sc sl2 + bias of 32 keys from k (element r, this lane: key k + 4 hh + row_of(r))
   // and this lane's query.
   // dir = 1: lane column = query, elements = keys; -1: the other way round.
@@ -535,9 +580,7 @@ struct AttnOp {
         for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - D);
         if constexpr (BIAS) {
           if (near) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              __hip_atomic_fetch_add(sums + e + row_of(r), dp[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            add_diagonals(sums + e, dp);
           } else {
             float t = 0.f;
 #pragma unroll
@@ -747,11 +790,13 @@ __global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
 extern __shared__ __attribute__((aligned(1024))) char attn_op_lds[];
 
 template <class T, bool BIAS>
-__global__ __launch_bounds__(256) void attn_op_fwd_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_fwd_k(
+    AttnOpArgs p) {
   AttnOp<T, BIAS>::fwd(p, attn_op_lds);
 }
 template <class T, bool BIAS>
-__global__ __launch_bounds__(256) void attn_op_dq_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_dq_k(
+    AttnOpArgs p) {
   AttnOp<T, BIAS>::dq(p, attn_op_lds);
 }
 template <class T, bool BIAS>
