@@ -35,17 +35,24 @@ struct AttnOpArgs {
   float* drow;   // [batch, heads, spad] rowsum(dO o O)
   float* bpart;  // [batch * heads * query blocks, buckets] shares of the bias gradient
   void* dbias;
-  // key blocks that hold sinks are seen by every query: their queries are
-  // split into chunks, whose shares of dK and dV are added up afterwards
+  // Grids of few blocks of 128 rows take 32 rows a workgroup instead, whose four
+  // waves share the other side's blocks.
+  int split_q, split_k;
+  // Every query sees the sinks.  Their keys (sink_rows: up to a multiple of 32)
+  // are handled twice: with the other keys for the queries whose window holds
+  // them, and by workgroups of 32 keys and chunk_len queries for the others; the
+  // shares of dK and dV are added up afterwards.  (chunks 0: short sequences;
+  // the sinks' own block visits every query.)
   float* spart;
-  int sink_blocks, chunks, chunk_len;
+  int sink_rows, chunks, chunk_len;
   unsigned short first[ATTN_OP_MAX_BUCKETS];  // first distance of each bucket of a side
   unsigned char bucket[ATTN_OP_MAX_FAR];      // of distances below `far`, one side
 };
 
+// bias_blocks: query blocks a head whose shares of the bias gradient are left in bpart.
 #define ATTN_OP_DECL(NAME)                                        \
   hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st); \
-  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st);
+  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st, int* bias_blocks);
 ATTN_OP_DECL(bf16_32)
 ATTN_OP_DECL(bf16_64)
 ATTN_OP_DECL(bf16_96)

@@ -76,6 +76,13 @@ int columns(int elt, int d) { return elt == 2 && d <= 32 ? 32 : d <= 64 ? 64 : e
 
 size_t rows(const AttnOpArgs& a) { return (size_t)a.batch * a.heads * a.spad; }
 
+// Work memory is the same for every form of the grid, so that its size does not
+// depend on the device.
+int sink_chunks(const AttnOpArgs& a) { return (a.s + a.chunk_len - 1) / a.chunk_len; }
+size_t bias_bytes(const AttnOpArgs& a) {
+  return align256(4 * (size_t)a.batch * a.heads * ((a.s + 31) / 32) * a.buckets);
+}
+
 }  // namespace
 
 // Fills what follows from the sizes: the window, buckets and the chunks of sink blocks.
@@ -99,12 +106,13 @@ void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
       a.bucket[n] = (unsigned char)c;
     }
   }
-  // Every query sees the sinks: their key blocks' queries go in chunks of about
-  // what another key block sees.
-  a.sink_blocks = (a.sinks + 127) / 128;
-  a.chunk_len = (((a.causal ? 1 : 2) * window + 128 + 63) / 64) * 64;
-  if (a.chunk_len < 512) a.chunk_len = 512;
-  a.chunks = a.sink_blocks ? (a.s + a.chunk_len - 1) / a.chunk_len : 1;
+  const long cus = device_compute_units(), blocks = (a.s + 31) / 32 * (long)a.batch;
+  a.split_q = blocks * a.heads <= cus;
+  a.split_k = blocks * a.kv_heads <= cus;
+  a.sink_rows = (a.sinks + 31) / 32 * 32;
+  a.chunk_len = 512;
+  while ((long)a.chunk_len * 64 < a.s) a.chunk_len *= 2;
+  a.chunks = a.sinks && !(a.split_k && a.s <= 2048) ? sink_chunks(a) : 0;
 }
 
 size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
@@ -112,11 +120,9 @@ size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
 }
 
 size_t attn_op_work_bytes(const AttnOpArgs& a, int elt) {
-  size_t n = align256(4 * rows(a));
-  if (a.buckets) n += align256(4 * (size_t)a.batch * a.heads * ((a.s + 127) / 128) * a.buckets);
-  if (a.chunks > 1)
-    n += align256(4 * (size_t)a.batch * a.kv_heads * a.sink_blocks * a.chunks * 2 * 128 * columns(elt, a.d));
-  return n;
+  return align256(4 * rows(a)) + bias_bytes(a) +
+         align256(4 * (size_t)a.batch * a.kv_heads * (a.sinks ? 1 + sink_chunks(a) : 0) * 2 * a.sink_rows *
+                  columns(elt, a.d));
 }
 
 namespace {
@@ -145,22 +151,22 @@ hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st) {
 
 hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work, hipStream_t st) {
   set_saved(a, saved);
-  const int nqb = (a.s + 127) / 128;
+  int nqb = 0;
   char* w = (char*)work;
   a.drow = (float*)w;
   w += align256(4 * rows(a));
   a.bpart = (float*)w;
-  if (a.buckets) w += align256(4 * (size_t)a.batch * a.heads * nqb * a.buckets);
+  w += bias_bytes(a);
   a.spart = (float*)w;
   const int c = columns(elt, a.d);
   hipError_t e;
   if (elt == 4)
-    e = c == 64 ? attn_op_bwd_f32_64(a, st) : attn_op_bwd_f32_128(a, st);
+    e = c == 64 ? attn_op_bwd_f32_64(a, st, &nqb) : attn_op_bwd_f32_128(a, st, &nqb);
   else
-    e = c == 32   ? attn_op_bwd_bf16_32(a, st)
-        : c == 64 ? attn_op_bwd_bf16_64(a, st)
-        : c == 96 ? attn_op_bwd_bf16_96(a, st)
-                  : attn_op_bwd_bf16_128(a, st);
+    e = c == 32   ? attn_op_bwd_bf16_32(a, st, &nqb)
+        : c == 64 ? attn_op_bwd_bf16_64(a, st, &nqb)
+        : c == 96 ? attn_op_bwd_bf16_96(a, st, &nqb)
+                  : attn_op_bwd_bf16_128(a, st, &nqb);
   if (e != hipSuccess || !a.bias) return e;
   if (a.bias_f32)
     hipLaunchKernelGGL(attn_op_dbias_k<float>, dim3(a.heads), dim3(256), 0, st, a.bpart, (float*)a.dbias, a.batch,

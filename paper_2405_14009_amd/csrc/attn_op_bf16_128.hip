@@ -1,5 +1,4 @@
 // Attention operator, bf16, kernels of 128 columns.
 #include "attn_op_kernels.h"
 
-hipError_t attn_op_fwd_bf16_128(const AttnOpArgs& a, hipStream_t st) { return attn_op_fwd_launch<TileB16<128>>(a, st); }
-hipError_t attn_op_bwd_bf16_128(const AttnOpArgs& a, hipStream_t st) { return attn_op_bwd_launch<TileB16<128>>(a, st); }
+ATTN_OP_DEFINE(bf16_128, TileB16<128>)

@@ -47,7 +47,8 @@ struct TileB16 {
   using A = Attn<HD_, false>;
   static constexpr int HD = HD_, TILE = A::TILE64;
   static constexpr bool ASYNC = true, REST = true;
-  static constexpr int WAVES = 2;  // a SIMD, of the kernels over queries
+  // waves a SIMD of the kernels over queries and keys
+  static constexpr int WAVES = 2, KWAVES = HD > 64 ? 1 : 2;
   using Rows = bf16x8[HD / 16];
   struct Offs {
     typename A::RowOffs ro;
@@ -68,9 +69,16 @@ struct TileB16 {
   static __device__ __forceinline__ void copy(char* tile, const Src& s, int wave, int lane, int row0, int nrows, int d) {
     A::template load_tile<64>(s.rs, tile, wave, lane, s.ld, row0, nrows, d);
   }
-  // 64 floats into a 1 KB area; issued by one wave
-  static __device__ __forceinline__ void vec(char* dst, const float* src, int lane) {
-    A::load_vec64(make_rsrc(src, 256), dst, lane, 0, 64);
+  // 32 rows by one wave alone
+  static __device__ __forceinline__ void copy_own(char* tile, const Src& s, int lane, int row0, int nrows, int d) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) A::template load_tile<32>(s.rs, tile, v, lane, s.ld, row0, nrows, d);
+  }
+  static __device__ __forceinline__ void own_landed() { A::own_copies_landed(); }
+  static __device__ __forceinline__ void own_read() { A::own_reads_done(); }
+  // n (32 or 64) floats into a 1 KB area; issued by one wave
+  static __device__ __forceinline__ void vec(char* dst, const float* src, int lane, int n = 64) {
+    A::load_vec64(make_rsrc(src, 4 * n), dst, lane, 0, n);
   }
   static __device__ __forceinline__ void rows(Rows& f, const E* base, long ld, int row, int nrows, int lane, int d) {
     A::load_stationary(f, base, ld, row, nrows, lane, d);
@@ -79,6 +87,10 @@ struct TileB16 {
   static __device__ __forceinline__ void score2(f32x16& a0, const char* t0, int b0, const Rows& s0, f32x16& a1,
                                                 const char* t1, int b1, const Rows& s1, const Offs& o, int) {
     A::template two_chains<2>(a0, t0, b0, s0, a1, t1, b1, s1, o.ro);
+  }
+  static __device__ __forceinline__ void score1(f32x16& a, const char* t, const Rows& s, const Offs& o, int) {
+#pragma unroll
+    for (int ks = 0; ks < HD / 16; ++ks) a = A::mfma(A::rd_row(t, o.ro, 0, ks), s[ks], a);
   }
   // a += rows x times rows y, both from registers
   static __device__ __forceinline__ void dot(f32x16& a, const Rows& x, const Rows& y) {
@@ -99,6 +111,11 @@ struct TileB16 {
                                                int nrows, int lane, float mul, int d) {
     A::store_rows_lds(acc, t, base, ld, row0, nrows, lane, mul, d);
   }
+  // columns 32 b.. alone
+  static __device__ __forceinline__ void store_cols(const f32x16& acc, E* base, long ld, int row0, int nrows, int b,
+                                                    int lane, float mul, int d) {
+    A::store_block(acc, base, ld, row0 + (lane & 31), nrows, b, lane, mul, d);
+  }
 };
 
 template <int HD_>
@@ -106,7 +123,7 @@ struct TileF32 {
   using E = float;
   static constexpr int HD = HD_, LD = HD + 8, TILE = 64 * LD * 4;
   static constexpr bool ASYNC = false, REST = false;
-  static constexpr int WAVES = HD > 64 ? 1 : 2;
+  static constexpr int WAVES = HD > 64 ? 1 : 2, KWAVES = 1;
   // the halves of a wave hold half of the columns each
   using Rows = float[HD / 2];
   struct Offs {
@@ -128,7 +145,21 @@ struct TileF32 {
       *(float4*)((float*)tile + r * LD + c) = v;
     }
   }
-  static __device__ __forceinline__ void vec(char* dst, const float* src, int lane) { ((float*)dst)[lane] = src[lane]; }
+  static __device__ __forceinline__ void copy_own(char* tile, const Src& s, int lane, int row0, int nrows, int d) {
+#pragma unroll
+    for (int n = 0; n < HD / 8; ++n) {
+      const int i = 64 * n + lane, r = i / (HD / 4), c = 4 * (i % (HD / 4));
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (row0 + r < nrows && c < d) v = *(const float4*)(s.p + (long)(row0 + r) * s.ld + c);
+      *(float4*)((float*)tile + r * LD + c) = v;
+    }
+  }
+  // (one wave's LDS accesses complete in order)
+  static __device__ __forceinline__ void own_landed() { asm volatile("" ::: "memory"); }
+  static __device__ __forceinline__ void own_read() { asm volatile("" ::: "memory"); }
+  static __device__ __forceinline__ void vec(char* dst, const float* src, int lane, int n = 64) {
+    if (lane < n) ((float*)dst)[lane] = src[lane];
+  }
   static __device__ __forceinline__ void rows(Rows& f, const E* base, long ld, int row, int nrows, int lane, int d) {
 #pragma unroll
     for (int k = 0; k < HD / 2; k += 4) {
@@ -161,6 +192,17 @@ struct TileF32 {
       a1 = mfma(w.w, s1[k + 3], a1);
     }
   }
+  static __device__ __forceinline__ void score1(f32x16& a, const char* t, const Rows& s, const Offs&, int lane) {
+    const float* x = (const float*)t + (lane & 31) * LD + (lane >> 5) * (HD / 2);
+#pragma unroll
+    for (int k = 0; k < HD / 2; k += 4) {
+      const float4 u = *(const float4*)(x + k);
+      a = mfma(u.x, s[k], a);
+      a = mfma(u.y, s[k + 1], a);
+      a = mfma(u.z, s[k + 2], a);
+      a = mfma(u.w, s[k + 3], a);
+    }
+  }
   static __device__ __forceinline__ void dot(f32x16& a, const Rows& x, const Rows& y) {
 #pragma unroll
     for (int k = 0; k < HD / 2; ++k) a = mfma(x[k], y[k], a);
@@ -173,18 +215,21 @@ struct TileF32 {
 #pragma unroll
       for (int b = 0; b < HD / 32; ++b) acc[b] = mfma(x[row_of(r) * LD + 32 * b], p[r], acc[b]);
   }
-  static __device__ __forceinline__ void store(const f32x16 (&acc)[HD / 32], char*, E* base, long ld, int row0,
-                                               int nrows, int lane, float mul, int d) {
+  static __device__ __forceinline__ void store_cols(const f32x16& acc, E* base, long ld, int row0, int nrows, int b,
+                                                    int lane, float mul, int d) {
     const int row = row0 + (lane & 31);
     if (row >= nrows) return;
-    E* p = base + (long)row * ld + 4 * (lane >> 5);
+    E* p = base + (long)row * ld + 32 * b + 4 * (lane >> 5);
 #pragma unroll
-    for (int b = 0; b < HD / 32; ++b)
+    for (int g = 0; g < 4; ++g)
+      if (32 * b + 8 * g + 4 * (lane >> 5) < d)
+        *(float4*)(p + 8 * g) =
+            make_float4(acc[4 * g] * mul, acc[4 * g + 1] * mul, acc[4 * g + 2] * mul, acc[4 * g + 3] * mul);
+  }
+  static __device__ __forceinline__ void store(const f32x16 (&acc)[HD / 32], char*, E* base, long ld, int row0,
+                                               int nrows, int lane, float mul, int d) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        if (32 * b + 8 * g + 4 * (lane >> 5) < d)
-          *(float4*)(p + 32 * b + 8 * g) = make_float4(acc[b][4 * g] * mul, acc[b][4 * g + 1] * mul,
-                                                       acc[b][4 * g + 2] * mul, acc[b][4 * g + 3] * mul);
+    for (int b = 0; b < HD / 32; ++b) store_cols(acc[b], base, ld, row0, nrows, b, lane, mul, d);
   }
 };
 
@@ -239,9 +284,8 @@ struct AttnOp {
   // i - b holds at row 0, so each element is shifted by b lanes (an addition
   // with a DPP operand) into the sum of its distance: to[0], to[16] for what
   // leaves the row of lanes and for rows 16 and on, to[32] for both.  30
-  // additions and three LDS atomics for 16 elements; the 16 atomics without the
-  // shifts cost half of the kernel (us, dq of 13B's heads at s 4096, window
-  // 2048, 64 buckets: DIAG).
+  // additions and three LDS atomics for 16 elements (us, dq of 40 heads of 128, s
+  // 4096, window 2048, 64 buckets: 469, against 821 with sixteen atomics).
   template <int R>
   static __device__ __forceinline__ void shift_in(float& stays, float& leaves, const f32x16& x) {
     constexpr int b = row_of(R) % 16;
@@ -297,17 +341,18 @@ struct AttnOp {
     int n1, t0, n;
     __device__ __forceinline__ int tile(int it) const { return it < n1 ? it : it - n1 + t0; }
   };
-  // key tiles of 64 for the queries [q0, q1]
+  // key tiles of NK for the queries [q0, q1]
+  template <int NK>
   static __device__ __forceinline__ Steps key_steps(const AttnOpArgs& p, int q0, int q1, int len) {
     Steps s;
     q1 = min(q1, len - 1);
     if (q1 < q0) return {0, 0, 0};
     const int lo = max(0, q0 - p.left), hi = min((long)len - 1, (long)q1 + p.right);
     const int ns = p.causal ? min(p.sinks, q1 + 1) : min(p.sinks, len);
-    const int nts = (ns + 63) / 64;
-    s.t0 = lo / 64;
+    const int nts = (ns + NK - 1) / NK;
+    s.t0 = lo / NK;
     s.n1 = min(nts, s.t0);
-    s.n = s.n1 + max(hi / 64, nts - 1) - s.t0 + 1;
+    s.n = s.n1 + max(hi / NK, nts - 1) - s.t0 + 1;
     return s;
   }
   // For 32 queries from q0 and NK keys from k0: whether none / all pairs are visible.
@@ -325,6 +370,46 @@ struct AttnOp {
     return k0 + NK <= p.sinks && (!p.causal || k0 + NK - 1 <= q0);
   }
 
+  // Key blocks visit one of three sets of pairs: those of the windows, those that
+  // are visible to a sink alone, or both.
+  enum { WINDOW, SINK, BOTH };
+  template <int MODE>
+  static __device__ __forceinline__ bool none_of(const AttnOpArgs& p, int q0, int k0, int len) {
+    if (q0 >= len || k0 >= len || (p.causal && k0 > q0 + 31)) return true;
+    const bool window = k0 - (q0 + 31) <= p.right && k0 + 31 - q0 >= -p.left;
+    const bool sink = k0 < p.sinks && (k0 - (q0 + 31) < -p.left || k0 + 31 - q0 > p.right);
+    return MODE == WINDOW ? !window : MODE == SINK ? !sink : !window && !sink;
+  }
+  template <int MODE>
+  static __device__ __forceinline__ bool all_of(const AttnOpArgs& p, int q0, int k0, int len) {
+    if (q0 + 32 > len || k0 + 32 > len) return false;
+    const bool window = k0 + 31 - q0 <= p.right && k0 - (q0 + 31) >= -p.left;
+    if (MODE != SINK && window) return true;
+    if (MODE == WINDOW || k0 + 32 > p.sinks || (p.causal && k0 + 31 > q0)) return false;
+    return MODE == BOTH || k0 + 31 - q0 < -p.left || k0 - (q0 + 31) > p.right;
+  }
+  // Lane column = key kk, elements = the queries q + 4 hh + row_of(r): others become 0.
+  template <int MODE>
+  static __device__ __forceinline__ void mask_queries(f32x16& sc, int q, int kk, int lane, int len, const AttnOpArgs& p) {
+    const int at = q + 4 * (lane >> 5);
+    const bool sink = MODE != WINDOW && kk < p.sinks;
+    int lo = (int)max(0L, (long)kk - p.right) - at;                  // the window's queries [lo, hi]
+    int hi = (int)min((long)len - 1, (long)kk + p.left) - at;
+    int first = p.causal ? kk - at : -at, last = len - 1 - at;       // a sink's
+    if (kk >= len) hi = lo - 1;
+    if (kk >= len || !sink) first = 1, last = 0;
+    if (hi < lo) lo = 1 << 29, hi = lo;
+    const unsigned w = (unsigned)(hi - lo);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int t = row_of(r);
+      const bool window = (unsigned)(t - lo) <= w;
+      const bool any = t >= first && t <= last;
+      const bool keep = MODE == WINDOW ? window : MODE == SINK ? any && !window : window || any;
+      if (!keep) sc[r] = 0.f;
+    }
+  }
+
   // Lane column = query qq, elements = the keys k + 4 hh + row_of(r): masked ones become v.
   static __device__ __forceinline__ void mask_keys(f32x16& sc, int k, int qq, int lane, float v, int len,
                                                    const AttnOpArgs& p) {
@@ -340,18 +425,6 @@ struct AttnOp {
       if (!((unsigned)(t - lo) <= w || t < sink)) sc[r] = v;
     }
   }
-  // Lane column = key kk, elements = the queries q + 4 hh + row_of(r).
-  static __device__ __forceinline__ void query_range(int& lo, unsigned& w, int q, int kk, int lane, int len,
-                                                     const AttnOpArgs& p) {
-    const int at = q + 4 * (lane >> 5);
-    const bool sink = kk < p.sinks;
-    lo = (int)max(0L, sink && !p.causal ? 0L : (long)kk - p.right) - at;
-    int hi = (int)(sink ? (long)len - 1 : min((long)len - 1, (long)kk + p.left)) - at;
-    if (kk >= len) hi = lo - 1;
-    if (hi < lo) lo = 1 << 29, hi = lo;
-    w = (unsigned)(hi - lo);
-  }
-
   // body(stage, it) for n steps, whose operands issue(stage, it) copies: the next
   // step's while this one computes, or (copies through registers) its own.  The
   // caller has issued step 0 in the first case.
@@ -379,30 +452,32 @@ struct AttnOp {
     f32x16 o[NB];
     float m, l;
   };
-  static __device__ __forceinline__ void fwd_tile(Fwd& st, const Rows& qf, const char* kt, const char* vt, const Offs& of,
-                                                  int k0, int q0, int qq, int lane, int len, const float* table,
-                                                  const AttnOpArgs& p) {
-    if (none_visible<64>(p, q0, k0, len)) return;
-    f32x16 sc[2];
-    zero(sc[0]);
-    zero(sc[1]);
-    T::score2(sc[0], kt, 0, qf, sc[1], kt, 1, qf, of, lane);
+  static __device__ __forceinline__ void reset(Fwd& st) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) zero(st.o[i]);
+    st.m = kNone;
+    st.l = 0.f;
+  }
+  // Scores of N blocks of 32 keys from k0 to exponentials, with the state moved to their maximum.
+  template <int N>
+  static __device__ __forceinline__ void softmax(Fwd& st, f32x16 (&sc)[N], int k0, int q0, int qq, int lane, int len,
+                                                 const float* table, const AttnOpArgs& p) {
     if constexpr (BIAS) {
       const int rel = k0 - q0;
-      const bool near = wave_uniform(rel + 63 > -p.far && rel - 31 < p.far);
+      const bool near = wave_uniform(rel + 32 * N - 1 > -p.far && rel - 31 < p.far);
       const int e = k0 + 4 * (lane >> 5) - qq + table_off(p);
       float c = 0.f;
       if (!near) c = rel < 0 ? table[0] : table[table_len(p) - 1];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) add_bias<1>(sc[j], table, e + 32 * j, c, near, p);
+      for (int j = 0; j < N; ++j) add_bias<1>(sc[j], table, e + 32 * j, c, near, p);
     }
-    if (wave_uniform(!all_visible<32, 64>(p, q0, k0, len))) {
-      mask_keys(sc[0], k0, qq, lane, -INFINITY, len, p);
-      mask_keys(sc[1], k0 + 32, qq, lane, -INFINITY, len, p);
+    if (wave_uniform(!all_visible<32, 32 * N>(p, q0, k0, len))) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) mask_keys(sc[j], k0 + 32 * j, qq, lane, -INFINITY, len, p);
     }
     float mx = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[j][r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -421,7 +496,7 @@ struct AttnOp {
     }
     float ls = 0.f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float e = __builtin_amdgcn_exp2f(BIAS ? sc[j][r] - st.m : fmaf(sc[j][r], p.sl2, -st.m));
@@ -429,6 +504,16 @@ struct AttnOp {
         ls += e;
       }
     st.l += ls;
+  }
+  static __device__ __forceinline__ void fwd_tile(Fwd& st, const Rows& qf, const char* kt, const char* vt, const Offs& of,
+                                                  int k0, int q0, int qq, int lane, int len, const float* table,
+                                                  const AttnOpArgs& p) {
+    if (none_visible<64>(p, q0, k0, len)) return;
+    f32x16 sc[2];
+    zero(sc[0]);
+    zero(sc[1]);
+    T::score2(sc[0], kt, 0, qf, sc[1], kt, 1, qf, of, lane);
+    softmax<2>(st, sc, k0, q0, qq, lane, len, table, p);
     T::outer(st.o, vt, 0, sc[0], of, lane);
     T::outer(st.o, vt, 1, sc[1], of, lane);
   }
@@ -444,7 +529,7 @@ struct AttnOp {
     const int b = z / p.heads, h = z % p.heads;
     const int len = length(p, b);
     const int q0 = qb * 128 + 32 * wave, qq = q0 + (lane & 31);
-    const Steps steps = key_steps(p, qb * 128, qb * 128 + 127, len);
+    const Steps steps = key_steps<64>(p, qb * 128, qb * 128 + 127, len);
     Src ks, vs;
     ks.set(base(p.k, b, h / p.group), p.k.t, len);
     vs.set(base(p.v, b, h / p.group), p.v.t, len);
@@ -460,21 +545,144 @@ struct AttnOp {
     Offs of;
     of.init(lane);
     Fwd st;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) zero(st.o[i]);
-    st.m = kNone;
-    st.l = 0.f;
+    reset(st);
     pipeline(steps.n, lds, STAGE, issue, [&](char* cur, int it) {
       fwd_tile(st, qf, cur, cur + TILE, of, steps.tile(it) * 64, q0, qq, lane, len, table, p);
     });
-    // rows without a visible token: zeros
-    const float l = st.l + __shfl_xor(st.l, 32, 64);
-    const float inv = l > 0.f ? 1.0f / l : (l == l ? 0.f : l);
+    fwd_store(st, p, b, h, q0, qq, len, lane, lds + wave * (STAGE / 4));
+  }
+
+  // 32 queries a workgroup: its waves take every fourth block of 32 keys, with
+  // tiles of their own, and join their sums through LDS.
+  static constexpr int OWN = 2 * (TILE / 2);
+  static_assert(NB * 4096 <= OWN, "a wave's sums in its tiles");
+  static __device__ __forceinline__ void fwd32(const AttnOpArgs& p, char* lds) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* const own = lds + wave * OWN;
+    float2* const stats = (float2*)(lds + 4 * OWN);  // [wave][lane]
+    float* const table = (float*)(lds + 4 * OWN + 2048);
+    const int bh = p.batch * p.heads, nqb = (p.s + 31) / 32;
+    const int z = blockIdx.x % bh, q0 = 32 * (nqb - 1 - blockIdx.x / bh), qq = q0 + (lane & 31);
+    const int b = z / p.heads, h = z % p.heads;
+    const int len = length(p, b);
+    const Steps steps = key_steps<32>(p, q0, q0 + 31, len);
+    Src ks, vs;
+    ks.set(base(p.k, b, h / p.group), p.k.t, len);
+    vs.set(base(p.v, b, h / p.group), p.v.t, len);
+    auto issue = [&](int it) {
+      const int k0 = steps.tile(it) * 32;
+      T::copy_own(own, ks, lane, k0, len, p.d);
+      T::copy_own(own + TILE / 2, vs, lane, k0, len, p.d);
+    };
+    if (wave < steps.n) issue(wave);
+    Rows qf;
+    T::rows(qf, base(p.q, b, h), p.q.t, qq, len, lane, p.d);
+    Offs of;
+    of.init(lane);
+    Fwd st;
+    reset(st);
+    if constexpr (BIAS) {
+      fill_table(p, h, table);
+      __syncthreads();
+    }
+    for (int it = wave; it < steps.n; it += 4) {
+      T::own_landed();
+      const int k0 = steps.tile(it) * 32;
+      if (!none_visible<32>(p, q0, k0, len)) {
+        f32x16 sc[1];
+        zero(sc[0]);
+        T::score1(sc[0], own, qf, of, lane);
+        softmax<1>(st, sc, k0, q0, qq, lane, len, table, p);
+        T::outer(st.o, own + TILE / 2, 0, sc[0], of, lane);
+      }
+      T::own_read();
+      if (it + 4 < steps.n) issue(it + 4);
+    }
+    put<NB>(st.o, own, lane);
+    stats[wave * 64 + lane] = make_float2(st.m, st.l);
+    __syncthreads();
+    // every wave joins the four states, wave 0 the statistics, each the columns it stores
+    float m = kNone, scale[4];
+    float l = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m = fmaxf(m, stats[u * 64 + lane].x);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float2 t = stats[u * 64 + lane];
+      scale[u] = __builtin_amdgcn_exp2f(t.x - m);
+      l += scale[u] * t.y;
+    }
+    st.m = m;
+    st.l = l;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      zero(st.o[i]);
+      if (i % 4 != wave) continue;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) add_scaled(st.o[i], lds + u * OWN, i, lane, scale[u]);
+    }
+    float inv;
+    const bool some = finish(st, inv, qq, len);
+    E* const to = out(p.o, b, h);
+    E* const rest = T::REST && p.m ? (E*)p.rest + ((long)b * p.s * p.heads + h) * p.d : nullptr;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (i % 4 != wave) continue;
+      T::store_cols(st.o[i], to, p.o.t, q0, p.s, i, lane, inv, p.d);
+      if constexpr (T::REST) {
+        if (!rest) continue;
+        T::A::keep_rest(st.o[i], inv);
+        T::store_cols(st.o[i], rest, (long)p.heads * p.d, q0, p.s, i, lane, 1.0f, p.d);
+      }
+    }
+    if (p.m && wave == 0) store_stats(st, p, z, qq, some, lane);
+  }
+
+  // A wave's blocks to its area, in chunks of 16 bytes a lane; and one of them back, scaled and added.
+  template <int N>
+  static __device__ __forceinline__ void put(const f32x16 (&a)[N], char* area, int lane) {
+    float4* to = (float4*)area + lane;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        to[(4 * i + c) * 64] = make_float4(a[i][4 * c], a[i][4 * c + 1], a[i][4 * c + 2], a[i][4 * c + 3]);
+  }
+  static __device__ __forceinline__ void add_scaled(f32x16& a, const char* area, int i, int lane, float mul) {
+    const float4* from = (const float4*)area + lane;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float4 v = from[(4 * i + c) * 64];
+      a[4 * c] += v.x * mul;
+      a[4 * c + 1] += v.y * mul;
+      a[4 * c + 2] += v.z * mul;
+      a[4 * c + 3] += v.w * mul;
+    }
+  }
+
+  // 1 / sum of this lane's row (0 for a row without a visible token, whose sums become zeros);
+  // whether there is one.
+  static __device__ __forceinline__ bool finish(Fwd& st, float& inv, int qq, int len) {
+    st.l += __shfl_xor(st.l, 32, 64);
+    const bool some = st.l > 0.f || st.l != st.l;
+    inv = some ? 1.0f / st.l : 0.f;
     if (qq >= len) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) zero(st.o[i]);
     }
-    char* const area = lds + wave * (STAGE / 4);
+    return some;
+  }
+  static __device__ __forceinline__ void store_stats(const Fwd& st, const AttnOpArgs& p, int z, int qq, bool some,
+                                                     int lane) {
+    if (lane >= 32 || qq >= p.spad) return;
+    p.m[(long)z * p.spad + qq] = some ? st.m : 0.f;
+    p.l[(long)z * p.spad + qq] = some ? __builtin_amdgcn_logf(st.l) : 0.f;
+  }
+  static __device__ __forceinline__ void fwd_store(Fwd& st, const AttnOpArgs& p, int b, int h, int q0, int qq, int len,
+                                                   int lane, char* area) {
+    float inv;
+    const bool some = finish(st, inv, qq, len);
     T::store(st.o, area, out(p.o, b, h), p.o.t, q0, p.s, lane, inv, p.d);
     if (!p.m) return;
     if constexpr (T::REST) {
@@ -483,17 +691,129 @@ struct AttnOp {
       T::store(st.o, area, (E*)p.rest + ((long)b * p.s * p.heads + h) * p.d, (long)p.heads * p.d, q0, p.s, lane, 1.0f,
                p.d);
     }
-    if (lane < 32 && qq < p.spad) {
-      const bool some = l > 0.f || l != l;
-      p.m[(long)z * p.spad + qq] = some ? st.m : 0.f;
-      p.l[(long)z * p.spad + qq] = some ? __builtin_amdgcn_logf(l) : 0.f;
-    }
+    store_stats(st, p, b * p.heads + h, qq, some, lane);
   }
 
   // -- dq, dbias and D -----------------------------------------------------------
   // P of a score block in place; x: after add_bias with BIAS, raw products otherwise.
   static __device__ __forceinline__ float prob(float x, float m, float l, const AttnOpArgs& p) {
     return __builtin_amdgcn_exp2f((BIAS ? x - m : fmaf(x, p.sl2, -m)) - l);
+  }
+
+  // A wave's 32 queries: rows of q and dout, statistics and D.
+  struct Queries {
+    Rows q, d;
+    float m, l, D;
+  };
+  static __device__ __forceinline__ void load_queries(Queries& w, const AttnOpArgs& p, int b, int h, int qq, int len,
+                                                      int lane, bool write) {
+    const long row = ((long)b * p.heads + h) * p.spad + qq;
+    T::rows(w.q, base(p.q, b, h), p.q.t, qq, len, lane, p.d);
+    T::rows(w.d, base(p.dout, b, h), p.dout.t, qq, len, lane, p.d);
+    f32x16 a;
+    zero(a);
+    {
+      Rows of;
+      T::rows(of, base(p.o, b, h), p.o.t, qq, len, lane, p.d);
+      T::dot(a, of, w.d);
+      if constexpr (T::REST) {
+        T::rows(of, (const E*)p.rest + ((long)b * p.s * p.heads + h) * p.d, (long)p.heads * p.d, qq, len, lane, p.d);
+        T::dot(a, of, w.d);
+      }
+    }
+    // the diagonal: row lane % 32 of column lane % 32, held by one half of the wave
+    const int want = (lane & 31) - 4 * (lane >> 5);
+    float D = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (row_of(r) == want) D = a[r];
+    D = ((lane >> 2) & 1) == (lane >> 5) ? D : 0.f;
+    w.D = D + __shfl_xor(D, 32, 64);
+    if (write && lane < 32 && qq < p.spad) p.drow[row] = qq < len ? w.D : 0.f;
+    w.m = qq < p.s ? p.m[row] : 0.f;
+    w.l = qq < p.s ? p.l[row] : 0.f;
+  }
+
+  // Sums of dS by distance: this half-wave's table of near ones, far ones on either side.
+  struct Sums {
+    float* near;
+    float left, right;
+  };
+  // Zeroed tables for every half-wave, behind the bias.
+  static __device__ __forceinline__ Sums start_sums(const AttnOpArgs& p, float* table, int wave, int lane) {
+    float* const all = table + table_len(p);
+    for (int e = threadIdx.x; e < 8 * table_len(p); e += 256) all[e] = 0.f;
+    return {all + (2 * wave + (lane >> 5)) * table_len(p), 0.f, 0.f};
+  }
+  // Eight tables into one, in order, then the sums of each bucket.  After a barrier.
+  static __device__ __forceinline__ void finish_sums(const AttnOpArgs& p, Sums& s, float* table, int wave, int lane,
+                                                     float* to) {
+    const int n = table_len(p), off = table_off(p);
+    float* const all = table + n;
+    float* const fars = table;  // the bias is no longer needed
+    const float fl = wave_sum(s.left), fr = wave_sum(s.right);
+    if (lane == 0) fars[wave] = fl, fars[4 + wave] = fr;
+    for (int e = threadIdx.x; e < n; e += 256) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t += all[i * n + e];
+      all[e] = t;
+    }
+    __syncthreads();
+    const int side = p.causal ? p.buckets : p.buckets / 2;
+    for (int c = wave; c < p.buckets; c += 4) {
+      const bool ahead = c >= side;
+      const int cs = ahead ? c - side : c;
+      // its distances [n0, n1); distance 0 counts once
+      const int n0 = max((int)p.first[cs], ahead ? 1 : 0);
+      const int n1 = cs == side - 1 ? off : p.first[cs + 1];
+      float t = 0.f;
+      for (int e = n0 + lane; e < n1; e += 64) t += all[ahead ? off + e : off - e];
+      t = wave_sum(t);
+      if (cs == side - 1) {
+        const float* f = fars + (ahead ? 4 : 0);
+        t += f[0] + f[1] + f[2] + f[3];
+      }
+      if (lane == 0) to[c] = t;
+    }
+  }
+
+  // acc += dS times the 32 keys from k (rows j of the tiles).
+  static __device__ __forceinline__ void dq_block(f32x16 (&acc)[NB], const Queries& w, const char* kt, const char* vt,
+                                                  int j, const Offs& of, int k, int q0, int qq, int lane, int len,
+                                                  const float* table, Sums& sums, const AttnOpArgs& p) {
+    if (none_visible<32>(p, q0, k, len)) return;
+    f32x16 sc, dp;
+    zero(sc);
+    zero(dp);
+    T::score2(sc, kt, j, w.q, dp, vt, j, w.d, of, lane);
+    const int rel = k - q0;
+    const bool near = BIAS && wave_uniform(rel + 31 > -p.far && rel - 31 < p.far);
+    const int e = k + 4 * (lane >> 5) - qq + (BIAS ? table_off(p) : 0);
+    if constexpr (BIAS) {
+      float c = 0.f;
+      if (!near) c = rel < 0 ? table[0] : table[table_len(p) - 1];
+      add_bias<1>(sc, table, e, c, near, p);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], w.m, w.l, p);
+    if (wave_uniform(!all_visible<32, 32>(p, q0, k, len))) mask_keys(sc, k, qq, lane, 0.f, len, p);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - w.D);
+    if constexpr (BIAS) {
+      if (near) {
+        add_diagonals(sums.near + e, dp);
+      } else {
+        float t = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t += dp[r];
+        if (rel < 0)
+          sums.left += t;
+        else
+          sums.right += t;
+      }
+    }
+    T::outer(acc, kt, j, dp, of, lane);
   }
 
   static __device__ __forceinline__ void dq(const AttnOpArgs& p, char* lds) {
@@ -505,7 +825,7 @@ struct AttnOp {
     const int b = z / p.heads, h = z % p.heads;
     const int len = length(p, b);
     const int q0 = qb * 128 + 32 * wave, qq = q0 + (lane & 31);
-    const Steps steps = key_steps(p, qb * 128, qb * 128 + 127, len);
+    const Steps steps = key_steps<64>(p, qb * 128, qb * 128 + 127, len);
     Src ks, vs;
     ks.set(base(p.k, b, h / p.group), p.k.t, len);
     vs.set(base(p.v, b, h / p.group), p.v.t, len);
@@ -515,40 +835,12 @@ struct AttnOp {
       T::copy(t + TILE, vs, wave, lane, k0, len, p.d);
     };
     if (T::ASYNC && steps.n > 0) issue(lds, 0);
-    Rows qf, df;
-    T::rows(qf, base(p.q, b, h), p.q.t, qq, len, lane, p.d);
-    T::rows(df, base(p.dout, b, h), p.dout.t, qq, len, lane, p.d);
-    float D = 0.f;
-    {
-      f32x16 a;
-      zero(a);
-      Rows of;
-      T::rows(of, base(p.o, b, h), p.o.t, qq, len, lane, p.d);
-      T::dot(a, of, df);
-      if constexpr (T::REST) {
-        T::rows(of, (const E*)p.rest + ((long)b * p.s * p.heads + h) * p.d, (long)p.heads * p.d, qq, len, lane, p.d);
-        T::dot(a, of, df);
-      }
-      // the diagonal: row lane % 32 of column lane % 32, held by one half of the wave
-      const int want = (lane & 31) - 4 * (lane >> 5);
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (row_of(r) == want) D = a[r];
-      const bool mine = ((lane >> 2) & 1) == (lane >> 5);
-      D = mine ? D : 0.f;
-      D += __shfl_xor(D, 32, 64);
-    }
-    if (lane < 32 && qq < p.spad) p.drow[(long)z * p.spad + qq] = qq < len ? D : 0.f;
-    const float m = qq < p.s ? p.m[(long)z * p.spad + qq] : 0.f;
-    const float l = qq < p.s ? p.l[(long)z * p.spad + qq] : 0.f;
-    // this half-wave's sums by distance, and those of far blocks on either side
-    float* sums = nullptr;
-    float far_l = 0.f, far_r = 0.f;
+    Queries w;
+    load_queries(w, p, b, h, qq, len, lane, true);
+    Sums sums = {nullptr, 0.f, 0.f};
     if constexpr (BIAS) {
       fill_table(p, h, table);
-      float* const all = table + table_len(p);
-      for (int e = threadIdx.x; e < 8 * table_len(p); e += 256) all[e] = 0.f;
-      sums = all + (2 * wave + (lane >> 5)) * table_len(p);
+      sums = start_sums(p, table, wave, lane);
     }
     Offs of;
     of.init(lane);
@@ -558,107 +850,128 @@ struct AttnOp {
     pipeline(steps.n, lds, STAGE, issue, [&](char* cur, int it) {
       const int k0 = steps.tile(it) * 64;
 #pragma unroll 1
-      for (int j = 0; j < 2; ++j) {
-        const int k = k0 + 32 * j;
-        if (none_visible<32>(p, q0, k, len)) continue;
-        f32x16 sc, dp;
-        zero(sc);
-        zero(dp);
-        T::score2(sc, cur, j, qf, dp, cur + TILE, j, df, of, lane);
-        const int rel = k - q0;
-        const bool near = BIAS && wave_uniform(rel + 31 > -p.far && rel - 31 < p.far);
-        const int e = k + 4 * (lane >> 5) - qq + (BIAS ? table_off(p) : 0);
-        if constexpr (BIAS) {
-          float c = 0.f;
-          if (!near) c = rel < 0 ? table[0] : table[table_len(p) - 1];
-          add_bias<1>(sc, table, e, c, near, p);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], m, l, p);
-        if (wave_uniform(!all_visible<32, 32>(p, q0, k, len))) mask_keys(sc, k, qq, lane, 0.f, len, p);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - D);
-        if constexpr (BIAS) {
-          if (near) {
-            add_diagonals(sums + e, dp);
-          } else {
-            float t = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) t += dp[r];
-            if (rel < 0)
-              far_l += t;
-            else
-              far_r += t;
-          }
-        }
-        T::outer(acc, cur, j, dp, of, lane);
-      }
+      for (int j = 0; j < 2; ++j)
+        dq_block(acc, w, cur, cur + TILE, j, of, k0 + 32 * j, q0, qq, lane, len, table, sums, p);
     });
     if (qq >= len) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) zero(acc[i]);
     }
     T::store(acc, lds + wave * (STAGE / 4), out(p.dq, b, h), p.dq.t, q0, p.s, lane, p.scale, p.d);
-    if constexpr (BIAS) {
-      // eight tables into one, in order, then the sums of each bucket
-      const int n = table_len(p), off = table_off(p);
-      float* const all = table + n;
-      float* const fars = table;  // the bias is no longer needed
-      far_l = wave_sum(far_l);
-      far_r = wave_sum(far_r);
-      if (lane == 0) fars[wave] = far_l, fars[4 + wave] = far_r;
-      for (int e = threadIdx.x; e < n; e += 256) {
-        float t = 0.f;
+    if constexpr (BIAS) finish_sums(p, sums, table, wave, lane, p.bpart + ((long)z * nqb + qb) * p.buckets);
+  }
+
+  // 32 queries a workgroup, as fwd32.
+  static __device__ __forceinline__ void dq32(const AttnOpArgs& p, char* lds) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* const own = lds + wave * OWN;
+    float* const table = (float*)(lds + 4 * OWN);
+    const int bh = p.batch * p.heads, nqb = (p.s + 31) / 32;
+    const int z = blockIdx.x % bh, qb = nqb - 1 - blockIdx.x / bh, q0 = 32 * qb, qq = q0 + (lane & 31);
+    const int b = z / p.heads, h = z % p.heads;
+    const int len = length(p, b);
+    const Steps steps = key_steps<32>(p, q0, q0 + 31, len);
+    Src ks, vs;
+    ks.set(base(p.k, b, h / p.group), p.k.t, len);
+    vs.set(base(p.v, b, h / p.group), p.v.t, len);
+    auto issue = [&](int it) {
+      const int k0 = steps.tile(it) * 32;
+      T::copy_own(own, ks, lane, k0, len, p.d);
+      T::copy_own(own + TILE / 2, vs, lane, k0, len, p.d);
+    };
+    if (wave < steps.n) issue(wave);
+    Queries w;
+    load_queries(w, p, b, h, qq, len, lane, wave == 0);
+    Sums sums = {nullptr, 0.f, 0.f};
+    Offs of;
+    of.init(lane);
+    f32x16 acc[NB];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t += all[i * n + e];
-        all[e] = t;
-      }
+    for (int i = 0; i < NB; ++i) zero(acc[i]);
+    if constexpr (BIAS) {
+      fill_table(p, h, table);
+      sums = start_sums(p, table, wave, lane);
       __syncthreads();
-      const int side = p.causal ? p.buckets : p.buckets / 2;
-      float* const to = p.bpart + ((long)z * nqb + qb) * p.buckets;
-      for (int c = wave; c < p.buckets; c += 4) {
-        const bool ahead = c >= side;
-        const int cs = ahead ? c - side : c;
-        // its distances [n0, n1); distance 0 counts once
-        const int n0 = max((int)p.first[cs], ahead ? 1 : 0);
-        const int n1 = cs == side - 1 ? off : p.first[cs + 1];
-        float t = 0.f;
-        for (int e = n0 + lane; e < n1; e += 64) t += all[ahead ? off + e : off - e];
-        t = wave_sum(t);
-        if (cs == side - 1) {
-          const float* f = fars + (ahead ? 4 : 0);
-          t += f[0] + f[1] + f[2] + f[3];
-        }
-        if (lane == 0) to[c] = t;
-      }
     }
+    for (int it = wave; it < steps.n; it += 4) {
+      T::own_landed();
+      dq_block(acc, w, own, own + TILE / 2, 0, of, steps.tile(it) * 32, q0, qq, lane, len, table, sums, p);
+      T::own_read();
+      if (it + 4 < steps.n) issue(it + 4);
+    }
+    put<NB>(acc, own, lane);
+    __syncthreads();
+    E* const to = out(p.dq, b, h);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      if (i % 4 != wave) continue;
+      zero(acc[i]);
+      if (qq < len) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) add_scaled(acc[i], lds + u * OWN, i, lane, 1.0f);
+      }
+      T::store_cols(acc[i], to, p.dq.t, q0, p.s, i, lane, p.scale, p.d);
+    }
+    if constexpr (BIAS) finish_sums(p, sums, table, wave, lane, p.bpart + ((long)z * nqb + qb) * p.buckets);
   }
 
   // -- dk and dv -------------------------------------------------------------------
+  // dk, dv += the 32 queries from q (rows j of the tiles), with their statistics.
+  template <int MODE>
+  static __device__ __forceinline__ void dkv_block(f32x16 (&dk)[NB], f32x16 (&dv)[NB], const Rows& kf, const Rows& vf,
+                                                   const char* qt, const char* dt, int j, const float* m, const float* l,
+                                                   const float* D, const Offs& of, int q, int k0, int kk, int lane,
+                                                   int len, const float* table, const AttnOpArgs& p) {
+    if (none_of<MODE>(p, q, k0, len)) return;
+    f32x16 sc, dp;
+    zero(sc);
+    zero(dp);
+    T::score2(sc, qt, j, kf, dp, dt, j, vf, of, lane);
+    if constexpr (BIAS) {
+      const int rel = k0 - q;
+      const bool near = wave_uniform(rel + 31 > -p.far && rel - 31 < p.far);
+      float c = 0.f;
+      if (!near) c = rel < 0 ? table[0] : table[table_len(p) - 1];
+      add_bias<-1>(sc, table, kk - q - 4 * (lane >> 5) + table_off(p), c, near, p);
+    }
+    const int at = 4 * (lane >> 5);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], m[at + row_of(r)], l[at + row_of(r)], p);
+    if (wave_uniform(!all_of<MODE>(p, q, k0, len))) mask_queries<MODE>(sc, q, kk, lane, len, p);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - D[at + row_of(r)]);
+    T::outer(dv, dt, j, sc, of, lane);
+    T::outer(dk, qt, j, dp, of, lane);
+  }
+
+  // This wave's rows k0.. of dk or dv as share `n` of the sinks' rows.
+  static __device__ __forceinline__ float* share(const AttnOpArgs& p, int z, int n, int which, int k0) {
+    return p.spart + ((((long)z * (1 + p.chunks) + n) * 2 + which) * p.sink_rows + k0) * HD;
+  }
+  static __device__ __forceinline__ void store_share(const f32x16& a, float* to, int i, int lane) {
+    to += (lane & 31) * HD + 32 * i + 4 * (lane >> 5);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *(float4*)(to + 8 * c) = make_float4(a[4 * c], a[4 * c + 1], a[4 * c + 2], a[4 * c + 3]);
+  }
+
   // A stage: a Q tile, a dO tile and the row vectors m, l, D of 64 queries.
   static constexpr int KSTAGE = 2 * TILE + 3072;
 
   static __device__ __forceinline__ void dkv(const AttnOpArgs& p, char* lds) {
+    const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
+    const int nkb = (p.s + 127) / 128;
+    if (kb >= nkb) return dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
     float* const table = (float*)(lds + STAGES * KSTAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, u = blockIdx.x / bk;
     const int b = z / p.kv_heads, hk = z % p.kv_heads;
     const int len = length(p, b);
-    const int units = p.sink_blocks * p.chunks;
-    const int kb = u < units ? u / p.chunks : u - units + p.sink_blocks;
     const int K0 = kb * 128, k0 = K0 + 32 * wave, kk = k0 + (lane & 31);
-    // the queries of this workgroup
-    int qlo, qhi;
-    if (u < units) {
-      const int c = u % p.chunks;
-      qlo = max(p.causal ? K0 : 0, c * p.chunk_len);
-      qhi = min(len, (c + 1) * p.chunk_len) - 1;
-    } else {
-      qlo = (int)max(0L, (long)K0 - p.right);
-      qhi = (int)min((long)len - 1, (long)K0 + 127 + p.left);
-    }
-    if (K0 >= len) qhi = -1;
+    // the queries whose windows hold these keys
+    const int qlo = (int)max(0L, (long)K0 - p.right);
+    const int qhi = K0 < len ? (int)min((long)len - 1, (long)K0 + 127 + p.left) : -1;
     const int t0 = qlo / 64, nt = qhi >= qlo ? qhi / 64 - t0 + 1 : 0;
     Src qs, ds;
     // step i: tile i % nt of head i / nt of the group; steps are issued and
@@ -696,39 +1009,11 @@ struct AttnOp {
           __syncthreads();
         }
       }
-      const int q64 = (t0 + tc) * 64;
       const float* vec = (const float*)(cur + 2 * TILE);
 #pragma unroll 1
-      for (int j = 0; j < 2; ++j) {
-        const int q = q64 + 32 * j;
-        if (none_visible<32>(p, q, k0, len)) continue;
-        f32x16 sc, dp;
-        zero(sc);
-        zero(dp);
-        T::score2(sc, cur, j, kf, dp, cur + TILE, j, vf, of, lane);
-        if constexpr (BIAS) {
-          const int rel = k0 - q;
-          const bool near = wave_uniform(rel + 31 > -p.far && rel - 31 < p.far);
-          float c = 0.f;
-          if (!near) c = rel < 0 ? table[0] : table[table_len(p) - 1];
-          add_bias<-1>(sc, table, kk - q - 4 * (lane >> 5) + table_off(p), c, near, p);
-        }
-        const float* row = vec + 32 * j + 4 * (lane >> 5);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], row[row_of(r)], row[256 + row_of(r)], p);
-        if (wave_uniform(!all_visible<32, 32>(p, q, k0, len))) {
-          int lo;
-          unsigned w;
-          query_range(lo, w, q, kk, lane, len, p);
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if ((unsigned)(row_of(r) - lo) > w) sc[r] = 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - row[512 + row_of(r)]);
-        T::outer(dv, cur + TILE, j, sc, of, lane);
-        T::outer(dk, cur, j, dp, of, lane);
-      }
+      for (int j = 0; j < 2; ++j)
+        dkv_block<WINDOW>(dk, dv, kf, vf, cur, cur + TILE, j, vec + 32 * j, vec + 256 + 32 * j, vec + 512 + 32 * j, of,
+                          (t0 + tc) * 64 + 32 * j, k0, kk, lane, len, table, p);
       if (++tc == nt) tc = 0, ++gc;
     });
     if (kk >= len) {
@@ -738,40 +1023,151 @@ struct AttnOp {
         zero(dv[i]);
       }
     }
-    if (u < units && p.chunks > 1) {
-      float* to = p.spart + (((long)z * units + u) * 2 * 128 + 32 * wave + (lane & 31)) * HD + 4 * (lane >> 5);
+    if (p.chunks && k0 < p.sink_rows) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          *(float4*)(to + 32 * i + 8 * c) =
-              make_float4(dk[i][4 * c], dk[i][4 * c + 1], dk[i][4 * c + 2], dk[i][4 * c + 3]);
-          *(float4*)(to + 128L * HD + 32 * i + 8 * c) =
-              make_float4(dv[i][4 * c], dv[i][4 * c + 1], dv[i][4 * c + 2], dv[i][4 * c + 3]);
-        }
+      for (int i = 0; i < NB; ++i) {
+        store_share(dk[i], share(p, z, 0, 0, k0), i, lane);
+        store_share(dv[i], share(p, z, 0, 1, k0), i, lane);
+      }
       return;
     }
     char* const area = lds + wave * (STAGE / 4);
     T::store(dk, area, out(p.dk, b, hk), p.dk.t, k0, p.s, lane, p.scale, p.d);
     T::store(dv, area, out(p.dv, b, hk), p.dv.t, k0, p.s, lane, 1.0f, p.d);
   }
+
+  // 32 keys a workgroup: its waves take every fourth block of 32 queries, of
+  // every head of the group, with tiles of their own.  MODE SINK: the sinks among
+  // the keys, for the queries of a chunk that see them as such.
+  static constexpr int KOWN = OWN + 3072;
+  template <int MODE>
+  static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* const own = lds + wave * KOWN;
+    float* const table = (float*)(lds + 4 * KOWN);
+    const int b = z / p.kv_heads, hk = z % p.kv_heads;
+    const int len = length(p, b);
+    const int kk = k0 + (lane & 31);
+    int qlo, qhi;
+    if (MODE == SINK) {
+      qlo = max(p.causal ? (int)min((long)p.s, (long)k0 + p.left + 1) : 0, chunk * p.chunk_len);
+      qhi = (int)min((long)len, (chunk + 1L) * p.chunk_len) - 1;
+    } else if (MODE == BOTH && k0 < p.sinks) {
+      qlo = p.causal ? k0 : 0;
+      qhi = len - 1;
+    } else {
+      qlo = (int)max(0L, (long)k0 - p.right);
+      qhi = (int)min((long)len - 1, (long)k0 + 31 + p.left);
+    }
+    if (k0 >= len) qhi = -1;
+    const int t0 = qlo / 32, nt = qhi >= qlo ? qhi / 32 - t0 + 1 : 0;
+    Rows kf, vf;
+    T::rows(kf, base(p.k, b, hk), p.k.t, kk, len, lane, p.d);
+    T::rows(vf, base(p.v, b, hk), p.v.t, kk, len, lane, p.d);
+    Offs of;
+    of.init(lane);
+    f32x16 dk[NB], dv[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      zero(dk[i]);
+      zero(dv[i]);
+    }
+    for (int g = 0; g < p.group; ++g) {
+      const int h = hk * p.group + g;
+      Src qs, ds;
+      qs.set(base(p.q, b, h), p.q.t, len);
+      ds.set(base(p.dout, b, h), p.dout.t, len);
+      const long rows = ((long)b * p.heads + h) * p.spad;
+      auto issue = [&](int it) {
+        const int row0 = (t0 + it) * 32;
+        T::copy_own(own, qs, lane, row0, len, p.d);
+        T::copy_own(own + TILE / 2, ds, lane, row0, len, p.d);
+        T::vec(own + OWN, p.m + rows + row0, lane, 32);
+        T::vec(own + OWN + 1024, p.l + rows + row0, lane, 32);
+        T::vec(own + OWN + 2048, p.drow + rows + row0, lane, 32);
+      };
+      if (wave < nt) issue(wave);
+      if constexpr (BIAS) {
+        __syncthreads();  // every wave is done with the last head's bias
+        fill_table(p, h, table);
+        __syncthreads();
+      }
+      const float* vec = (const float*)(own + OWN);
+      for (int it = wave; it < nt; it += 4) {
+        T::own_landed();
+        dkv_block<MODE>(dk, dv, kf, vf, own, own + TILE / 2, 0, vec, vec + 256, vec + 512, of, (t0 + it) * 32, k0, kk,
+                        lane, len, table, p);
+        T::own_read();
+        if (it + 4 < nt) issue(it + 4);
+      }
+    }
+    // one of the two sums after the other through LDS
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      __syncthreads();
+      if (which)
+        put<NB>(dv, own, lane);
+      else
+        put<NB>(dk, own, lane);
+      __syncthreads();
+      const AttnOpView& view = which ? p.dv : p.dk;
+      const int n = MODE == SINK ? 1 + chunk : 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        if (i % 4 != wave) continue;
+        f32x16 a;
+        zero(a);
+        if (kk < len) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) add_scaled(a, lds + u * KOWN, i, lane, 1.0f);
+        }
+        if (p.chunks && k0 < p.sink_rows)
+          store_share(a, share(p, z, n, which, k0), i, lane);
+        else
+          T::store_cols(a, out(view, b, hk), view.t, k0, p.s, i, lane, which ? 1.0f : p.scale, p.d);
+      }
+    }
+  }
+  static __device__ __forceinline__ void dkv_split(const AttnOpArgs& p, char* lds) {
+    const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
+    const int nkb = (p.s + 31) / 32;
+    if (kb >= nkb)
+      dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
+    else if (p.chunks)
+      dkv32<WINDOW>(p, lds, z, kb * 32, 0);
+    else
+      dkv32<BOTH>(p, lds, z, kb * 32, 0);
+  }
+
+  // LDS of the kernels.
+  static size_t table_bytes(const AttnOpArgs& a) { return BIAS ? 4 * (2 * (size_t)a.far + 384) : 0; }
+  static size_t fwd_lds(const AttnOpArgs& a, bool split) {
+    return (split ? 4 * OWN + 2048 : STAGES * STAGE) + table_bytes(a);
+  }
+  static size_t dq_lds(const AttnOpArgs& a, bool split) { return (split ? 4 * OWN : STAGES * STAGE) + 9 * table_bytes(a); }
+  static size_t dkv_lds(const AttnOpArgs& a, bool split) {
+    const size_t both = 4 * KOWN, whole = STAGES * KSTAGE;
+    return (split ? both : a.chunks && both > whole ? both : whole) + table_bytes(a);
+  }
 };
 
-// Key blocks with sinks: dk and dv from their chunks' shares, in order.  One
-// workgroup per sequence, key head and 8 keys; a thread sums 4 columns.
+// The sinks' rows of dk and dv from their shares, in order.  One workgroup per
+// sequence, key head and 8 keys; a thread sums 4 columns.
 template <class T>
 __global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
   constexpr int HD = T::HD, C4 = HD / 4;
+  using E = typename T::E;
   const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, r8 = blockIdx.x / bk;
   const int b = z / p.kv_heads, h = z % p.kv_heads;
   for (int i = threadIdx.x; i < 8 * 2 * C4; i += 256) {
     const int c = 4 * (i % C4), which = i / C4 % 2, row = 8 * r8 + i / (2 * C4);
-    const int kb = row / 128;
     if (row >= p.s || c >= p.d) continue;
-    const float* src = p.spart + ((((long)z * p.sink_blocks + kb) * p.chunks * 2 + which) * 128 + row % 128) * HD + c;
+    const float* src = p.spart + (((long)z * (1 + p.chunks) * 2 + which) * p.sink_rows + row) * HD + c;
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int n = 0; n < p.chunks; ++n) {
-      const float4 v = *(const float4*)(src + (long)n * 2 * 128 * HD);
+#pragma unroll 8
+    for (int n = 0; n <= p.chunks; ++n) {
+      const float4 v = *(const float4*)(src + (long)n * 2 * p.sink_rows * HD);
       t.x += v.x;
       t.y += v.y;
       t.z += v.z;
@@ -779,9 +1175,8 @@ __global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
     }
     const float mul = which ? 1.0f : p.scale;
     const AttnOpView& v = which ? p.dv : p.dk;
-    typename T::E* o = (typename T::E*)v.p + (long)b * v.b + (long)row * v.t + (long)h * v.h + c;
-    typename T::E w[4] = {(typename T::E)(t.x * mul), (typename T::E)(t.y * mul), (typename T::E)(t.z * mul),
-                          (typename T::E)(t.w * mul)};
+    E* o = (E*)v.p + (long)b * v.b + (long)row * v.t + (long)h * v.h + c;
+    const E w[4] = {(E)(t.x * mul), (E)(t.y * mul), (E)(t.z * mul), (E)(t.w * mul)};
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = w[e];
   }
@@ -795,46 +1190,79 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T
   AttnOp<T, BIAS>::fwd(p, attn_op_lds);
 }
 template <class T, bool BIAS>
+__global__ __launch_bounds__(256) void attn_op_fwd32_k(AttnOpArgs p) {
+  AttnOp<T, BIAS>::fwd32(p, attn_op_lds);
+}
+template <class T, bool BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_dq_k(
     AttnOpArgs p) {
   AttnOp<T, BIAS>::dq(p, attn_op_lds);
 }
 template <class T, bool BIAS>
-__global__ __launch_bounds__(256) void attn_op_dkv_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) void attn_op_dq32_k(AttnOpArgs p) {
+  AttnOp<T, BIAS>::dq32(p, attn_op_lds);
+}
+template <class T, bool BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::KWAVES, T::KWAVES))) void attn_op_dkv_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::dkv(p, attn_op_lds);
 }
+template <class T, bool BIAS>
+__global__ __launch_bounds__(256) void attn_op_dkv32_k(AttnOpArgs p) {
+  AttnOp<T, BIAS>::dkv_split(p, attn_op_lds);
+}
 
-template <class T>
+constexpr size_t kLds = 160 * 1024;  // of a compute unit
+constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 384);
+
+template <class T, bool BIAS>
 hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
-  using K = AttnOp<T, false>;
-  const dim3 grid((unsigned)((a.s + 127) / 128 * (long)a.batch * a.heads));
-  const size_t table = a.bias ? 4 * (2 * (size_t)a.far + 384) : 0;
-  if (a.bias)
-    hipLaunchKernelGGL((attn_op_fwd_k<T, true>), grid, dim3(256), K::STAGES * K::STAGE + table, st, a);
+  using K = AttnOp<T, BIAS>;
+  static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 9 * kTableMost <= kLds &&
+                    4 * K::KOWN + kTableMost <= kLds && K::STAGES * K::KSTAGE + kTableMost <= kLds,
+                "LDS at the largest table");
+  const bool split = a.split_q;
+  const long rows = split ? 32 : 128;
+  const dim3 grid((unsigned)((a.s + rows - 1) / rows * a.batch * a.heads));
+  if (split)
+    hipLaunchKernelGGL((attn_op_fwd32_k<T, BIAS>), grid, dim3(256), K::fwd_lds(a, true), st, a);
   else
-    hipLaunchKernelGGL((attn_op_fwd_k<T, false>), grid, dim3(256), K::STAGES * K::STAGE, st, a);
+    hipLaunchKernelGGL((attn_op_fwd_k<T, BIAS>), grid, dim3(256), K::fwd_lds(a, false), st, a);
   return hipGetLastError();
 }
 
-template <class T>
-hipError_t attn_op_bwd_launch(const AttnOpArgs& a, hipStream_t st) {
-  using K = AttnOp<T, false>;
-  const long nb = (a.s + 127) / 128;
-  const size_t table = a.bias ? 4 * (2 * (size_t)a.far + 384) : 0;
-  const dim3 gq((unsigned)(nb * a.batch * a.heads));
-  const dim3 gk((unsigned)((nb + (long)a.sink_blocks * (a.chunks - 1)) * a.batch * a.kv_heads));
-  if (a.bias) {
-    hipLaunchKernelGGL((attn_op_dq_k<T, true>), gq, dim3(256), K::STAGES * K::STAGE + 9 * table, st, a);
-    hipLaunchKernelGGL((attn_op_dkv_k<T, true>), gk, dim3(256), K::STAGES * K::KSTAGE + table, st, a);
-  } else {
-    hipLaunchKernelGGL((attn_op_dq_k<T, false>), gq, dim3(256), K::STAGES * K::STAGE, st, a);
-    hipLaunchKernelGGL((attn_op_dkv_k<T, false>), gk, dim3(256), K::STAGES * K::KSTAGE, st, a);
-  }
-  if (a.sink_blocks && a.chunks > 1) {
-    const long rows = a.sink_blocks * 128L < a.s ? a.sink_blocks * 128L : a.s;
-    hipLaunchKernelGGL((attn_op_sinks_k<T>), dim3((unsigned)((rows + 7) / 8 * a.batch * a.kv_heads)), dim3(256), 0, st, a);
-  }
+template <class T, bool BIAS>
+hipError_t attn_op_bwd_launch(const AttnOpArgs& a, hipStream_t st, int* bias_blocks) {
+  using K = AttnOp<T, BIAS>;
+  // (the one form that does not always fit: eight tables of a far bias next to the tiles of fp32 heads of 128)
+  const bool sq = a.split_q && K::dq_lds(a, true) <= kLds, sk = a.split_k;
+  const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
+  const dim3 gq((unsigned)(nq * a.batch * a.heads));
+  const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads));
+  *bias_blocks = (int)nq;
+  if (sq)
+    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, true), st, a);
+  else
+    hipLaunchKernelGGL((attn_op_dq_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, false), st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (sk)
+    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, true), st, a);
+  else
+    hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, false), st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.chunks) return e;
+  const long rows = a.sink_rows < a.s ? a.sink_rows : a.s;
+  hipLaunchKernelGGL((attn_op_sinks_k<T>), dim3((unsigned)((rows + 7) / 8 * a.batch * a.kv_heads)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+#define ATTN_OP_DEFINE(NAME, T)                                                                    \
+  hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st) {                             \
+    return a.bias ? attn_op_fwd_launch<T, true>(a, st) : attn_op_fwd_launch<T, false>(a, st);      \
+  }                                                                                                \
+  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st, int* bias_blocks) {           \
+    return a.bias ? attn_op_bwd_launch<T, true>(a, st, bias_blocks)                                \
+                  : attn_op_bwd_launch<T, false>(a, st, bias_blocks);                              \
+  }

@@ -50,7 +50,7 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   a.buckets = c.buckets;
   a.bias_f32 = c.bias_dtype == RC_FP32;
   attn_op_plan(a, c.window, c.max_distance);
-  const long units = ((long)a.s + 127) / 128 + (long)a.sink_blocks * a.chunks;
+  const long units = ((long)a.s + 127) / 128 + (long)a.sink_rows / 32 * a.chunks;
   if (units * a.batch > 0x7fffffffL / a.heads)
     return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks of 128 tokens");
   return RC_OK;

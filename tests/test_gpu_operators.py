@@ -80,6 +80,26 @@ CASES = [
 ]
 
 
+# The same on grids of more than 256 blocks of 32 tokens, which take 128 tokens a workgroup.
+CASES += [
+    (300, 1, 1, 1, 64, True, 0, 0, 0, 0, None),
+    (5, 300, 12, 12, 128, True, 70, 4, 0, 0, None),
+    (2, 700, 12, 12, 64, True, 40, 130, 0, 0, None),
+    (1, 1100, 12, 2, 128, True, 65, 4, 0, 0, None),
+    (1, 1300, 9, 9, 40, False, 31, 200, 0, 0, None),
+    (6, 260, 8, 8, 96, False, 33, 5, 0, 0, (260, 0, 129, 128, 1, 200)),
+    (2, 257, 18, 6, 80, True, 100, 70, 0, 0, None),
+    (4, 300, 9, 9, 64, True, 0, 0, 32, 128, (300, 299, 17, 0)),
+    (2, 333, 16, 8, 128, False, 0, 0, 32, 128, None),
+    (1, 600, 20, 10, 32, False, 0, 0, 128, 1024, None),
+    (1, 1400, 8, 2, 128, True, 90, 33, 128, 1024, None),
+    (3, 280, 14, 2, 128, False, 70, 6, 32, 100, (280, 31, 0)),
+    (1, 2100, 6, 6, 64, True, 50, 10, 64, 512, (1777,)),
+    (1, 2200, 1, 1, 16, True, 50, 10, 0, 0, None),   # a small grid, but a long sequence: the sinks' own workgroups
+    (1, 2200, 2, 1, 128, False, 50, 40, 8, 20, None),
+]
+
+
 @pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:10]))
 def test_attention(case, kind):

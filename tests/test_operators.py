@@ -42,13 +42,14 @@ def test_attention_memory_holds_every_part(bf16, batch, seq, heads, kv, d):
     # two statistics a row, rows padded to blocks of 64, and what o's rounding drops
     assert saved >= 2 * 4 * rows + (2 * batch * seq * heads * d if bf16 else 0)
     assert work >= 4 * rows
-    # with a bias: a sum per bucket of each block of 128 queries
+    # with a bias: a sum per bucket of each block of 32 queries
+    blocks = -(-seq // 32)
     assert memory(**size, buckets=32, max_distance=128)[2] >= up(4 * rows) + 4 * batch * heads * blocks * 32
-    # with sinks in a window: shares of 128 rows of dk and dv from each chunk of queries
+    # with sinks in a window: shares of 32 rows of dk and dv, of the window and each chunk of queries
     if seq > 512:
         chunks = -(-seq // 512)
         got = memory(**size, window=40, sinks=4, buckets=32, max_distance=128)[2]
-        assert got >= up(4 * rows) + 4 * batch * heads * blocks * 32 + 4 * batch * kv * chunks * 2 * 128 * d
+        assert got >= up(4 * rows) + 4 * batch * heads * blocks * 32 + 4 * batch * kv * (1 + chunks) * 2 * 32 * d
 
 
 BAD_ATTENTION = [
