@@ -21,9 +21,8 @@
 // Bias: the distances of less than `far` tokens have a table in LDS (the
 // bias of distance e - off at entry e); a block whose distances are all at
 // least that takes one value.  Its gradient: each wave adds the dS of a near
-// block to a table of its own by distance (the halves of a wave to one
-// table each: no two lanes of an instruction meet, every sum has a fixed
-// order); far blocks add up in registers.  The tables are summed by buckets
+// block to a table of its own by distance (no two lanes of an instruction meet:
+// every sum has a fixed order); far blocks add up in registers.  The tables are summed by buckets
 // when the workgroup ends, and over workgroups by a kernel of its own.
 //
 // D is formed by the same chain of matrix instructions as do.v: where a row
@@ -48,7 +47,7 @@ struct TileB16 {
   static constexpr int HD = HD_, TILE = A::TILE64;
   static constexpr bool ASYNC = true, REST = true;
   // waves a SIMD of the kernels over queries and keys
-  static constexpr int WAVES = 2, KWAVES = HD > 64 ? 1 : 2;
+  static constexpr int WAVES = 2, KWAVES = HD > 96 ? 1 : 2;
   using Rows = bf16x8[HD / 16];
   struct Offs {
     typename A::RowOffs ro;
@@ -258,10 +257,13 @@ struct AttnOp {
   }
 
   // -- bias table --------------------------------------------------------------
-  // Entry e holds the bias (base 2) of distance j - i = e - off.  A near block
-  // of 64 by 128 tokens reaches at most 190 tokens beyond `far`.
-  static __device__ __forceinline__ int table_off(const AttnOpArgs& p) { return p.far + 192; }
-  static __device__ __forceinline__ int table_len(const AttnOpArgs& p) { return 2 * p.far + 384; }
+  // Entry e holds the bias (base 2) of distance j - i = e - off.  A near block of
+  // 32 queries and 64 keys reaches at most 94 tokens beyond `far` (and 67 beyond
+  // a causal query, where the sums by distance count in).
+  static __host__ __device__ __forceinline__ int table_off(const AttnOpArgs& p) { return p.far + 96; }
+  static __host__ __device__ __forceinline__ int table_len(const AttnOpArgs& p) {
+    return p.far + 96 + (p.causal ? 96 : p.far + 96);
+  }
   static __device__ __forceinline__ int bucket_of(const AttnOpArgs& p, int rel) {
     const int side = p.causal ? p.buckets : p.buckets / 2;
     const int n = p.causal ? max(-rel, 0) : abs(rel);
@@ -284,7 +286,7 @@ struct AttnOp {
   // i - b holds at row 0, so each element is shifted by b lanes (an addition
   // with a DPP operand) into the sum of its distance: to[0], to[16] for what
   // leaves the row of lanes and for rows 16 and on, to[32] for both.  30
-  // additions and three LDS atomics for 16 elements (us, dq of 40 heads of 128, s
+  // additions and three LDS atomics a half for 16 elements (us, dq of 40 heads of 128, s
   // 4096, window 2048, 64 buckets: 469, against 821 with sixteen atomics).
   template <int R>
   static __device__ __forceinline__ void shift_in(float& stays, float& leaves, const f32x16& x) {
@@ -297,7 +299,7 @@ struct AttnOp {
       leaves += __int_as_float(__builtin_amdgcn_update_dpp(0, v, 0x110 + 16 - b, 0xf, 0xf, true));  // lane i + b - 16
     }
   }
-  static __device__ __forceinline__ void add_diagonals(float* to, const f32x16& x) {
+  static __device__ __forceinline__ void add_diagonals(float* to, const f32x16& x, int lane) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
     shift_in<0>(s0, s1, x);
     shift_in<1>(s0, s1, x);
@@ -315,9 +317,14 @@ struct AttnOp {
     shift_in<13>(s1, s2, x);
     shift_in<14>(s1, s2, x);
     shift_in<15>(s1, s2, x);
-    __hip_atomic_fetch_add(to, s0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    __hip_atomic_fetch_add(to + 16, s1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    __hip_atomic_fetch_add(to + 32, s2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    // one half of the wave after the other: no two lanes of an instruction meet
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      if ((lane >> 5) == half) {
+        __hip_atomic_fetch_add(to, s0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        __hip_atomic_fetch_add(to + 16, s1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        __hip_atomic_fetch_add(to + 32, s2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      }
   }
 
   // x = sc sl2 + bias of 32 keys from k (element r, this lane: key k + 4 hh + row_of(r))
@@ -432,13 +439,14 @@ struct AttnOp {
   template <class Issue, class Body>
   static __device__ __forceinline__ void pipeline(int n, char* lds, int stage, Issue issue, Body body) {
     stage_sync();
-    for (int it = 0; it < n; ++it) {
-      if constexpr (T::ASYNC) {
-        char* const cur = lds + (it & 1) * stage;
+    if constexpr (T::ASYNC) {
+      for (int it = 0; it < n; ++it) {
         if (it + 1 < n) issue(lds + (~it & 1) * stage, it + 1);
-        body(cur, it);
+        body(lds + (it & 1) * stage, it);
         stage_sync();
-      } else {
+      }
+    } else {
+      for (int it = 0; it < n; ++it) {
         issue(lds, it);
         stage_sync();
         body(lds, it);
@@ -695,15 +703,11 @@ struct AttnOp {
   }
 
   // -- dq, dbias and D -----------------------------------------------------------
-  // P of a score block in place; x: after add_bias with BIAS, raw products otherwise.
-  static __device__ __forceinline__ float prob(float x, float m, float l, const AttnOpArgs& p) {
-    return __builtin_amdgcn_exp2f((BIAS ? x - m : fmaf(x, p.sl2, -m)) - l);
-  }
-
-  // A wave's 32 queries: rows of q and dout, statistics and D.
+  // A wave's 32 queries: rows of q and dout, the reference score, and what turns
+  // do.v into dS / 2^(x - m) = do.v / sum - D / sum.
   struct Queries {
     Rows q, d;
-    float m, l, D;
+    float m, inv, D;
   };
   static __device__ __forceinline__ void load_queries(Queries& w, const AttnOpArgs& p, int b, int h, int qq, int len,
                                                       int lane, bool write) {
@@ -728,53 +732,54 @@ struct AttnOp {
     for (int r = 0; r < 16; ++r)
       if (row_of(r) == want) D = a[r];
     D = ((lane >> 2) & 1) == (lane >> 5) ? D : 0.f;
-    w.D = D + __shfl_xor(D, 32, 64);
-    if (write && lane < 32 && qq < p.spad) p.drow[row] = qq < len ? w.D : 0.f;
+    D += __shfl_xor(D, 32, 64);
+    if (write && lane < 32 && qq < p.spad) p.drow[row] = qq < len ? D : 0.f;
     w.m = qq < p.s ? p.m[row] : 0.f;
-    w.l = qq < p.s ? p.l[row] : 0.f;
+    w.inv = qq < p.s ? __builtin_amdgcn_exp2f(-p.l[row]) : 0.f;
+    w.D = D * w.inv;
   }
 
-  // Sums of dS by distance: this half-wave's table of near ones, far ones on either side.
+  // Sums of dS by distance: this wave's table of near ones, far ones on either side.
   struct Sums {
     float* near;
     float left, right;
   };
-  // Zeroed tables for every half-wave, behind the bias.
-  static __device__ __forceinline__ Sums start_sums(const AttnOpArgs& p, float* table, int wave, int lane) {
+  // A zeroed table for every wave, behind the bias.
+  static __device__ __forceinline__ Sums start_sums(const AttnOpArgs& p, float* table, int wave) {
     float* const all = table + table_len(p);
-    for (int e = threadIdx.x; e < 8 * table_len(p); e += 256) all[e] = 0.f;
-    return {all + (2 * wave + (lane >> 5)) * table_len(p), 0.f, 0.f};
+    for (int e = threadIdx.x; e < 4 * table_len(p); e += 256) all[e] = 0.f;
+    return {all + wave * table_len(p), 0.f, 0.f};
   }
-  // Eight tables into one, in order, then the sums of each bucket.  After a barrier.
+  // The sums of each bucket over the four tables, in order, by eight lanes each.  After a barrier.
   static __device__ __forceinline__ void finish_sums(const AttnOpArgs& p, Sums& s, float* table, int wave, int lane,
                                                      float* to) {
     const int n = table_len(p), off = table_off(p);
-    float* const all = table + n;
+    const float* const all = table + n;
     float* const fars = table;  // the bias is no longer needed
     const float fl = wave_sum(s.left), fr = wave_sum(s.right);
     if (lane == 0) fars[wave] = fl, fars[4 + wave] = fr;
-    for (int e = threadIdx.x; e < n; e += 256) {
-      float t = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t += all[i * n + e];
-      all[e] = t;
-    }
     __syncthreads();
-    const int side = p.causal ? p.buckets : p.buckets / 2;
-    for (int c = wave; c < p.buckets; c += 4) {
+    const int side = p.causal ? p.buckets : p.buckets / 2, part = threadIdx.x % 8;
+    for (int c0 = 0; c0 < p.buckets; c0 += 32) {
+      const int c = min(c0 + (int)threadIdx.x / 8, p.buckets - 1);
       const bool ahead = c >= side;
       const int cs = ahead ? c - side : c;
       // its distances [n0, n1); distance 0 counts once
       const int n0 = max((int)p.first[cs], ahead ? 1 : 0);
-      const int n1 = cs == side - 1 ? off : p.first[cs + 1];
+      const int n1 = cs == side - 1 ? (ahead ? n - off : off + 1) : p.first[cs + 1];
       float t = 0.f;
-      for (int e = n0 + lane; e < n1; e += 64) t += all[ahead ? off + e : off - e];
-      t = wave_sum(t);
+      for (int e = n0 + part; e < n1; e += 8) {
+        const float* x = all + (ahead ? off + e : off - e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t += x[i * n];
+      }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) t += __shfl_xor(t, o, 64);
       if (cs == side - 1) {
         const float* f = fars + (ahead ? 4 : 0);
         t += f[0] + f[1] + f[2] + f[3];
       }
-      if (lane == 0) to[c] = t;
+      if (part == 0 && c0 + (int)threadIdx.x / 8 < p.buckets) to[c] = t;
     }
   }
 
@@ -796,13 +801,13 @@ struct AttnOp {
       add_bias<1>(sc, table, e, c, near, p);
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], w.m, w.l, p);
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - w.m : fmaf(sc[r], p.sl2, -w.m));
     if (wave_uniform(!all_visible<32, 32>(p, q0, k, len))) mask_keys(sc, k, qq, lane, 0.f, len, p);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - w.D);
+    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * fmaf(dp[r], w.inv, -w.D);
     if constexpr (BIAS) {
       if (near) {
-        add_diagonals(sums.near + e, dp);
+        add_diagonals(sums.near + e, dp, lane);
       } else {
         float t = 0.f;
 #pragma unroll
@@ -840,7 +845,7 @@ struct AttnOp {
     Sums sums = {nullptr, 0.f, 0.f};
     if constexpr (BIAS) {
       fill_table(p, h, table);
-      sums = start_sums(p, table, wave, lane);
+      sums = start_sums(p, table, wave);
     }
     Offs of;
     of.init(lane);
@@ -891,7 +896,7 @@ struct AttnOp {
     for (int i = 0; i < NB; ++i) zero(acc[i]);
     if constexpr (BIAS) {
       fill_table(p, h, table);
-      sums = start_sums(p, table, wave, lane);
+      sums = start_sums(p, table, wave);
       __syncthreads();
     }
     for (int it = wave; it < steps.n; it += 4) {
@@ -917,6 +922,16 @@ struct AttnOp {
   }
 
   // -- dk and dv -------------------------------------------------------------------
+  static __device__ __forceinline__ void load_rows16(f32x16& row, const float* from) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float4 v = *(const float4*)__builtin_assume_aligned(from + 8 * c, 16);
+      row[4 * c] = v.x;
+      row[4 * c + 1] = v.y;
+      row[4 * c + 2] = v.z;
+      row[4 * c + 3] = v.w;
+    }
+  }
   // dk, dv += the 32 queries from q (rows j of the tiles), with their statistics.
   template <int MODE>
   static __device__ __forceinline__ void dkv_block(f32x16 (&dk)[NB], f32x16 (&dv)[NB], const Rows& kf, const Rows& vf,
@@ -936,11 +951,22 @@ struct AttnOp {
       add_bias<-1>(sc, table, kk - q - 4 * (lane >> 5) + table_off(p), c, near, p);
     }
     const int at = 4 * (lane >> 5);
+    f32x16 row;  // a statistic of the block's queries
+    load_rows16(row, m + at);
+    if constexpr (BIAS) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = prob(sc[r], m[at + row_of(r)], l[at + row_of(r)], p);
+      for (int r = 0; r < 16; ++r) sc[r] -= row[r];
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = fmaf(sc[r], p.sl2, -row[r]);
+    }
+    load_rows16(row, l + at);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(sc[r] - row[r]);
+    load_rows16(row, D + at);
     if (wave_uniform(!all_of<MODE>(p, q, k0, len))) mask_queries<MODE>(sc, q, kk, lane, len, p);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - D[at + row_of(r)]);
+    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - row[r]);
     T::outer(dv, dt, j, sc, of, lane);
     T::outer(dk, qt, j, dp, of, lane);
   }
@@ -1141,11 +1167,11 @@ struct AttnOp {
   }
 
   // LDS of the kernels.
-  static size_t table_bytes(const AttnOpArgs& a) { return BIAS ? 4 * (2 * (size_t)a.far + 384) : 0; }
+  static size_t table_bytes(const AttnOpArgs& a) { return BIAS ? 4 * (size_t)table_len(a) : 0; }
   static size_t fwd_lds(const AttnOpArgs& a, bool split) {
     return (split ? 4 * OWN + 2048 : STAGES * STAGE) + table_bytes(a);
   }
-  static size_t dq_lds(const AttnOpArgs& a, bool split) { return (split ? 4 * OWN : STAGES * STAGE) + 9 * table_bytes(a); }
+  static size_t dq_lds(const AttnOpArgs& a, bool split) { return (split ? 4 * OWN : STAGES * STAGE) + 5 * table_bytes(a); }
   static size_t dkv_lds(const AttnOpArgs& a, bool split) {
     const size_t both = 4 * KOWN, whole = STAGES * KSTAGE;
     return (split ? both : a.chunks && both > whole ? both : whole) + table_bytes(a);
@@ -1212,12 +1238,12 @@ __global__ __launch_bounds__(256) void attn_op_dkv32_k(AttnOpArgs p) {
 }
 
 constexpr size_t kLds = 160 * 1024;  // of a compute unit
-constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 384);
+constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 192);
 
 template <class T, bool BIAS>
 hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
   using K = AttnOp<T, BIAS>;
-  static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 9 * kTableMost <= kLds &&
+  static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 5 * kTableMost <= kLds &&
                     4 * K::KOWN + kTableMost <= kLds && K::STAGES * K::KSTAGE + kTableMost <= kLds,
                 "LDS at the largest table");
   const bool split = a.split_q;
@@ -1233,7 +1259,7 @@ hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
 template <class T, bool BIAS>
 hipError_t attn_op_bwd_launch(const AttnOpArgs& a, hipStream_t st, int* bias_blocks) {
   using K = AttnOp<T, BIAS>;
-  // (the one form that does not always fit: eight tables of a far bias next to the tiles of fp32 heads of 128)
+  // (the one form that does not always fit: five tables of a far bias next to the tiles of fp32 heads of 128)
   const bool sq = a.split_q && K::dq_lds(a, true) <= kLds, sk = a.split_k;
   const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
   const dim3 gq((unsigned)(nq * a.batch * a.heads));

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import math
 from typing import Optional, Sequence
 
@@ -24,33 +25,28 @@ def _torch():
 def _kind(t, name):
     """The library's dtype of a tensor."""
     torch = _torch()
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if t.dtype == torch.bfloat16:
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
         return L.RC_BF16
-    if t.dtype == torch.float32:
+    if dtype is torch.float32:
         return L.RC_FP32
-    raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+    raise ValueError(f"{name} must be bfloat16 or float32, not {dtype}")
 
 
-def _same(t, name, like, shape):
-    """Checks a tensor that goes with `like`; a view of it."""
-    if _kind(t, name) != _kind(like, "q") or t.device != like.device:
-        raise ValueError(f"{name} must have the type and device of q")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    return _view(t, name)
-
-
-def _view(t, name):
-    if t.dim() != 4:
-        raise ValueError(f"{name} must be [batch, tokens, heads, head_dim]")
+def _view(t, name, like, shape):
+    """A view of a tensor that goes with q (`like`)."""
+    if t is not like:
+        if _kind(t, name) != _kind(like, "q") or t.device != like.device:
+            raise ValueError(f"{name} must have the type and device of q")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     b, s, h, d = t.stride()
-    if d != 1 and t.shape[3] > 1:
+    if d != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the elements of a head must be contiguous")
     # the stride of a dimension of one element says nothing: any will do
-    b, s, h = (x if n > 1 else 0 for x, n in zip((b, s, h), t.shape))
-    return L.RcView(t.data_ptr(), b, s, h)
+    return L.RcView(t.data_ptr(), b if shape[0] > 1 else 0, s if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
 
 
 def _on(device):
@@ -61,20 +57,32 @@ def _on(device):
     return torch.cuda.device(device), torch.cuda.current_stream(device)
 
 
+@functools.lru_cache(maxsize=256)
+def _config(kind, batch, seq, heads, kv, d, causal, window, sinks, buckets, max_distance, bias_kind, scale):
+    """A checked configuration, with the bytes of its saved and work memory."""
+    c = L.RcAttention(kind, batch, seq, heads, kv, d, causal, window, sinks, buckets, max_distance, bias_kind,
+                      scale)
+    saved, work = ctypes.c_size_t(), ctypes.c_size_t()
+    L.check(L.load().rc_attention_memory(ctypes.byref(c), ctypes.byref(saved), ctypes.byref(work)))
+    return c, saved.value, work.value
+
+
 class _Call:
     """What a forward and a backward call have in common."""
+
+    __slots__ = ("shape", "kv_shape", "q", "k", "v", "bias", "lengths", "c", "saved_bytes", "work_bytes", "lib")
 
     def __init__(self, q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale):
         torch = _torch()
         kind = _kind(q, "q")
         if q.dim() != 4:
             raise ValueError("q must be [batch, tokens, heads, head_dim]")
-        batch, seq, heads, d = q.shape
+        self.shape = shape = q.shape
+        batch, seq, heads, d = shape
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k must be [batch, tokens, kv_heads, head_dim]")
         kv = k.shape[2]
-        self.shape, self.kv_shape = (batch, seq, heads, d), (batch, seq, kv, d)
-        self.q, self.k, self.v = _view(q, "q"), _same(k, "k", q, self.kv_shape), _same(v, "v", q, self.kv_shape)
+        self.kv_shape = (batch, seq, kv, d)
         self.bias = self.lengths = None
         buckets, bias_kind = 0, L.RC_FP32
         if rel_bias is not None:
@@ -84,21 +92,21 @@ class _Call:
             if not rel_bias.is_contiguous() or rel_bias.device != q.device:
                 raise ValueError("rel_bias must be contiguous and on the device of q")
             buckets = rel_bias.shape[1]
-            self.bias = ctypes.c_void_p(rel_bias.data_ptr())
+            self.bias = rel_bias.data_ptr()
         if lengths is not None:
             if not isinstance(lengths, torch.Tensor) or lengths.device != q.device:
                 raise TypeError("lengths must be a tensor on the device of q")
-            if lengths.dtype != torch.int32 or tuple(lengths.shape) != (batch,) or not lengths.is_contiguous():
+            if lengths.dtype != torch.int32 or lengths.shape != (batch,) or not lengths.is_contiguous():
                 raise ValueError(f"lengths must be a contiguous int32 tensor of {batch}")
-            self.lengths = ctypes.c_void_p(lengths.data_ptr())
+            self.lengths = lengths.data_ptr()
         if scale is None:
             scale = 1.0 / math.sqrt(d) if d else 0.0
-        self.c = L.RcAttention(kind, batch, seq, heads, kv, d, 1 if causal else 0, int(window), int(sinks),
-                               buckets, int(max_distance) if buckets else 0, bias_kind, scale)
+        self.c, self.saved_bytes, self.work_bytes = _config(
+            kind, batch, seq, heads, kv, d, 1 if causal else 0, int(window), int(sinks), buckets,
+            int(max_distance) if buckets else 0, bias_kind, float(scale))
+        self.q = _view(q, "q", q, shape)
+        self.k, self.v = _view(k, "k", q, self.kv_shape), _view(v, "v", q, self.kv_shape)
         self.lib = L.load()
-        saved, work = ctypes.c_size_t(), ctypes.c_size_t()
-        L.check(self.lib.rc_attention_memory(ctypes.byref(self.c), ctypes.byref(saved), ctypes.byref(work)))
-        self.saved_bytes, self.work_bytes = saved.value, work.value
 
 
 def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: int = 0, rel_bias=None,
@@ -119,12 +127,11 @@ def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: i
     ctx, stream = _on(q.device)
     with ctx:
         o = torch.empty(c.shape, dtype=q.dtype, device=q.device) if out is None else out
-        ov = _same(o, "out", q, c.shape)
+        ov = _view(o, "out", q, c.shape)
         saved = torch.empty(c.saved_bytes, dtype=torch.uint8, device=q.device) if save else None
         L.check(c.lib.rc_attention_forward(
             ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
-            ctypes.byref(ov), ctypes.c_void_p(saved.data_ptr() if save else None),
-            ctypes.c_void_p(stream.cuda_stream)))
+            ctypes.byref(ov), saved.data_ptr() if save else None, stream.cuda_stream))
     return o, saved
 
 
@@ -139,12 +146,12 @@ def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: 
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
     if not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device:
         raise ValueError("saved must be what attention_forward returned for these arguments")
-    ov, dov = _same(o, "o", q, c.shape), _same(dout, "dout", q, c.shape)
+    ov, dov = _view(o, "o", q, c.shape), _view(dout, "dout", q, c.shape)
     ctx, stream = _on(q.device)
     with ctx:
         def given(t, name, shape):
             t = torch.empty(shape, dtype=q.dtype, device=q.device) if t is None else t
-            return t, _same(t, name, q, shape)
+            return t, _view(t, name, q, shape)
 
         (dq, dqv), (dk, dkv), (dv, dvv) = given(dq, "dq", c.shape), given(dk, "dk", c.kv_shape), given(
             dv, "dv", c.kv_shape)
@@ -152,9 +159,9 @@ def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: 
         work = torch.empty(c.work_bytes, dtype=torch.uint8, device=q.device)
         L.check(c.lib.rc_attention_backward(
             ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
-            ctypes.byref(ov), ctypes.c_void_p(saved.data_ptr()), ctypes.byref(dov), ctypes.byref(dqv),
-            ctypes.byref(dkv), ctypes.byref(dvv), None if dbias is None else ctypes.c_void_p(dbias.data_ptr()),
-            ctypes.c_void_p(work.data_ptr()), ctypes.c_void_p(stream.cuda_stream)))
+            ctypes.byref(ov), saved.data_ptr(), ctypes.byref(dov), ctypes.byref(dqv), ctypes.byref(dkv),
+            ctypes.byref(dvv), None if dbias is None else dbias.data_ptr(), work.data_ptr(),
+            stream.cuda_stream))
     return dq, dk, dv, dbias
 
 
