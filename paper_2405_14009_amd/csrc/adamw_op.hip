@@ -6,7 +6,7 @@
 // The work is one pass over the streams (28 bytes an element with fp32
 // moments and gradients, 16 with 8-bit ones), so HBM bounds it.  The tensors'
 // descriptors travel as kernel arguments, up to MAX of them a launch, and
-// workgroups take chunks of CHUNK elements of any tensor: a set of many small
+// workgroups take chunks of elements of any tensor: a set of many small
 // tensors is one launch, and no table has to be copied to the device.
 //
 // 8-bit moments.  Blocks of 128 elements of a tensor share a power of two per
@@ -35,7 +35,11 @@ namespace {
 
 constexpr int NT = 256;
 constexpr int MAX = 48;       // tensors a launch: their descriptors fill 3.4 of the 4 KB of arguments
-constexpr int CHUNK = 4096;   // elements a workgroup takes
+// Elements that a workgroup takes: one turn of its threads, two where the
+// moments are only read (us at one / two turns: 8-bit step of 4.0e8 parameters
+// with bf16 gradients 1285 / 1395, fp32 step of 1.5e8 784 / 798, reading 8-bit
+// moments of 4.0e8 1230 / 890, whose two output streams alternate more coarsely).
+constexpr int CHUNK8 = 2048, CHUNK32 = 1024, CHUNK_READ = 4096;
 
 struct Tensor {
   float* p;
@@ -57,6 +61,15 @@ struct Args {
   int n;
   Tensor t[MAX];
 };
+
+// 8 bytes, streamed past the caches as the fp32 arrays are (adam.h).
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void load8_nt(void* to, const void* from) {
+  *(u32x2*)to = __builtin_nontemporal_load((const u32x2*)from);
+}
+__device__ __forceinline__ void store8_nt(void* to, const void* from) {
+  __builtin_nontemporal_store(*(const u32x2*)from, (u32x2*)to);
+}
 
 // N consecutive elements at i of a tensor, and their stores; scalar at its end
 // or where the pointers are not aligned.
@@ -94,7 +107,7 @@ __device__ __forceinline__ void load_grad(float (&x)[N], const Tensor& t, long i
   if (wide) {
     bf16 b[N];
 #pragma unroll
-    for (int k = 0; k < N; k += 4) *(uint2*)(b + k) = *(const uint2*)(g + i + k);
+    for (int k = 0; k < N; k += 4) load8_nt(b + k, g + i + k);
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = (float)b[k];
   } else {
@@ -173,8 +186,8 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long
   const uint8_t* const vc = (const uint8_t*)t.v + i;
   uint32_t mw[2] = {0, 0}, vw[2] = {0, 0};
   if (wide) {
-    *(uint2*)mw = *(const uint2*)mc;
-    *(uint2*)vw = *(const uint2*)vc;
+    load8_nt(mw, mc);
+    load8_nt(vw, vc);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -238,8 +251,8 @@ __device__ __forceinline__ void step8(const Tensor& t, const AdamwHyper& h, long
   uint8_t* const mo = (uint8_t*)t.m + i + (MODE == BANKS ? to : 0);
   uint8_t* const vo = (uint8_t*)t.v + i + (MODE == BANKS ? to : 0);
   if (wide) {
-    *(uint2*)mo = *(const uint2*)mw;
-    *(uint2*)vo = *(const uint2*)vw;
+    store8_nt(mo, mw);
+    store8_nt(vo, vw);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -290,8 +303,8 @@ __device__ __forceinline__ const Tensor& tensor_of(const Args& a, int c) {
 template <int BITS, int MODE>
 __global__ __launch_bounds__(NT) void adamw_tensors_k(Args a) {
   const Tensor& t = tensor_of(a, blockIdx.x);
+  constexpr int N = BITS == 8 ? 8 : 4, CHUNK = BITS == 8 ? CHUNK8 : CHUNK32;
   const long at = (long)((int)blockIdx.x - t.first) * CHUNK;
-  constexpr int N = BITS == 8 ? 8 : 4;
   for (int k = 0; k < CHUNK; k += NT * N) {
     const long i = at + k + (long)threadIdx.x * N;
     if constexpr (BITS == 8)
@@ -305,8 +318,8 @@ __global__ __launch_bounds__(NT) void adamw_tensors_k(Args a) {
 template <int BITS>
 __global__ __launch_bounds__(NT) void adamw_read_k(Args a) {
   const Tensor& t = tensor_of(a, blockIdx.x);
-  const long at = (long)((int)blockIdx.x - t.first) * CHUNK;
-  for (int k = 0; k < CHUNK; k += NT * 8) {
+  const long at = (long)((int)blockIdx.x - t.first) * CHUNK_READ;
+  for (int k = 0; k < CHUNK_READ; k += NT * 8) {
     const long i = at + k + (long)threadIdx.x * 8, left_l = t.n - i;
     if (left_l <= 0) return;
     const int left = left_l < 8 ? (int)left_l : 8;
@@ -344,13 +357,13 @@ bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
 // launch(args, chunks) for groups of up to MAX of the tensors, whose descriptors set(tensor, i) makes.
 template <class Set, class Launch>
-hipError_t in_groups(const rc_adamw_tensor* ts, int n, Args& a, Set set, Launch launch) {
+hipError_t in_groups(const rc_adamw_tensor* ts, int n, int chunk, Args& a, Set set, Launch launch) {
   for (int at = 0; at < n;) {
     long chunks = 0;
     a.n = 0;
     for (; at < n && a.n < MAX; ++at) {
       if (ts[at].count == 0) continue;
-      const long own = (ts[at].count + CHUNK - 1) / CHUNK;
+      const long own = (ts[at].count + chunk - 1) / chunk;
       if (a.n && chunks + own > 0x7fffffffL) break;
       Tensor& t = a.t[a.n++];
       t = set(ts[at], at);
@@ -395,7 +408,7 @@ hipError_t adamw_tensors(const rc_adamw_tensor* ts, int n, int bits, const Adamw
   a.h = h;
   a.to = 0;
   return in_groups(
-      ts, n, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, bits); },
+      ts, n, bits == 8 ? CHUNK8 : CHUNK32, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, bits); },
       [&](dim3 grid) {
         if (bits == 8)
           hipLaunchKernelGGL((adamw_tensors_k<8, IN_PLACE>), grid, dim3(NT), 0, s, a);
@@ -409,7 +422,7 @@ hipError_t adamw_banks(const rc_adamw_tensor* ts, int n, const AdamwHyper& h, lo
   a.h = h;
   a.to = to;
   return in_groups(
-      ts, n, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, 8); },
+      ts, n, CHUNK8, a, [&](const rc_adamw_tensor& x, int) { return step_tensor(x, 8); },
       [&](dim3 grid) {
         if (undo)
           hipLaunchKernelGGL((adamw_tensors_k<8, UNDO>), grid, dim3(NT), 0, s, a);
@@ -423,7 +436,7 @@ hipError_t adamw_read(const rc_adamw_tensor* ts, int n, int bits, float* const* 
   a.h = {};
   a.to = 0;
   return in_groups(
-      ts, n, a,
+      ts, n, CHUNK_READ, a,
       [&](const rc_adamw_tensor& x, int i) {
         const size_t moment = bits == 8 ? 8 : 16;
         const bool wide = aligned(m[i], 16) && aligned(v[i], 16) && aligned(x.exp_avg, moment) &&

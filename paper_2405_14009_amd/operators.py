@@ -215,6 +215,7 @@ class AdamW:
         self.decay = [True] * n if decay is None else [bool(x) for x in decay]
         self.adam = L.RcAdamConfig(lr, beta1, beta2, eps, weight_decay)
         self.device = self.params[0].device if n else None
+        self._counts = [p.numel() for p in self.params]
 
         def pointer(lists, i, name, types, count):
             if len(lists) != n:
@@ -270,12 +271,14 @@ class AdamW:
         for name, tensors in zip(("exp_avg", "exp_avg_sq"), out):
             if len(tensors) != n:
                 raise ValueError(f"{name} must have {n} entries")
-            for i, (t, p) in enumerate(zip(tensors, self.params)):
-                if not isinstance(t, torch.Tensor) or t.device != self.device:
+            pointers = (ctypes.c_void_p * max(1, n))()
+            for i, (t, count) in enumerate(zip(tensors, self._counts)):
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != self.device.index:
                     raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
-                if t.dtype != torch.float32 or t.numel() != p.numel() or not t.is_contiguous():
-                    raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {p.numel()} elements")
-            arrays.append((ctypes.c_void_p * max(1, n))(*[t.data_ptr() for t in tensors]))
+                if t.dtype is not torch.float32 or t.numel() != count or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {count} elements")
+                pointers[i] = t.data_ptr()
+            arrays.append(pointers)
         if n:
             ctx, stream = _on(self.device)
             with ctx:
