@@ -33,11 +33,12 @@ struct AttnOpArgs {
   float *m, *l;
   void* rest;
   float* drow;   // [batch, heads, spad] rowsum(dO o O)
-  float* bpart;  // [batch * heads * query blocks, buckets] shares of the bias gradient
+  float* bpart;  // [batch, heads, bias_blocks, buckets] shares of the bias gradient, by query block
+  int bias_blocks;
   void* dbias;
   // Grids of few blocks of 128 rows take 32 rows a workgroup instead, whose four
   // waves share the other side's blocks.
-  int split_q, split_k;
+  int split_f, split_q, split_k;  // forward, dq, dk and dv
   // Every query sees the sinks.  Their keys (sink_rows: up to a multiple of 32)
   // are handled twice: with the other keys for the queries whose window holds
   // them, and by workgroups of 32 keys and chunk_len queries for the others; the
@@ -49,10 +50,9 @@ struct AttnOpArgs {
   unsigned char bucket[ATTN_OP_MAX_FAR];      // of distances below `far`, one side
 };
 
-// bias_blocks: query blocks a head whose shares of the bias gradient are left in bpart.
 #define ATTN_OP_DECL(NAME)                                        \
   hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st); \
-  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st, int* bias_blocks);
+  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st);
 ATTN_OP_DECL(bf16_32)
 ATTN_OP_DECL(bf16_64)
 ATTN_OP_DECL(bf16_96)

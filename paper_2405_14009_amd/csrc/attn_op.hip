@@ -1,5 +1,5 @@
 // Host side of the attention operator: scratch memory, buckets, launches; and
-// the sum of the bias gradient's shares.
+// the sum of several calls' bias gradients.
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -41,24 +41,6 @@ int border(int exact, int k, int max_distance, int step) {
   if (std::fabs(x - near) > 1e-6 * x) return (int)std::ceil(x);
   const auto want = power((uint32_t)max_distance, step, power((uint32_t)exact, k - step));
   return at_least(power((uint32_t)near, k), want) ? near : near + 1;
-}
-
-// dbias[h, c] = sum of the shares of head h in the order of (sequence, query
-// block): sixteen or fewer groups of threads take every g-th share, then add up.
-template <class E>
-__global__ __launch_bounds__(256) void attn_op_dbias_k(const float* part, E* out, int batch, int heads, int nqb,
-                                                       int buckets) {
-  __shared__ float red[256];
-  const int h = blockIdx.x, groups = 256 / buckets, g = threadIdx.x / buckets, c = threadIdx.x % buckets;
-  float t = 0.f;
-  if (g < groups)
-    for (int i = g; i < batch * nqb; i += groups)
-      t += part[(((long)(i / nqb) * heads + h) * nqb + i % nqb) * buckets + c];
-  red[threadIdx.x] = t;
-  __syncthreads();
-  if (g != 0) return;
-  for (int k = 1; k < groups; ++k) t += red[k * buckets + c];
-  out[(long)h * buckets + c] = (E)t;
 }
 
 __global__ __launch_bounds__(256) void attn_op_add_dbias_k(AttnOpShares shares, int n, long count, float* out,
@@ -108,11 +90,12 @@ void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
   }
   const long cus = device_compute_units(), blocks = (a.s + 31) / 32 * (long)a.batch;
   a.split_q = blocks * a.heads <= cus;
+  a.split_f = blocks * a.heads <= 2 * cus;
   a.split_k = blocks * a.kv_heads <= cus;
   a.sink_rows = (a.sinks + 31) / 32 * 32;
   a.chunk_len = 512;
   while ((long)a.chunk_len * 64 < a.s) a.chunk_len *= 2;
-  a.chunks = a.sinks && !(a.split_k && a.s <= 2048) ? sink_chunks(a) : 0;
+  a.chunks = a.sinks && !(a.split_k && a.s <= a.chunk_len) ? sink_chunks(a) : 0;
 }
 
 size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
@@ -151,7 +134,6 @@ hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st) {
 
 hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work, hipStream_t st) {
   set_saved(a, saved);
-  int nqb = 0;
   char* w = (char*)work;
   a.drow = (float*)w;
   w += align256(4 * rows(a));
@@ -159,22 +141,11 @@ hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work
   w += bias_bytes(a);
   a.spart = (float*)w;
   const int c = columns(elt, a.d);
-  hipError_t e;
-  if (elt == 4)
-    e = c == 64 ? attn_op_bwd_f32_64(a, st, &nqb) : attn_op_bwd_f32_128(a, st, &nqb);
-  else
-    e = c == 32   ? attn_op_bwd_bf16_32(a, st, &nqb)
-        : c == 64 ? attn_op_bwd_bf16_64(a, st, &nqb)
-        : c == 96 ? attn_op_bwd_bf16_96(a, st, &nqb)
-                  : attn_op_bwd_bf16_128(a, st, &nqb);
-  if (e != hipSuccess || !a.bias) return e;
-  if (a.bias_f32)
-    hipLaunchKernelGGL(attn_op_dbias_k<float>, dim3(a.heads), dim3(256), 0, st, a.bpart, (float*)a.dbias, a.batch,
-                       a.heads, nqb, a.buckets);
-  else
-    hipLaunchKernelGGL(attn_op_dbias_k<bf16>, dim3(a.heads), dim3(256), 0, st, a.bpart, (bf16*)a.dbias, a.batch,
-                       a.heads, nqb, a.buckets);
-  return hipGetLastError();
+  if (elt == 4) return c == 64 ? attn_op_bwd_f32_64(a, st) : attn_op_bwd_f32_128(a, st);
+  return c == 32   ? attn_op_bwd_bf16_32(a, st)
+         : c == 64 ? attn_op_bwd_bf16_64(a, st)
+         : c == 96 ? attn_op_bwd_bf16_96(a, st)
+                   : attn_op_bwd_bf16_128(a, st);
 }
 
 hipError_t attn_op_add_dbias(const AttnOpShares& shares, int n, long count, float* out, int accumulate, hipStream_t st) {

@@ -23,7 +23,7 @@
 // least that takes one value.  Its gradient: each wave adds the dS of a near
 // block to a table of its own by distance (no two lanes of an instruction meet:
 // every sum has a fixed order); far blocks add up in registers.  The tables are summed by buckets
-// when the workgroup ends, and over workgroups by a kernel of its own.
+// when the workgroup ends, and over workgroups by the next kernel (dk and dv).
 //
 // D is formed by the same chain of matrix instructions as do.v: where a row
 // sees one token only, dS is exactly zero.
@@ -985,9 +985,34 @@ struct AttnOp {
   // A stage: a Q tile, a dO tile and the row vectors m, l, D of 64 queries.
   static constexpr int KSTAGE = 2 * TILE + 3072;
 
+  // dbias[h, c] = sum of the query blocks' shares in the order of (sequence,
+  // block): 256 / buckets groups of threads take every g-th share, then add up.
+  // By workgroups behind the others of the dk and dv kernels, which run after
+  // the one that leaves the shares.
+  static __device__ __forceinline__ void dbias(const AttnOpArgs& p, int h, float* red) {
+    const int groups = 256 / p.buckets, g = threadIdx.x / p.buckets, c = threadIdx.x % p.buckets;
+    const int n = p.batch * p.bias_blocks;
+    float t = 0.f;
+    if (g < groups)
+#pragma unroll 4
+      for (int i = g; i < n; i += groups)
+        t += p.bpart[(((long)(i / p.bias_blocks) * p.heads + h) * p.bias_blocks + i % p.bias_blocks) * p.buckets + c];
+    red[threadIdx.x] = t;
+    __syncthreads();
+    if (g != 0) return;
+    for (int k = 1; k < groups; ++k) t += red[k * p.buckets + c];
+    const long at = (long)h * p.buckets + c;
+    if (p.bias_f32)
+      ((float*)p.dbias)[at] = t;
+    else
+      ((bf16*)p.dbias)[at] = (bf16)t;
+  }
+
   static __device__ __forceinline__ void dkv(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
-    const int nkb = (p.s + 127) / 128;
+    const int nkb = (p.s + 127) / 128, units = nkb + p.sink_rows / 32 * p.chunks;
+    if constexpr (BIAS)
+      if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
     if (kb >= nkb) return dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
     float* const table = (float*)(lds + STAGES * KSTAGE);
     const int lane = threadIdx.x & 63;
@@ -1157,7 +1182,9 @@ struct AttnOp {
   }
   static __device__ __forceinline__ void dkv_split(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
-    const int nkb = (p.s + 31) / 32;
+    const int nkb = (p.s + 31) / 32, units = nkb + p.sink_rows / 32 * p.chunks;
+    if constexpr (BIAS)
+      if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
     if (kb >= nkb)
       dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
     else if (p.chunks)
@@ -1246,7 +1273,7 @@ hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
   static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 5 * kTableMost <= kLds &&
                     4 * K::KOWN + kTableMost <= kLds && K::STAGES * K::KSTAGE + kTableMost <= kLds,
                 "LDS at the largest table");
-  const bool split = a.split_q;
+  const bool split = a.split_f;
   const long rows = split ? 32 : 128;
   const dim3 grid((unsigned)((a.s + rows - 1) / rows * a.batch * a.heads));
   if (split)
@@ -1257,14 +1284,15 @@ hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
 }
 
 template <class T, bool BIAS>
-hipError_t attn_op_bwd_launch(const AttnOpArgs& a, hipStream_t st, int* bias_blocks) {
+hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
+  AttnOpArgs a = args;
   using K = AttnOp<T, BIAS>;
   // (the one form that does not always fit: five tables of a far bias next to the tiles of fp32 heads of 128)
   const bool sq = a.split_q && K::dq_lds(a, true) <= kLds, sk = a.split_k;
   const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
   const dim3 gq((unsigned)(nq * a.batch * a.heads));
-  const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads));
-  *bias_blocks = (int)nq;
+  const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
+  a.bias_blocks = (int)nq;
   if (sq)
     hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, true), st, a);
   else
@@ -1288,7 +1316,6 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& a, hipStream_t st, int* bias_blo
   hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st) {                             \
     return a.bias ? attn_op_fwd_launch<T, true>(a, st) : attn_op_fwd_launch<T, false>(a, st);      \
   }                                                                                                \
-  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st, int* bias_blocks) {           \
-    return a.bias ? attn_op_bwd_launch<T, true>(a, st, bias_blocks)                                \
-                  : attn_op_bwd_launch<T, false>(a, st, bias_blocks);                              \
+  hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st) {                             \
+    return a.bias ? attn_op_bwd_launch<T, true>(a, st) : attn_op_bwd_launch<T, false>(a, st);      \
   }

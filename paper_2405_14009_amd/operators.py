@@ -8,7 +8,6 @@ outputs and scratch memory from PyTorch, so they may be captured into a graph.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import math
@@ -17,8 +16,16 @@ from typing import Optional, Sequence
 from . import _lib as L
 
 
+_modules = {}
+
+
 def _torch():
-    import torch
+    """PyTorch, imported with the first call."""
+    torch = _modules.get("torch")
+    if torch is None:
+        import torch
+        _modules["torch"] = torch
+        _modules["kinds"] = {torch.bfloat16: L.RC_BF16, torch.float32: L.RC_FP32}
     return torch
 
 
@@ -27,18 +34,17 @@ def _kind(t, name):
     torch = _torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    dtype = t.dtype
-    if dtype is torch.bfloat16:
-        return L.RC_BF16
-    if dtype is torch.float32:
-        return L.RC_FP32
-    raise ValueError(f"{name} must be bfloat16 or float32, not {dtype}")
+    kind = _modules["kinds"].get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
+    return kind
 
 
-def _view(t, name, like, shape):
-    """A view of a tensor that goes with q (`like`)."""
-    if t is not like:
-        if _kind(t, name) != _kind(like, "q") or t.device != like.device:
+def _view(t, name, q, shape):
+    """A view of a tensor that goes with q."""
+    if t is not q:
+        _kind(t, name)
+        if t.dtype is not q.dtype or t.device != q.device:
             raise ValueError(f"{name} must have the type and device of q")
         if t.shape != shape:
             raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
@@ -49,12 +55,30 @@ def _view(t, name, like, shape):
     return L.RcView(t.data_ptr(), b if shape[0] > 1 else 0, s if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
 
 
+def _new(shape, q):
+    """An output of ours and its view."""
+    t = _torch().empty(shape, dtype=q.dtype, device=q.device)
+    _, s, h, d = shape
+    return t, L.RcView(t.data_ptr(), s * h * d, h * d, d)
+
+
 def _on(device):
-    """The device as PyTorch's current one, and its stream."""
-    torch = _torch()
-    if device.index is None or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext(), torch.cuda.current_stream(device)
-    return torch.cuda.device(device), torch.cuda.current_stream(device)
+    """The device as PyTorch's current one (None: it is), and its stream's handle."""
+    cuda = _torch().cuda
+    index = device.index
+    if index is None or index == cuda.current_device():
+        return None, cuda.current_stream(index).cuda_stream
+    return cuda.device(device), cuda.current_stream(index).cuda_stream
+
+
+def _call(on, function, *args):
+    if on is None:
+        status = function(*args)
+    else:
+        with on:
+            status = function(*args)
+    if status != L.RC_OK:
+        L.check(status)
 
 
 @functools.lru_cache(maxsize=256)
@@ -124,14 +148,12 @@ def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: i
     None with save=False.  out: a tensor for o."""
     torch = _torch()
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
-    ctx, stream = _on(q.device)
-    with ctx:
-        o = torch.empty(c.shape, dtype=q.dtype, device=q.device) if out is None else out
-        ov = _view(o, "out", q, c.shape)
-        saved = torch.empty(c.saved_bytes, dtype=torch.uint8, device=q.device) if save else None
-        L.check(c.lib.rc_attention_forward(
-            ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
-            ctypes.byref(ov), saved.data_ptr() if save else None, stream.cuda_stream))
+    on, stream = _on(q.device)
+    o, ov = _new(c.shape, q) if out is None else (out, _view(out, "out", q, c.shape))
+    saved = torch.empty(c.saved_bytes, dtype=torch.uint8, device=q.device) if save else None
+    ref = ctypes.byref
+    _call(on, c.lib.rc_attention_forward, ref(c.c), ref(c.q), ref(c.k), ref(c.v), c.bias, c.lengths, ref(ov),
+          saved.data_ptr() if save else None, stream)
     return o, saved
 
 
@@ -147,21 +169,16 @@ def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: 
     if not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device:
         raise ValueError("saved must be what attention_forward returned for these arguments")
     ov, dov = _view(o, "o", q, c.shape), _view(dout, "dout", q, c.shape)
-    ctx, stream = _on(q.device)
-    with ctx:
-        def given(t, name, shape):
-            t = torch.empty(shape, dtype=q.dtype, device=q.device) if t is None else t
-            return t, _view(t, name, q, shape)
-
-        (dq, dqv), (dk, dkv), (dv, dvv) = given(dq, "dq", c.shape), given(dk, "dk", c.kv_shape), given(
-            dv, "dv", c.kv_shape)
-        dbias = None if rel_bias is None else torch.empty_like(rel_bias)
-        work = torch.empty(c.work_bytes, dtype=torch.uint8, device=q.device)
-        L.check(c.lib.rc_attention_backward(
-            ctypes.byref(c.c), ctypes.byref(c.q), ctypes.byref(c.k), ctypes.byref(c.v), c.bias, c.lengths,
-            ctypes.byref(ov), saved.data_ptr(), ctypes.byref(dov), ctypes.byref(dqv), ctypes.byref(dkv),
-            ctypes.byref(dvv), None if dbias is None else dbias.data_ptr(), work.data_ptr(),
-            stream.cuda_stream))
+    on, stream = _on(q.device)
+    dq, dqv = _new(c.shape, q) if dq is None else (dq, _view(dq, "dq", q, c.shape))
+    dk, dkv = _new(c.kv_shape, q) if dk is None else (dk, _view(dk, "dk", q, c.kv_shape))
+    dv, dvv = _new(c.kv_shape, q) if dv is None else (dv, _view(dv, "dv", q, c.kv_shape))
+    dbias = None if rel_bias is None else torch.empty_like(rel_bias)
+    work = torch.empty(c.work_bytes, dtype=torch.uint8, device=q.device)
+    ref = ctypes.byref
+    _call(on, c.lib.rc_attention_backward, ref(c.c), ref(c.q), ref(c.k), ref(c.v), c.bias, c.lengths, ref(ov),
+          saved.data_ptr(), ref(dov), ref(dqv), ref(dkv), ref(dvv), None if dbias is None else dbias.data_ptr(),
+          work.data_ptr(), stream)
     return dq, dk, dv, dbias
 
 
@@ -228,6 +245,9 @@ class AdamW:
                                  f"{' or '.join(str(x) for x in types)}")
             return t.data_ptr()
 
+        used = [p.data_ptr() for p in self.params if p.numel()]
+        if len(set(used)) != len(used):
+            raise ValueError("a parameter is listed twice")
         if len(self.decay) != n or len(self.copies) != n or len(self.grads) != n:
             raise ValueError(f"grads, decay and copies must have {n} entries")
         self._tensors = (L.RcAdamwTensor * max(1, n))()
@@ -253,10 +273,9 @@ class AdamW:
         if not self.params:
             self.steps = number
             return
-        ctx, stream = _on(self.device)
-        with ctx:
-            L.check(self._lib.rc_adamw_step(self._tensors, len(self.params), ctypes.byref(self.adam), self.state_bits,
-                                            number, float(grad_scale), ctypes.c_void_p(stream.cuda_stream)))
+        on, stream = _on(self.device)
+        _call(on, self._lib.rc_adamw_step, self._tensors, len(self.params), ctypes.byref(self.adam),
+              self.state_bits, number, float(grad_scale), stream)
         self.steps = number
 
     def moments(self, out=None):
@@ -280,8 +299,6 @@ class AdamW:
                 pointers[i] = t.data_ptr()
             arrays.append(pointers)
         if n:
-            ctx, stream = _on(self.device)
-            with ctx:
-                L.check(self._lib.rc_adamw_read(self._tensors, n, self.state_bits, *arrays,
-                                                ctypes.c_void_p(stream.cuda_stream)))
+            on, stream = _on(self.device)
+            _call(on, self._lib.rc_adamw_read, self._tensors, n, self.state_bits, *arrays, stream)
         return out[0], out[1]

@@ -101,6 +101,12 @@ def kernel_class(name: str) -> str:
         return "attn_fwd"
     if "attn_bwd" in name:
         return "attn_bwd"
+    if "attn_op_fwd" in name:
+        return "attn_fwd"
+    if "attn_op_add_dbias" in name:
+        return "reduce"
+    if "attn_op_" in name:            # dq, dk and dv, the sinks' shares
+        return "attn_bwd"
     if re.search(r"ln_(fwd|bwd)(_wave)?_k", name):
         return "layernorm"
     if "colsum" in name:

@@ -261,3 +261,17 @@ def test_moment_formats():
                 want[:1] = np.where(want[:1] == 0, 1, want[:1])
             assert np.array_equal(c[:-1], want)
     assert ref.encode_v(np.array([1e-30, 1.0]))[0][0] == 1 and ref.encode_v(np.array([0.0, 1.0]))[0][0] == 0
+
+
+@pytest.mark.parametrize("name,cls", [
+    ("void (anonymous namespace)::attn_op_fwd_k<(anonymous namespace)::TileB16<128>, true>(AttnOpArgs)", "attn_fwd"),
+    ("void (anonymous namespace)::attn_op_fwd32_k<(anonymous namespace)::TileF32<64>, false>(AttnOpArgs)", "attn_fwd"),
+    ("void (anonymous namespace)::attn_op_dq_k<(anonymous namespace)::TileB16<64>, true>(AttnOpArgs)", "attn_bwd"),
+    ("void (anonymous namespace)::attn_op_dkv32_k<(anonymous namespace)::TileB16<64>, true>(AttnOpArgs)", "attn_bwd"),
+    ("void (anonymous namespace)::attn_op_sinks_k<(anonymous namespace)::TileB16<64> >(AttnOpArgs)", "attn_bwd"),
+    ("(anonymous namespace)::attn_op_add_dbias_k(AttnOpShares, int, long, float*, int)", "reduce"),
+    ("void (anonymous namespace)::adamw_tensors_k<8, 1>((anonymous namespace)::Args)", "adamw"),
+])
+def test_profile_classes_of_the_operators(name, cls):
+    from paper_2405_14009_amd.profile_summary import kernel_class
+    assert kernel_class(name) == cls
