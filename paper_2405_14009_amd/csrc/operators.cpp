@@ -20,7 +20,7 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   if (c.heads % c.kv_heads) return rc_set_error(RC_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
   if (c.causal != 0 && c.causal != 1) return rc_set_error(RC_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (c.window < 0 || c.sinks < 0) return rc_set_error(RC_ERR_INVALID_ARG, "window and sinks must not be negative");
-  if (!(c.scale > 0.f) || !std::isfinite(c.scale))
+  if (!(c.scale > 0.f) || !std::isfinite(c.scale * 1.4426950408889634f))
     return rc_set_error(RC_ERR_INVALID_ARG, "scale must be finite and above zero");
   if (c.buckets) {
     const int side = c.causal ? c.buckets : c.buckets / 2;
@@ -141,7 +141,7 @@ rc_status bias_args(const rc_attention* c, const void* bias, const int32_t* leng
   return RC_OK;
 }
 
-constexpr int64_t kMaxCount = (int64_t)1 << 42;
+constexpr int64_t kMaxCount = (int64_t)1 << 40;
 
 rc_status moment_args(const rc_adamw_tensor& t, int state_bits, const std::string& name) {
   if (!t.exp_avg || !t.exp_avg_sq) return fail(RC_ERR_INVALID_ARG, name + "null array");

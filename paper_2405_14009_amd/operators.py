@@ -5,6 +5,8 @@ over many tensors.
 Argument marshalling only: every step runs in the HIP library.  The calls
 enqueue on PyTorch's current stream of the tensors' device and take their
 outputs and scratch memory from PyTorch, so they may be captured into a graph.
+Autograd does not record them: a backward pass is a call of its own, as it is
+for a stage.
 """
 from __future__ import annotations
 

@@ -64,6 +64,7 @@ BAD_ATTENTION = [
     (dict(scale=-1.0), "INVALID_ARG", b"scale"),
     (dict(scale=math.nan), "INVALID_ARG", b"scale"),
     (dict(scale=math.inf), "INVALID_ARG", b"scale"),
+    (dict(scale=3e38), "INVALID_ARG", b"scale"),
     (dict(buckets=-4), "INVALID_ARG", b"buckets"),
     (dict(buckets=1, max_distance=8), "INVALID_ARG", b"buckets"),
     (dict(buckets=7, max_distance=8, causal=0), "INVALID_ARG", b"even"),
