@@ -23,6 +23,7 @@ struct AttnOpArgs {
   int batch, s, spad, heads, kv_heads, group, d;
   // token j is in the window of token i iff -left <= j - i <= right
   int causal, left, right, sinks;
+  int seen;  // no row sees more tokens
   float scale, sl2;  // of the products, and with log2(e)
   // relative position bias [heads, buckets]; distances of `far` or more share
   // the last bucket of their side

@@ -78,6 +78,8 @@ void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
   a.right = a.causal ? 0 : a.left;
   if (!window) a.sinks = 0;
   a.sinks = a.sinks < a.s ? a.sinks : a.s;
+  const long seen = window ? (a.causal ? 1L : 2L) * window + a.sinks : a.s;
+  a.seen = (int)(seen < a.s ? seen : a.s);
   if (a.buckets) {
     const int side = a.causal ? a.buckets : a.buckets / 2, exact = side / 2, k = side - exact;
     for (int c = 0; c < side; ++c)

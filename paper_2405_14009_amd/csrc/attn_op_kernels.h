@@ -96,14 +96,25 @@ struct TileB16 {
 #pragma unroll
     for (int ks = 0; ks < HD / 16; ++ks) a = A::mfma(x[ks], y[ks], a);
   }
-  // acc += (32 rows j of the tile)^T times the block p
+  // acc += (32 rows j of the tile)^T times the block p, which is rounded to bf16 for
+  // that; FINE: and times what the rounding drops.
+  template <bool FINE>
   static __device__ __forceinline__ void outer(f32x16 (&acc)[HD / 32], const char* tile, int j, const f32x16& p,
                                                const Offs& o, int) {
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const bf16x8 pf = A::pack_half(p, hf);
+      bf16x8 rest;
+      if constexpr (FINE) {
 #pragma unroll
-      for (int b = 0; b < HD / 32; ++b) acc[b] = A::mfma(A::rd_tr(tile, o.to, b, 2 * j + hf), pf, acc[b]);
+        for (int e = 0; e < 8; ++e) rest[e] = (bf16)(p[8 * hf + e] - (float)pf[e]);
+      }
+#pragma unroll
+      for (int b = 0; b < HD / 32; ++b) {
+        const bf16x8 t = A::rd_tr(tile, o.to, b, 2 * j + hf);
+        acc[b] = A::mfma(t, pf, acc[b]);
+        if constexpr (FINE) acc[b] = A::mfma(t, rest, acc[b]);
+      }
     }
   }
   static __device__ __forceinline__ void store(const f32x16 (&acc)[HD / 32], char* t, E* base, long ld, int row0,
@@ -206,6 +217,7 @@ struct TileF32 {
 #pragma unroll
     for (int k = 0; k < HD / 2; ++k) a = mfma(x[k], y[k], a);
   }
+  template <bool>
   static __device__ __forceinline__ void outer(f32x16 (&acc)[HD / 32], const char* tile, int j, const f32x16& p,
                                                const Offs&, int lane) {
     const float* x = (const float*)tile + (32 * j + 4 * (lane >> 5)) * LD + (lane & 31);
@@ -513,6 +525,15 @@ struct AttnOp {
       }
     st.l += ls;
   }
+  // One block of 64 keys.  D = do.o keeps the rounding of the
+  // exponentials to bf16, as the root of the sum of squares of a row's
+  // probabilities next to dS's own: it counts where rows see few tokens (rel-L2
+  // of dq, 12 tokens a sequence: 2.8e-3, against 2.4e-3), and where the bias
+  // gradient sums it over the far bucket, which holds most of a long row
+  // (2133 tokens, both directions, 8 buckets: 4.1e-3, against 1.7e-3).  There the
+  // forward also adds what the rounding drops (FINE; us, 32 heads of 128, s 2048, with
+  // a bias: 64 -> 75).
+  template <bool FINE>
   static __device__ __forceinline__ void fwd_tile(Fwd& st, const Rows& qf, const char* kt, const char* vt, const Offs& of,
                                                   int k0, int q0, int qq, int lane, int len, const float* table,
                                                   const AttnOpArgs& p) {
@@ -522,12 +543,13 @@ struct AttnOp {
     zero(sc[1]);
     T::score2(sc[0], kt, 0, qf, sc[1], kt, 1, qf, of, lane);
     softmax<2>(st, sc, k0, q0, qq, lane, len, table, p);
-    T::outer(st.o, vt, 0, sc[0], of, lane);
-    T::outer(st.o, vt, 1, sc[1], of, lane);
+    T::template outer<FINE>(st.o, vt, 0, sc[0], of, lane);
+    T::template outer<FINE>(st.o, vt, 1, sc[1], of, lane);
   }
 
   static constexpr int STAGE = 2 * TILE;
 
+  template <bool FINE>
   static __device__ __forceinline__ void fwd(const AttnOpArgs& p, char* lds) {
     float* const table = (float*)(lds + STAGES * STAGE);
     const int lane = threadIdx.x & 63;
@@ -555,7 +577,7 @@ struct AttnOp {
     Fwd st;
     reset(st);
     pipeline(steps.n, lds, STAGE, issue, [&](char* cur, int it) {
-      fwd_tile(st, qf, cur, cur + TILE, of, steps.tile(it) * 64, q0, qq, lane, len, table, p);
+      fwd_tile<FINE>(st, qf, cur, cur + TILE, of, steps.tile(it) * 64, q0, qq, lane, len, table, p);
     });
     fwd_store(st, p, b, h, q0, qq, len, lane, lds + wave * (STAGE / 4));
   }
@@ -564,6 +586,7 @@ struct AttnOp {
   // tiles of their own, and join their sums through LDS.
   static constexpr int OWN = 2 * (TILE / 2);
   static_assert(NB * 4096 <= OWN, "a wave's sums in its tiles");
+  template <bool FINE>
   static __device__ __forceinline__ void fwd32(const AttnOpArgs& p, char* lds) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -602,7 +625,7 @@ struct AttnOp {
         zero(sc[0]);
         T::score1(sc[0], own, qf, of, lane);
         softmax<1>(st, sc, k0, q0, qq, lane, len, table, p);
-        T::outer(st.o, own + TILE / 2, 0, sc[0], of, lane);
+        T::template outer<FINE>(st.o, own + TILE / 2, 0, sc[0], of, lane);
       }
       T::own_read();
       if (it + 4 < steps.n) issue(it + 4);
@@ -783,7 +806,10 @@ struct AttnOp {
     }
   }
 
-  // acc += dS times the 32 keys from k (rows j of the tiles).
+  // acc += dS times the 32 keys from k (rows j of the tiles).  FINE (small grids,
+  // rows of few tokens): with what the rounding of dS drops, which there costs little
+  // and is not averaged over a row.
+  template <bool FINE>
   static __device__ __forceinline__ void dq_block(f32x16 (&acc)[NB], const Queries& w, const char* kt, const char* vt,
                                                   int j, const Offs& of, int k, int q0, int qq, int lane, int len,
                                                   const float* table, Sums& sums, const AttnOpArgs& p) {
@@ -818,7 +844,7 @@ struct AttnOp {
           sums.right += t;
       }
     }
-    T::outer(acc, kt, j, dp, of, lane);
+    T::template outer<FINE>(acc, kt, j, dp, of, lane);
   }
 
   static __device__ __forceinline__ void dq(const AttnOpArgs& p, char* lds) {
@@ -856,7 +882,7 @@ struct AttnOp {
       const int k0 = steps.tile(it) * 64;
 #pragma unroll 1
       for (int j = 0; j < 2; ++j)
-        dq_block(acc, w, cur, cur + TILE, j, of, k0 + 32 * j, q0, qq, lane, len, table, sums, p);
+        dq_block<false>(acc, w, cur, cur + TILE, j, of, k0 + 32 * j, q0, qq, lane, len, table, sums, p);
     });
     if (qq >= len) {
 #pragma unroll
@@ -867,6 +893,7 @@ struct AttnOp {
   }
 
   // 32 queries a workgroup, as fwd32.
+  template <bool FINE>
   static __device__ __forceinline__ void dq32(const AttnOpArgs& p, char* lds) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -901,7 +928,7 @@ struct AttnOp {
     }
     for (int it = wave; it < steps.n; it += 4) {
       T::own_landed();
-      dq_block(acc, w, own, own + TILE / 2, 0, of, steps.tile(it) * 32, q0, qq, lane, len, table, sums, p);
+      dq_block<FINE>(acc, w, own, own + TILE / 2, 0, of, steps.tile(it) * 32, q0, qq, lane, len, table, sums, p);
       T::own_read();
       if (it + 4 < steps.n) issue(it + 4);
     }
@@ -933,7 +960,7 @@ struct AttnOp {
     }
   }
   // dk, dv += the 32 queries from q (rows j of the tiles), with their statistics.
-  template <int MODE>
+  template <int MODE, bool FINE>
   static __device__ __forceinline__ void dkv_block(f32x16 (&dk)[NB], f32x16 (&dv)[NB], const Rows& kf, const Rows& vf,
                                                    const char* qt, const char* dt, int j, const float* m, const float* l,
                                                    const float* D, const Offs& of, int q, int k0, int kk, int lane,
@@ -967,8 +994,8 @@ struct AttnOp {
     if (wave_uniform(!all_of<MODE>(p, q, k0, len))) mask_queries<MODE>(sc, q, kk, lane, len, p);
 #pragma unroll
     for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (dp[r] - row[r]);
-    T::outer(dv, dt, j, sc, of, lane);
-    T::outer(dk, qt, j, dp, of, lane);
+    T::template outer<FINE>(dv, dt, j, sc, of, lane);
+    T::template outer<FINE>(dk, qt, j, dp, of, lane);
   }
 
   // This wave's rows k0.. of dk or dv as share `n` of the sinks' rows.
@@ -1013,7 +1040,7 @@ struct AttnOp {
     const int nkb = (p.s + 127) / 128, units = nkb + p.sink_rows / 32 * p.chunks;
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
-    if (kb >= nkb) return dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
+    if (kb >= nkb) return dkv32<SINK, false>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
     float* const table = (float*)(lds + STAGES * KSTAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1063,7 +1090,7 @@ struct AttnOp {
       const float* vec = (const float*)(cur + 2 * TILE);
 #pragma unroll 1
       for (int j = 0; j < 2; ++j)
-        dkv_block<WINDOW>(dk, dv, kf, vf, cur, cur + TILE, j, vec + 32 * j, vec + 256 + 32 * j, vec + 512 + 32 * j, of,
+        dkv_block<WINDOW, false>(dk, dv, kf, vf, cur, cur + TILE, j, vec + 32 * j, vec + 256 + 32 * j, vec + 512 + 32 * j, of,
                           (t0 + tc) * 64 + 32 * j, k0, kk, lane, len, table, p);
       if (++tc == nt) tc = 0, ++gc;
     });
@@ -1091,7 +1118,7 @@ struct AttnOp {
   // every head of the group, with tiles of their own.  MODE SINK: the sinks among
   // the keys, for the queries of a chunk that see them as such.
   static constexpr int KOWN = OWN + 3072;
-  template <int MODE>
+  template <int MODE, bool FINE>
   static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1147,8 +1174,8 @@ struct AttnOp {
       const float* vec = (const float*)(own + OWN);
       for (int it = wave; it < nt; it += 4) {
         T::own_landed();
-        dkv_block<MODE>(dk, dv, kf, vf, own, own + TILE / 2, 0, vec, vec + 256, vec + 512, of, (t0 + it) * 32, k0, kk,
-                        lane, len, table, p);
+        dkv_block<MODE, FINE>(dk, dv, kf, vf, own, own + TILE / 2, 0, vec, vec + 256, vec + 512, of, (t0 + it) * 32,
+                              k0, kk, lane, len, table, p);
         T::own_read();
         if (it + 4 < nt) issue(it + 4);
       }
@@ -1180,17 +1207,18 @@ struct AttnOp {
       }
     }
   }
+  template <bool FINE>
   static __device__ __forceinline__ void dkv_split(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
     const int nkb = (p.s + 31) / 32, units = nkb + p.sink_rows / 32 * p.chunks;
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
     if (kb >= nkb)
-      dkv32<SINK>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
+      dkv32<SINK, FINE>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
     else if (p.chunks)
-      dkv32<WINDOW>(p, lds, z, kb * 32, 0);
+      dkv32<WINDOW, FINE>(p, lds, z, kb * 32, 0);
     else
-      dkv32<BOTH>(p, lds, z, kb * 32, 0);
+      dkv32<BOTH, FINE>(p, lds, z, kb * 32, 0);
   }
 
   // LDS of the kernels.
@@ -1237,49 +1265,52 @@ __global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
 
 extern __shared__ __attribute__((aligned(1024))) char attn_op_lds[];
 
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_fwd_k(
     AttnOpArgs p) {
-  AttnOp<T, BIAS>::fwd(p, attn_op_lds);
+  AttnOp<T, BIAS>::template fwd<FINE>(p, attn_op_lds);
 }
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) void attn_op_fwd32_k(AttnOpArgs p) {
-  AttnOp<T, BIAS>::fwd32(p, attn_op_lds);
+  AttnOp<T, BIAS>::template fwd32<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_dq_k(
     AttnOpArgs p) {
   AttnOp<T, BIAS>::dq(p, attn_op_lds);
 }
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) void attn_op_dq32_k(AttnOpArgs p) {
-  AttnOp<T, BIAS>::dq32(p, attn_op_lds);
+  AttnOp<T, BIAS>::template dq32<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::KWAVES, T::KWAVES))) void attn_op_dkv_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::dkv(p, attn_op_lds);
 }
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) void attn_op_dkv32_k(AttnOpArgs p) {
-  AttnOp<T, BIAS>::dkv_split(p, attn_op_lds);
+  AttnOp<T, BIAS>::template dkv_split<FINE>(p, attn_op_lds);
 }
 
 constexpr size_t kLds = 160 * 1024;  // of a compute unit
+// Rows of so few tokens take the FINE kernels (rel-L2 of dq over that of its own
+// rounding, 142 tokens: 1.50 with the coarse forward, 1.46 with the fine one; 4
+// tokens: 1.9 with the coarse backward).
+constexpr int kSeenForward = 160, kSeenBackward = 64;
 constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 192);
 
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
   using K = AttnOp<T, BIAS>;
   static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 5 * kTableMost <= kLds &&
                     4 * K::KOWN + kTableMost <= kLds && K::STAGES * K::KSTAGE + kTableMost <= kLds,
                 "LDS at the largest table");
-  const bool split = a.split_f;
-  const long rows = split ? 32 : 128;
+  const long rows = a.split_f ? 32 : 128;
   const dim3 grid((unsigned)((a.s + rows - 1) / rows * a.batch * a.heads));
-  if (split)
-    hipLaunchKernelGGL((attn_op_fwd32_k<T, BIAS>), grid, dim3(256), K::fwd_lds(a, true), st, a);
+  if (a.split_f)
+    hipLaunchKernelGGL((attn_op_fwd32_k<T, BIAS, FINE>), grid, dim3(256), K::fwd_lds(a, true), st, a);
   else
-    hipLaunchKernelGGL((attn_op_fwd_k<T, BIAS>), grid, dim3(256), K::fwd_lds(a, false), st, a);
+    hipLaunchKernelGGL((attn_op_fwd_k<T, BIAS, FINE>), grid, dim3(256), K::fwd_lds(a, false), st, a);
   return hipGetLastError();
 }
 
@@ -1293,14 +1324,19 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
   const dim3 gq((unsigned)(nq * a.batch * a.heads));
   const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
   a.bias_blocks = (int)nq;
-  if (sq)
-    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, true), st, a);
+  const bool fine = T::REST && a.seen <= kSeenBackward;
+  if (sq && fine)
+    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, T::REST>), gq, dim3(256), K::dq_lds(a, true), st, a);
+  else if (sq)
+    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, false>), gq, dim3(256), K::dq_lds(a, true), st, a);
   else
     hipLaunchKernelGGL((attn_op_dq_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, false), st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (sk)
-    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, true), st, a);
+  if (sk && fine)
+    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, T::REST>), gk, dim3(256), K::dkv_lds(a, true), st, a);
+  else if (sk)
+    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, false>), gk, dim3(256), K::dkv_lds(a, true), st, a);
   else
     hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, false), st, a);
   e = hipGetLastError();
@@ -1314,7 +1350,9 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
 
 #define ATTN_OP_DEFINE(NAME, T)                                                                    \
   hipError_t attn_op_fwd_##NAME(const AttnOpArgs& a, hipStream_t st) {                             \
-    return a.bias ? attn_op_fwd_launch<T, true>(a, st) : attn_op_fwd_launch<T, false>(a, st);      \
+    return a.bias                   ? attn_op_fwd_launch<T, true, T::REST>(a, st)                  \
+           : a.seen <= kSeenForward ? attn_op_fwd_launch<T, false, T::REST>(a, st)                 \
+                                    : attn_op_fwd_launch<T, false, false>(a, st);                  \
   }                                                                                                \
   hipError_t attn_op_bwd_##NAME(const AttnOpArgs& a, hipStream_t st) {                             \
     return a.bias ? attn_op_bwd_launch<T, true>(a, st) : attn_op_bwd_launch<T, false>(a, st);      \
