@@ -97,7 +97,7 @@ def attention(q, k, v, do=None, *, causal=True, window=0, sinks=0, bias=None, ma
     return out, mag
 
 
-def bounds(out, mag, kind, bias_kind=None):
+def bounds(out, mag, kind, bias_kind=None, fine=False):
     """How far each element of an output may be from its 64-bit value.
 
     half: half a step of a type, relative (bf16 2^-8, fp32 2^-24).
@@ -111,7 +111,9 @@ def bounds(out, mag, kind, bias_kind=None):
     probabilities); do.v and D are sums in 32 bits of absolute value
     |do| |v|; and, bf16, dS is rounded before its products.  The sums over
     tokens add 32-bit roundings: under 2^-16 of the absolute values for the up
-    to 2^8 in a row of one accumulator here."""
+    to 2^8 in a row of one accumulator here.
+    fine: calls whose o takes the probabilities and o itself as two bf16 numbers each
+    where D is formed, so that D is off by 2 * 2^-16 in place of eP."""
     half = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
     r = half[kind] if kind == torch.bfloat16 else 0.0
     exact = 2.0 ** -24
@@ -125,15 +127,15 @@ def bounds(out, mag, kind, bias_kind=None):
         if name in ("o", "dv"):
             e = (ep + sums) * m[0]
         else:
-            e = ((r if name != "dbias" else 0.0) + ex + sums) * m[0] + ep * m[1] + sums * m[2]
+            e = ((r if name != "dbias" else 0.0) + ex + sums) * m[0] + (2.0 ** -15 + ex if fine else ep) * m[1] + sums * m[2]
         got[name] = (e + last * (ref.abs() + e)) * 1.01 + 1e-30
     return got
 
 
-def check_attention(got, out, mag, kind, bias_kind=None):
+def check_attention(got, out, mag, kind, bias_kind=None, fine=False):
     """Every element within its bound; returns the worst share of a bound."""
     worst = {}
-    for name, bound in bounds(out, mag, kind, bias_kind).items():
+    for name, bound in bounds(out, mag, kind, bias_kind, fine).items():
         x = got[name].cpu().to(F64)
         assert x.shape == out[name].shape, name
         assert bool(torch.isfinite(x).all()), f"{name}: not finite"

@@ -264,6 +264,23 @@ def test_large_scores(kind):
     compare(t, do, run(t, do, **how), **how)
 
 
+@pytest.mark.parametrize("s,buckets", [(1300, 8), (64, 16)])
+def test_bias_gradient_of_bf16_tensors_in_32_bits(s, buckets):
+    """A bias and its gradient in fp32 next to bf16 tensors (a stage's): the far bucket holds
+    most of a long row, and what D is off by sums up there.  D = do.o is formed from
+    probabilities and outputs of two bf16 numbers each, so no value that was rounded to bf16
+    once enters: the error stays below half of one such rounding, 2^-10 (with
+    probabilities of one bf16 number it was 4e-3)."""
+    t, do = inputs(1, s, 2, 2, 64)
+    how = dict(causal=False, rel_bias=normal(9, 2, buckets, kind=F32), max_distance=128)
+    got = run(t, do, **how)
+    out, mag = ref.attention(t["q"], t["k"], t["v"], do, causal=False, bias=how["rel_bias"], max_distance=128)
+    worst = ref.check_attention({"dbias": got["dbias"]}, {"dbias": out["dbias"]}, mag, BF16, F32, fine=True)
+    rel = float((got["dbias"].cpu().double() - out["dbias"]).norm() / out["dbias"].norm())
+    print(f"[bias gradient] s {s}: rel-L2 {rel:.1e}, share of the bound {worst}")
+    assert rel < 2.0 ** -10
+
+
 def test_gradients_against_differences():
     """dq, dk, dv and dbias of a small fp32 call against central differences of
     the 64-bit operator.  A difference of step e = 2^-10 is off by e^2 / 6 of a
