@@ -444,7 +444,9 @@ typedef struct rc_view {
  * o_i = sum_j P_ij v_j, P_ij = softmax over the visible j of
  *   scale q_i.k_j + bias[head, bucket(j - i)].
  * Tokens at or behind their sequence's length have o = 0 and gradients of 0, and
- * nothing of theirs is read.
+ * nothing of theirs is read.  (Infinities and NaN of a token within its
+ * sequence may also reach rows that do not see it: their product with a zero
+ * probability is NaN.)
  *
  * Query head h reads key / value head h / (heads / kv_heads).
  *
@@ -456,7 +458,8 @@ typedef struct rc_view {
  *
  * Requirements (otherwise RC_ERR_UNSUPPORTED): head_dim a multiple of 8, at
  * most 128; buckets at most 128, max_distance at most 1024; seq_len at most
- * 2^24; bf16: a head's tokens span less than 2^31 bytes in every tensor. */
+ * 2^24; batch heads ceil(seq_len / 128) below 2^24 (with a window as much per 8
+ * sinks); bf16: a head's tokens span less than 2^31 bytes in every tensor. */
 typedef struct rc_attention {
   int32_t dtype;        /* rc_dtype of q, k, v, o and their gradients */
   int32_t batch, seq_len, heads, kv_heads, head_dim;
@@ -492,7 +495,7 @@ rc_status rc_attention_backward(const rc_attention* a, const rc_view* q, const r
                                 void* dbias, void* work, void* hip_stream);
 
 /* One tensor of an AdamW step.  Its arrays are contiguous and have `count`
- * elements; pointers need only the alignment of their elements (aligned to 16
+ * elements (less than 2^34 - 2^10 + 1); pointers need only the alignment of their elements (aligned to 16
  * bytes they are read faster).
  * 32-bit moments: exp_avg and exp_avg_sq are fp32, both scales NULL.
  * 8-bit moments: one byte an element, and a byte for each 128 consecutive

@@ -7,6 +7,9 @@
 #include "recycle_stage.h"
 
 constexpr int ADAMW_BLOCK = 128;  // elements that share a power of two (8-bit moments)
+// A launch holds fewer than 2^32 threads: workgroups of 256, each of at least 1024 elements.
+constexpr long ADAMW_MAX_GROUPS = (1L << 24) - 1;
+constexpr int64_t ADAMW_MAX_COUNT = ADAMW_MAX_GROUPS * 1024;
 
 struct AdamwHyper {
   double beta1, beta2, grad_scale;  // the 32-bit arguments, widened

@@ -364,7 +364,7 @@ hipError_t in_groups(const rc_adamw_tensor* ts, int n, int chunk, Args& a, Set s
     for (; at < n && a.n < MAX; ++at) {
       if (ts[at].count == 0) continue;
       const long own = (ts[at].count + chunk - 1) / chunk;
-      if (a.n && chunks + own > 0x7fffffffL) break;
+      if (a.n && chunks + own > ADAMW_MAX_GROUPS) break;
       Tensor& t = a.t[a.n++];
       t = set(ts[at], at);
       t.n = ts[at].count;

@@ -7,6 +7,9 @@
 
 #include "recycle_stage.h"
 
+// A launch holds fewer than 2^32 threads: workgroups of 256.
+constexpr long ATTN_OP_MAX_GROUPS = (1L << 24) - 1;
+
 // Distances in tokens at which the last bucket of a side has to begin at the latest.
 constexpr int ATTN_OP_MAX_FAR = 1024;
 constexpr int ATTN_OP_MAX_BUCKETS = 128;

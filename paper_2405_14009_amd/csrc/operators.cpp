@@ -50,9 +50,10 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   a.buckets = c.buckets;
   a.bias_f32 = c.bias_dtype == RC_FP32;
   attn_op_plan(a, c.window, c.max_distance);
-  const long units = ((long)a.s + 127) / 128 + (long)a.sink_rows / 32 * a.chunks;
-  if (units * a.batch > 0x7fffffffL / a.heads)
-    return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks of 128 tokens");
+  // workgroups a batch and head: of the kernels over queries, over keys, and over the sinks' rows
+  const long units = std::max((a.s + 127) / 128 + (long)a.sink_rows / 32 * a.chunks, (std::min(a.sinks, a.s) + 7L) / 8);
+  if (units * a.batch > (ATTN_OP_MAX_GROUPS - a.heads) / a.heads)
+    return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^24 - 1 blocks of 128 tokens of a head");
   return RC_OK;
 }
 
@@ -140,8 +141,6 @@ rc_status bias_args(const rc_attention* c, const void* bias, const int32_t* leng
   a.lengths = lengths;
   return RC_OK;
 }
-
-constexpr int64_t kMaxCount = (int64_t)1 << 40;
 
 rc_status moment_args(const rc_adamw_tensor& t, int state_bits, const std::string& name) {
   if (!t.exp_avg || !t.exp_avg_sq) return fail(RC_ERR_INVALID_ARG, name + "null array");
@@ -234,7 +233,7 @@ rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam
     for (int i = 0; i < n; ++i) {
       const rc_adamw_tensor& t = tensors[i];
       const std::string name = "tensor " + std::to_string(i) + ": ";
-      if (t.count < 0 || t.count > kMaxCount) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
+      if (t.count < 0 || t.count > ADAMW_MAX_COUNT) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
       if (t.grad_dtype != RC_FP32 && t.grad_dtype != RC_BF16)
         return fail(RC_ERR_INVALID_ARG, name + "unknown grad_dtype");
       if (t.count == 0) continue;
@@ -259,7 +258,7 @@ rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state
     for (int i = 0; i < n; ++i) {
       const rc_adamw_tensor& t = tensors[i];
       const std::string name = "tensor " + std::to_string(i) + ": ";
-      if (t.count < 0 || t.count > kMaxCount) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
+      if (t.count < 0 || t.count > ADAMW_MAX_COUNT) return fail(RC_ERR_INVALID_ARG, name + "count out of range");
       if (t.count == 0) continue;
       TRY(moment_args(t, state_bits, name));
       if (!exp_avg[i] || !exp_avg_sq[i] || ((uintptr_t)exp_avg[i] | (uintptr_t)exp_avg_sq[i]) % 4)

@@ -247,9 +247,6 @@ class AdamW:
                                  f"{' or '.join(str(x) for x in types)}")
             return t.data_ptr()
 
-        used = [p.data_ptr() for p in self.params if p.numel()]
-        if len(set(used)) != len(used):
-            raise ValueError("a parameter is listed twice")
         if len(self.decay) != n or len(self.copies) != n or len(self.grads) != n:
             raise ValueError(f"grads, decay and copies must have {n} entries")
         self._tensors = (L.RcAdamwTensor * max(1, n))()
@@ -267,6 +264,18 @@ class AdamW:
                 t.copy = pointer(self.copies, i, "copies", (bf16,), count)
             t.count, t.decay = count, self.decay[i]
             t.grad_dtype = L.RC_BF16 if self.grads[i].dtype == bf16 else L.RC_FP32
+        written = (self.params, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale or (), self.exp_avg_sq_scale or (),
+                   self.copies)
+        # (first byte, byte behind the last one, whether a step writes them)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w)
+                       for w, lists in ((True, written), (False, (self.grads,)))
+                       for tensors in lists for t in tensors if t is not None and t.numel())
+        end, write_end = 0, 0
+        for first, last, w in spans:
+            if first < (end if w else write_end):
+                raise ValueError("a tensor that a step writes is listed twice or overlaps another one")
+            end = max(end, last)
+            write_end = max(write_end, last) if w else write_end
 
     def step(self, grad_scale: float = 1.0, *, step: Optional[int] = None) -> None:
         """One step with grad_scale * grads, as step number `step` (by default one

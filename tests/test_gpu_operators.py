@@ -478,3 +478,54 @@ def test_moments_as_values(bits, offset):
     for i, (_, wm, wv) in enumerate(state(opt)):
         assert np.array_equal(m[i].cpu().numpy(), wm.astype(np.float32)), i
         assert np.array_equal(v[i].cpu().numpy(), wv.astype(np.float32)), i
+
+
+def test_refusals_of_the_python_calls():
+    """What the wrappers refuse before the library sees it; nothing is enqueued."""
+    pkg = ops()
+    q, k = torch.zeros(2, 40, 4, 64, device="cuda"), torch.zeros(2, 40, 2, 64, device="cuda")
+    o, saved = pkg.attention_forward(q, k, k)
+    bias = torch.zeros(4, 16, device="cuda")
+    for error, call in (
+            (TypeError, lambda: pkg.attention_forward(q.cpu(), k, k)),
+            (ValueError, lambda: pkg.attention_forward(q.half(), k.half(), k.half())),
+            (ValueError, lambda: pkg.attention_forward(q[0], k, k)),
+            (ValueError, lambda: pkg.attention_forward(q, k[:, :39], k)),
+            (ValueError, lambda: pkg.attention_forward(q, k, k.bfloat16())),
+            (ValueError, lambda: pkg.attention_forward(q, k, k.transpose(2, 3).contiguous().transpose(2, 3))),
+            (ValueError, lambda: pkg.attention_forward(q, k, k, rel_bias=bias[:3])),
+            (ValueError, lambda: pkg.attention_forward(q, k, k, rel_bias=bias.t())),
+            (ValueError, lambda: pkg.attention_forward(q, k, k, rel_bias=bias.half())),
+            (ValueError, lambda: pkg.attention_forward(q, k, k, lengths=torch.zeros(2, device="cuda"))),
+            (TypeError, lambda: pkg.attention_forward(q, k, k, lengths=torch.zeros(2, dtype=torch.int32))),
+            (ValueError, lambda: pkg.attention_forward(q, k, k, out=o[:, :39])),
+            (pkg.InvalidArgError, lambda: pkg.attention_forward(q, k, k, out=q)),
+            (pkg.InvalidArgError, lambda: pkg.attention_forward(q, k, k, out=o[:, :1].expand(q.shape))),
+            (ValueError, lambda: pkg.attention_backward(o, q, k, k, o, saved[:-1])),
+            (ValueError, lambda: pkg.attention_backward(o, q, k, k, o, None)),
+            (pkg.InvalidArgError, lambda: pkg.attention_backward(o, q, k, k, o, saved, dq=q))):
+        with pytest.raises(error):
+            call()
+
+    x = torch.zeros(300, device="cuda")
+    p, g = x[:100], x[100:200]
+    half = torch.zeros(100, dtype=BF16, device="cuda")
+    for kw in (dict(params=[p, p], grads=[g, g]), dict(params=[p, x[50:150]], grads=[x[200:], x[200:]]),
+               dict(params=[p], grads=[p]), dict(params=[p], grads=[x[99:199]]),
+               dict(params=[p], grads=[g], exp_avg=[x[200:]], exp_avg_sq=[x[200:]]),
+               dict(params=[p, g], grads=[x[200:], x[200:]], copies=[half, half]),
+               dict(params=[p], grads=[g[:99]]), dict(params=[half], grads=[g]), dict(params=[p], grads=[]),
+               dict(params=[p], grads=[g], decay=[True, False]), dict(params=[p], grads=[g], state_bits=16),
+               dict(params=[p], grads=[g], exp_avg=[x[200:]]),
+               dict(params=[p], grads=[g], exp_avg=[x[200:]], exp_avg_sq=[x[200:]], state_bits=8)):
+        with pytest.raises(ValueError):
+            pkg.AdamW(**kw)
+    with pytest.raises(TypeError):
+        pkg.AdamW([p.cpu()], [g])
+    with pytest.raises(TypeError):
+        pkg.AdamW([p], [g.cpu()])
+    opt = pkg.AdamW([p, x[200:]], [g, g])          # one gradient for two parameters is read only
+    for out in ([[p], [p]], [[p, p[:99]], [p, p]], [[p, half], [p, p]]):
+        with pytest.raises(ValueError):
+            opt.moments(out)
+    assert float(x.abs().sum()) == 0.0

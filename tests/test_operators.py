@@ -76,6 +76,9 @@ BAD_ATTENTION = [
     (dict(head_dim=60), "UNSUPPORTED", b"head_dim"),
     (dict(head_dim=136), "UNSUPPORTED", b"head_dim"),
     (dict(seq_len=(1 << 24) + 1), "UNSUPPORTED", b"seq_len"),
+    (dict(seq_len=1, batch=1 << 24, heads=1, kv_heads=1), "UNSUPPORTED", b"blocks"),
+    (dict(seq_len=129, batch=1 << 20, heads=8, kv_heads=1), "UNSUPPORTED", b"blocks"),
+    (dict(seq_len=128, batch=1 << 20, heads=4, kv_heads=4, window=2, sinks=128), "UNSUPPORTED", b"blocks"),
     (dict(seq_len=1 << 24, batch=1 << 12, heads=8, kv_heads=8), "UNSUPPORTED", b"blocks"),
 ]
 
@@ -85,6 +88,10 @@ def test_attention_refusals(kw, status, word):
     L, lib = lib_or_skip()
     assert memory(**kw)[0] == getattr(L, "RC_ERR_" + status)
     assert word in lib.rc_last_error()
+
+
+def test_attention_takes_the_most_blocks_of_a_launch():
+    assert memory(seq_len=128, batch=(1 << 24) - 2, heads=1, kv_heads=1)[0] == 0
 
 
 def test_attention_refuses_tensors_before_any_device_work():
@@ -148,6 +155,7 @@ def test_adamw_refusals():
     bad = L.RC_ERR_INVALID_ARG
     for kw, word in ((dict(bits=16), b"state_bits"), (dict(number=0), b"step"), (dict(n=-1), b"negative"),
                      (dict(adam=None), b"null"), (dict(count=-1), b"count"), (dict(count=1 << 50), b"count"),
+                     (dict(count=(1 << 34) - 1023), b"count"),
                      (dict(grad_dtype=3), b"grad_dtype"), (dict(param=None), b"null"), (dict(exp_avg=None), b"null"),
                      (dict(bits=8), b"scales"), (dict(exp_avg_scale=64), b"scales"),
                      (dict(bits=8, exp_avg_scale=64), b"scales"), (dict(param=4098), b"aligned"),
