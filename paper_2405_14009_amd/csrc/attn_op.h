@@ -40,7 +40,7 @@ struct AttnOpArgs {
   float* bpart;  // [batch, heads, bias_blocks, buckets] shares of the bias gradient, by query block
   int bias_blocks;
   void* dbias;
-  // Grids of few blocks of 128 rows take 32 rows a workgroup instead, whose four
+  // fp32, and grids of few blocks of 128 rows, take 32 rows a workgroup instead, whose four
   // waves share the other side's blocks.
   int split_f, split_q, split_k;  // forward, dq, dk and dv
   // Every query sees the sinks.  Their keys (sink_rows: up to a multiple of 32)
@@ -61,7 +61,9 @@ ATTN_OP_DECL(bf16_32)
 ATTN_OP_DECL(bf16_64)
 ATTN_OP_DECL(bf16_96)
 ATTN_OP_DECL(bf16_128)
+ATTN_OP_DECL(f32_32)
 ATTN_OP_DECL(f32_64)
+ATTN_OP_DECL(f32_96)
 ATTN_OP_DECL(f32_128)
 #undef ATTN_OP_DECL
 
@@ -79,7 +81,7 @@ hipError_t attn_op_add_dbias(const AttnOpShares& shares, int n, long count, floa
 // pointers are set from `saved` (null: nothing is kept for a backward pass) and
 // `work`.
 size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt);
-size_t attn_op_work_bytes(const AttnOpArgs& a, int elt);
-void attn_op_plan(AttnOpArgs& a, int window, int max_distance);
+size_t attn_op_work_bytes(const AttnOpArgs& a);
+void attn_op_plan(AttnOpArgs& a, int elt, int window, int max_distance);
 hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st);
 hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work, hipStream_t st);

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256) void attn_op_add_dbias_k(AttnOpShares shares, 
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-int columns(int elt, int d) { return elt == 2 && d <= 32 ? 32 : d <= 64 ? 64 : elt == 2 && d <= 96 ? 96 : 128; }
+int columns(int d) { return (d + 31) / 32 * 32; }
 
 size_t rows(const AttnOpArgs& a) { return (size_t)a.batch * a.heads * a.spad; }
 
@@ -68,7 +68,7 @@ size_t bias_bytes(const AttnOpArgs& a) {
 }  // namespace
 
 // Fills what follows from the sizes: the window, buckets and the chunks of sink blocks.
-void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
+void attn_op_plan(AttnOpArgs& a, int elt, int window, int max_distance) {
   const int far = 1 << 30;
   a.spad = (a.s + 63) / 64 * 64;
   a.group = a.heads / a.kv_heads;
@@ -91,11 +91,13 @@ void attn_op_plan(AttnOpArgs& a, int window, int max_distance) {
     }
   }
   const long cus = device_compute_units(), blocks = (a.s + 31) / 32 * (long)a.batch;
-  a.split_q = blocks * a.heads <= cus;
-  a.split_f = blocks * a.heads <= 2 * cus;
-  a.split_k = blocks * a.kv_heads <= cus;
+  a.split_q = elt == 4 || blocks * a.heads <= cus;
+  a.split_f = elt == 4 || blocks * a.heads <= 2 * cus;
+  a.split_k = elt == 4 || blocks * a.kv_heads <= cus;
   a.sink_rows = (a.sinks + 31) / 32 * 32;
-  a.chunk_len = 512;
+  // (us of dk and dv: fp32, 4 sequences of 955, 16 / 4 heads of 96, window 6, 16 sinks: 185 by chunks
+  // of 512, 122 by 128; bf16, 2 sequences of 2048, 16 heads of 128, window 512: 72 and 79)
+  a.chunk_len = elt == 4 ? 128 : 512;
   while ((long)a.chunk_len * 64 < a.s) a.chunk_len *= 2;
   a.chunks = a.sinks && !(a.split_k && a.s <= a.chunk_len) ? sink_chunks(a) : 0;
 }
@@ -104,10 +106,10 @@ size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
   return 2 * align256(4 * rows(a)) + (elt == 2 ? align256(2 * (size_t)a.batch * a.s * a.heads * a.d) : 0);
 }
 
-size_t attn_op_work_bytes(const AttnOpArgs& a, int elt) {
+size_t attn_op_work_bytes(const AttnOpArgs& a) {
   return align256(4 * rows(a)) + bias_bytes(a) +
          align256(4 * (size_t)a.batch * a.kv_heads * (a.sinks ? 1 + sink_chunks(a) : 0) * 2 * a.sink_rows *
-                  columns(elt, a.d));
+                  columns(a.d));
 }
 
 namespace {
@@ -126,8 +128,12 @@ void set_saved(AttnOpArgs& a, const void* saved) {
 
 hipError_t attn_op_forward(AttnOpArgs a, int elt, void* saved, hipStream_t st) {
   set_saved(a, saved);
-  const int c = columns(elt, a.d);
-  if (elt == 4) return c == 64 ? attn_op_fwd_f32_64(a, st) : attn_op_fwd_f32_128(a, st);
+  const int c = columns(a.d);
+  if (elt == 4)
+    return c == 32   ? attn_op_fwd_f32_32(a, st)
+           : c == 64 ? attn_op_fwd_f32_64(a, st)
+           : c == 96 ? attn_op_fwd_f32_96(a, st)
+                     : attn_op_fwd_f32_128(a, st);
   return c == 32   ? attn_op_fwd_bf16_32(a, st)
          : c == 64 ? attn_op_fwd_bf16_64(a, st)
          : c == 96 ? attn_op_fwd_bf16_96(a, st)
@@ -142,8 +148,12 @@ hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work
   a.bpart = (float*)w;
   w += bias_bytes(a);
   a.spart = (float*)w;
-  const int c = columns(elt, a.d);
-  if (elt == 4) return c == 64 ? attn_op_bwd_f32_64(a, st) : attn_op_bwd_f32_128(a, st);
+  const int c = columns(a.d);
+  if (elt == 4)
+    return c == 32   ? attn_op_bwd_f32_32(a, st)
+           : c == 64 ? attn_op_bwd_f32_64(a, st)
+           : c == 96 ? attn_op_bwd_f32_96(a, st)
+                     : attn_op_bwd_f32_128(a, st);
   return c == 32   ? attn_op_bwd_bf16_32(a, st)
          : c == 64 ? attn_op_bwd_bf16_64(a, st)
          : c == 96 ? attn_op_bwd_bf16_96(a, st)

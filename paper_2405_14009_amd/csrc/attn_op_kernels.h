@@ -45,9 +45,10 @@ struct TileB16 {
   using E = bf16;
   using A = Attn<HD_, false>;
   static constexpr int HD = HD_, TILE = A::TILE64;
-  static constexpr bool ASYNC = true, REST = true;
+  static constexpr bool DIRECT = false, REST = true;
   // waves a SIMD of the kernels over queries and keys
   static constexpr int WAVES = 2, KWAVES = HD > 96 ? 1 : 2;
+  static constexpr int FWAVES = 1, QWAVES = 1, DWAVES = 1;  // of the kernels of 32 rows, at least
   using Rows = bf16x8[HD / 16];
   struct Offs {
     typename A::RowOffs ro;
@@ -68,7 +69,10 @@ struct TileB16 {
   static __device__ __forceinline__ void copy(char* tile, const Src& s, int wave, int lane, int row0, int nrows, int d) {
     A::template load_tile<64>(s.rs, tile, wave, lane, s.ld, row0, nrows, d);
   }
-  // 32 rows by one wave alone
+  // 32 rows by one wave alone into an area of its own (OWN bytes), and what the products read of them
+  static constexpr int OWN = TILE / 2;
+  using Block = const char*;
+  static __device__ __forceinline__ Block block(const Src&, const char* own, int, int, int) { return own; }
   static __device__ __forceinline__ void copy_own(char* tile, const Src& s, int lane, int row0, int nrows, int d) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) A::template load_tile<32>(s.rs, tile, v, lane, s.ld, row0, nrows, d);
@@ -79,6 +83,7 @@ struct TileB16 {
   static __device__ __forceinline__ void vec(char* dst, const float* src, int lane, int n = 64) {
     A::load_vec64(make_rsrc(src, 4 * n), dst, lane, 0, n);
   }
+  static __device__ __forceinline__ const float* vec_of(const char* own, const float*) { return (const float*)own; }
   static __device__ __forceinline__ void rows(Rows& f, const E* base, long ld, int row, int nrows, int lane, int d) {
     A::load_stationary(f, base, ld, row, nrows, lane, d);
   }
@@ -128,13 +133,23 @@ struct TileB16 {
   }
 };
 
+// fp32: no tiles.  A matrix instruction of 32x32x2 takes 64 cycles for the 4 bytes a
+// lane of either operand, so the products read theirs from the caches as they go;
+// no barrier ties the waves of a workgroup, and with 32 rows a workgroup (the only
+// form) what no pair of a block of 32 x 32 needs is not computed.  us of a training
+// step (tiles of 64 rows in LDS, 128 rows a workgroup, against this): 4 sequences
+// of 955, 16 / 4 heads of 96, window 6, 16 sinks: 528, 274; 2 of 814, 11 heads of 128,
+// both directions, a bias: 774, 562 (matrix instructions run in 58 % of the
+// cycles of the busy compute units; most of the rest is vector work next to one wave a SIMD and
+// the ends of the workgroups).
 template <int HD_>
 struct TileF32 {
   using E = float;
-  static constexpr int HD = HD_, LD = HD + 8, TILE = 64 * LD * 4;
-  static constexpr bool ASYNC = false, REST = false;
-  static constexpr int WAVES = HD > 64 ? 1 : 2, KWAVES = 1;
-  // the halves of a wave hold half of the columns each
+  static constexpr int HD = HD_;
+  static constexpr bool DIRECT = true, REST = false;
+  static constexpr int OWN = 0;
+  static constexpr int FWAVES = 2, QWAVES = HD > 96 ? 1 : 2, DWAVES = HD > 64 ? 1 : 2;
+  // of every 8 columns the halves of a wave hold 4 each
   using Rows = float[HD / 2];
   struct Offs {
     __device__ __forceinline__ void init(int) {}
@@ -147,33 +162,33 @@ struct TileF32 {
       ld = ld_;
     }
   };
-  static __device__ __forceinline__ void copy(char* tile, const Src& s, int wave, int lane, int row0, int nrows, int d) {
-    for (int i = wave * 64 + lane; i < 64 * (HD / 4); i += 256) {
-      const int r = i / (HD / 4), c = 4 * (i % (HD / 4));
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row0 + r < nrows && c < d) v = *(const float4*)(s.p + (long)(row0 + r) * s.ld + c);
-      *(float4*)((float*)tile + r * LD + c) = v;
+  // 32 rows: rows behind the last one and columns behind the head stand for
+  // others of the tensor, whose products meet zeros or are not stored.
+  struct Block {
+    const char* p;  // first row
+    unsigned ld;    // bytes
+    int last, d;
+    __device__ __forceinline__ float4 row4(int lane, int i) const {
+      const char* const at = p + 32 * min(i, d / 8 - 1);
+      return *(const float4*)(at + (min(lane & 31, last) * ld + 16u * (lane >> 5)));
     }
-  }
-  static __device__ __forceinline__ void copy_own(char* tile, const Src& s, int lane, int row0, int nrows, int d) {
-#pragma unroll
-    for (int n = 0; n < HD / 8; ++n) {
-      const int i = 64 * n + lane, r = i / (HD / 4), c = 4 * (i % (HD / 4));
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (row0 + r < nrows && c < d) v = *(const float4*)(s.p + (long)(row0 + r) * s.ld + c);
-      *(float4*)((float*)tile + r * LD + c) = v;
+    __device__ __forceinline__ float at(int lane, int r, int b) const {
+      const unsigned c = min(32 * b + (lane & 31), d - 1);
+      return *(const float*)(p + (min(4 * (lane >> 5) + row_of(r), last) * ld + 4 * c));
     }
+  };
+  static __device__ __forceinline__ Block block(const Src& s, const char*, int row0, int nrows, int d) {
+    return {(const char*)(s.p + (long)row0 * s.ld), (unsigned)(4 * s.ld), nrows - 1 - row0, d};
   }
-  // (one wave's LDS accesses complete in order)
-  static __device__ __forceinline__ void own_landed() { asm volatile("" ::: "memory"); }
-  static __device__ __forceinline__ void own_read() { asm volatile("" ::: "memory"); }
-  static __device__ __forceinline__ void vec(char* dst, const float* src, int lane, int n = 64) {
-    if (lane < n) ((float*)dst)[lane] = src[lane];
-  }
+  static __device__ __forceinline__ void copy_own(char*, const Src&, int, int, int, int) {}
+  static __device__ __forceinline__ void own_landed() {}
+  static __device__ __forceinline__ void own_read() {}
+  static __device__ __forceinline__ void vec(char*, const float*, int, int) {}
+  static __device__ __forceinline__ const float* vec_of(const char*, const float* src) { return src; }
   static __device__ __forceinline__ void rows(Rows& f, const E* base, long ld, int row, int nrows, int lane, int d) {
 #pragma unroll
     for (int k = 0; k < HD / 2; k += 4) {
-      const int c = (lane >> 5) * (HD / 2) + k;
+      const int c = 2 * k + 4 * (lane >> 5);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (row < nrows && c < d) v = *(const float4*)(base + (long)row * ld + c);
       f[k] = v.x;
@@ -185,46 +200,50 @@ struct TileF32 {
   static __device__ __forceinline__ f32x16 mfma(float a, float b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
   }
-  static __device__ __forceinline__ void score2(f32x16& a0, const char* t0, int b0, const Rows& s0, f32x16& a1,
-                                                const char* t1, int b1, const Rows& s1, const Offs&, int lane) {
-    const float* x = (const float*)t0 + (32 * b0 + (lane & 31)) * LD + (lane >> 5) * (HD / 2);
-    const float* y = (const float*)t1 + (32 * b1 + (lane & 31)) * LD + (lane >> 5) * (HD / 2);
+  static __device__ __forceinline__ void mfma4(f32x16& a, const float4& u, const float* s) {
+    a = mfma(u.x, s[0], a);
+    a = mfma(u.y, s[1], a);
+    a = mfma(u.z, s[2], a);
+    a = mfma(u.w, s[3], a);
+  }
+  // Loads run AHEAD of the products that take them (the compiler, left to itself,
+  // issues each just before).
+  static constexpr int AHEAD = HD / 8 < 4 ? HD / 8 : 4;
+  static __device__ __forceinline__ void score1(f32x16& a, const Block& t, const Rows& s, const Offs&, int lane) {
+    float4 u[AHEAD];
 #pragma unroll
-    for (int k = 0; k < HD / 2; k += 4) {
-      const float4 u = *(const float4*)(x + k), w = *(const float4*)(y + k);
-      a0 = mfma(u.x, s0[k], a0);
-      a1 = mfma(w.x, s1[k], a1);
-      a0 = mfma(u.y, s0[k + 1], a0);
-      a1 = mfma(w.y, s1[k + 1], a1);
-      a0 = mfma(u.z, s0[k + 2], a0);
-      a1 = mfma(w.z, s1[k + 2], a1);
-      a0 = mfma(u.w, s0[k + 3], a0);
-      a1 = mfma(w.w, s1[k + 3], a1);
+    for (int i = 0; i < AHEAD; ++i) u[i] = t.row4(lane, i);
+#pragma unroll
+    for (int i = 0; i < HD / 8; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      const float4 x = u[i % AHEAD];
+      if (i + AHEAD < HD / 8) u[i % AHEAD] = t.row4(lane, i + AHEAD);
+      mfma4(a, x, s + 4 * i);
     }
   }
-  static __device__ __forceinline__ void score1(f32x16& a, const char* t, const Rows& s, const Offs&, int lane) {
-    const float* x = (const float*)t + (lane & 31) * LD + (lane >> 5) * (HD / 2);
-#pragma unroll
-    for (int k = 0; k < HD / 2; k += 4) {
-      const float4 u = *(const float4*)(x + k);
-      a = mfma(u.x, s[k], a);
-      a = mfma(u.y, s[k + 1], a);
-      a = mfma(u.z, s[k + 2], a);
-      a = mfma(u.w, s[k + 3], a);
-    }
+  static __device__ __forceinline__ void score2(f32x16& a0, const Block& t0, int, const Rows& s0, f32x16& a1,
+                                                const Block& t1, int, const Rows& s1, const Offs& o, int lane) {
+    score1(a0, t0, s0, o, lane);
+    score1(a1, t1, s1, o, lane);
   }
   static __device__ __forceinline__ void dot(f32x16& a, const Rows& x, const Rows& y) {
 #pragma unroll
     for (int k = 0; k < HD / 2; ++k) a = mfma(x[k], y[k], a);
   }
   template <bool>
-  static __device__ __forceinline__ void outer(f32x16 (&acc)[HD / 32], const char* tile, int j, const f32x16& p,
-                                               const Offs&, int lane) {
-    const float* x = (const float*)tile + (32 * j + 4 * (lane >> 5)) * LD + (lane & 31);
+  static __device__ __forceinline__ void outer(f32x16 (&acc)[HD / 32], const Block& t, int, const f32x16& p, const Offs&,
+                                               int lane) {
+    constexpr int NB = HD / 32, N = 16 * NB, A = 16;
+    float u[A];
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int i = 0; i < A; ++i) u[i] = t.at(lane, i / NB, i % NB);
 #pragma unroll
-      for (int b = 0; b < HD / 32; ++b) acc[b] = mfma(x[row_of(r) * LD + 32 * b], p[r], acc[b]);
+    for (int i = 0; i < N; ++i) {
+      if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+      const float x = u[i % A];
+      if (i + A < N) u[i % A] = t.at(lane, (i + A) / NB, (i + A) % NB);
+      acc[i % NB] = mfma(x, p[i / NB], acc[i % NB]);
+    }
   }
   static __device__ __forceinline__ void store_cols(const f32x16& acc, E* base, long ld, int row0, int nrows, int b,
                                                     int lane, float mul, int d) {
@@ -237,11 +256,6 @@ struct TileF32 {
         *(float4*)(p + 8 * g) =
             make_float4(acc[4 * g] * mul, acc[4 * g + 1] * mul, acc[4 * g + 2] * mul, acc[4 * g + 3] * mul);
   }
-  static __device__ __forceinline__ void store(const f32x16 (&acc)[HD / 32], char*, E* base, long ld, int row0,
-                                               int nrows, int lane, float mul, int d) {
-#pragma unroll
-    for (int b = 0; b < HD / 32; ++b) store_cols(acc[b], base, ld, row0, nrows, b, lane, mul, d);
-  }
 };
 
 template <class T, bool BIAS>
@@ -250,7 +264,8 @@ struct AttnOp {
   using Rows = typename T::Rows;
   using Offs = typename T::Offs;
   using Src = typename T::Src;
-  static constexpr int HD = T::HD, NB = HD / 32, TILE = T::TILE;
+  using Block = typename T::Block;
+  static constexpr int HD = T::HD, NB = HD / 32;
   static constexpr float kNone = -3.402823466e38f;
 
   static __device__ __forceinline__ void zero(f32x16& a) {
@@ -445,25 +460,14 @@ struct AttnOp {
     }
   }
   // body(stage, it) for n steps, whose operands issue(stage, it) copies: the next
-  // step's while this one computes, or (copies through registers) its own.  The
-  // caller has issued step 0 in the first case.
-  static constexpr int STAGES = T::ASYNC ? 2 : 1;
+  // step's while this one computes.  The caller has issued step 0.
   template <class Issue, class Body>
   static __device__ __forceinline__ void pipeline(int n, char* lds, int stage, Issue issue, Body body) {
     stage_sync();
-    if constexpr (T::ASYNC) {
-      for (int it = 0; it < n; ++it) {
-        if (it + 1 < n) issue(lds + (~it & 1) * stage, it + 1);
-        body(lds + (it & 1) * stage, it);
-        stage_sync();
-      }
-    } else {
-      for (int it = 0; it < n; ++it) {
-        issue(lds, it);
-        stage_sync();
-        body(lds, it);
-        __syncthreads();
-      }
+    for (int it = 0; it < n; ++it) {
+      if (it + 1 < n) issue(lds + (~it & 1) * stage, it + 1);
+      body(lds + (it & 1) * stage, it);
+      stage_sync();
     }
   }
 
@@ -547,11 +551,11 @@ struct AttnOp {
     T::template outer<FINE>(st.o, vt, 1, sc[1], of, lane);
   }
 
-  static constexpr int STAGE = 2 * TILE;
+  static constexpr int TILE = 2 * T::OWN, STAGE = 2 * TILE;
 
   template <bool FINE>
   static __device__ __forceinline__ void fwd(const AttnOpArgs& p, char* lds) {
-    float* const table = (float*)(lds + STAGES * STAGE);
+    float* const table = (float*)(lds + 2 * STAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bh = p.batch * p.heads, nqb = (p.s + 127) / 128;
@@ -568,7 +572,7 @@ struct AttnOp {
       T::copy(t, ks, wave, lane, k0, len, p.d);
       T::copy(t + TILE, vs, wave, lane, k0, len, p.d);
     };
-    if (T::ASYNC && steps.n > 0) issue(lds, 0);
+    if (steps.n > 0) issue(lds, 0);
     Rows qf;
     T::rows(qf, base(p.q, b, h), p.q.t, qq, len, lane, p.d);
     if constexpr (BIAS) fill_table(p, h, table);
@@ -583,9 +587,8 @@ struct AttnOp {
   }
 
   // 32 queries a workgroup: its waves take every fourth block of 32 keys, with
-  // tiles of their own, and join their sums through LDS.
-  static constexpr int OWN = 2 * (TILE / 2);
-  static_assert(NB * 4096 <= OWN, "a wave's sums in its tiles");
+  // tiles of their own (or none), and join their sums through LDS.
+  static constexpr int SUMS = NB * 4096, OWN = 2 * T::OWN > SUMS ? 2 * T::OWN : SUMS;
   template <bool FINE>
   static __device__ __forceinline__ void fwd32(const AttnOpArgs& p, char* lds) {
     const int lane = threadIdx.x & 63;
@@ -604,7 +607,7 @@ struct AttnOp {
     auto issue = [&](int it) {
       const int k0 = steps.tile(it) * 32;
       T::copy_own(own, ks, lane, k0, len, p.d);
-      T::copy_own(own + TILE / 2, vs, lane, k0, len, p.d);
+      T::copy_own(own + T::OWN, vs, lane, k0, len, p.d);
     };
     if (wave < steps.n) issue(wave);
     Rows qf;
@@ -623,9 +626,10 @@ struct AttnOp {
       if (!none_visible<32>(p, q0, k0, len)) {
         f32x16 sc[1];
         zero(sc[0]);
-        T::score1(sc[0], own, qf, of, lane);
+        T::score1(sc[0], T::block(ks, own, k0, len, p.d), qf, of, lane);
+        const Block vb = T::block(vs, own + T::OWN, k0, len, p.d);
         softmax<1>(st, sc, k0, q0, qq, lane, len, table, p);
-        T::template outer<FINE>(st.o, own + TILE / 2, 0, sc[0], of, lane);
+        T::template outer<FINE>(st.o, vb, 0, sc[0], of, lane);
       }
       T::own_read();
       if (it + 4 < steps.n) issue(it + 4);
@@ -810,7 +814,7 @@ struct AttnOp {
   // rows of few tokens): with what the rounding of dS drops, which there costs little
   // and is not averaged over a row.
   template <bool FINE>
-  static __device__ __forceinline__ void dq_block(f32x16 (&acc)[NB], const Queries& w, const char* kt, const char* vt,
+  static __device__ __forceinline__ void dq_block(f32x16 (&acc)[NB], const Queries& w, const Block& kt, const Block& vt,
                                                   int j, const Offs& of, int k, int q0, int qq, int lane, int len,
                                                   const float* table, Sums& sums, const AttnOpArgs& p) {
     if (none_visible<32>(p, q0, k, len)) return;
@@ -848,7 +852,7 @@ struct AttnOp {
   }
 
   static __device__ __forceinline__ void dq(const AttnOpArgs& p, char* lds) {
-    float* const table = (float*)(lds + STAGES * STAGE);
+    float* const table = (float*)(lds + 2 * STAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bh = p.batch * p.heads, nqb = (p.s + 127) / 128;
@@ -865,7 +869,7 @@ struct AttnOp {
       T::copy(t, ks, wave, lane, k0, len, p.d);
       T::copy(t + TILE, vs, wave, lane, k0, len, p.d);
     };
-    if (T::ASYNC && steps.n > 0) issue(lds, 0);
+    if (steps.n > 0) issue(lds, 0);
     Queries w;
     load_queries(w, p, b, h, qq, len, lane, true);
     Sums sums = {nullptr, 0.f, 0.f};
@@ -910,7 +914,7 @@ struct AttnOp {
     auto issue = [&](int it) {
       const int k0 = steps.tile(it) * 32;
       T::copy_own(own, ks, lane, k0, len, p.d);
-      T::copy_own(own + TILE / 2, vs, lane, k0, len, p.d);
+      T::copy_own(own + T::OWN, vs, lane, k0, len, p.d);
     };
     if (wave < steps.n) issue(wave);
     Queries w;
@@ -928,7 +932,9 @@ struct AttnOp {
     }
     for (int it = wave; it < steps.n; it += 4) {
       T::own_landed();
-      dq_block<FINE>(acc, w, own, own + TILE / 2, 0, of, steps.tile(it) * 32, q0, qq, lane, len, table, sums, p);
+      const int k0 = steps.tile(it) * 32;
+      dq_block<FINE>(acc, w, T::block(ks, own, k0, len, p.d), T::block(vs, own + T::OWN, k0, len, p.d), 0, of, k0, q0, qq,
+                     lane, len, table, sums, p);
       T::own_read();
       if (it + 4 < steps.n) issue(it + 4);
     }
@@ -962,7 +968,7 @@ struct AttnOp {
   // dk, dv += the 32 queries from q (rows j of the tiles), with their statistics.
   template <int MODE, bool FINE>
   static __device__ __forceinline__ void dkv_block(f32x16 (&dk)[NB], f32x16 (&dv)[NB], const Rows& kf, const Rows& vf,
-                                                   const char* qt, const char* dt, int j, const float* m, const float* l,
+                                                   const Block& qt, const Block& dt, int j, const float* m, const float* l,
                                                    const float* D, const Offs& of, int q, int k0, int kk, int lane,
                                                    int len, const float* table, const AttnOpArgs& p) {
     if (none_of<MODE>(p, q, k0, len)) return;
@@ -1041,7 +1047,7 @@ struct AttnOp {
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
     if (kb >= nkb) return dkv32<SINK, false>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
-    float* const table = (float*)(lds + STAGES * KSTAGE);
+    float* const table = (float*)(lds + 2 * KSTAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = z / p.kv_heads, hk = z % p.kv_heads;
@@ -1068,7 +1074,7 @@ struct AttnOp {
                (wave == 0 ? p.m : wave == 1 ? p.l : p.drow) + ((long)b * p.heads + h) * p.spad + row0, lane);
       if (++ti == nt) ti = 0, ++gi;
     };
-    if (T::ASYNC && nt > 0) issue(lds, 0);
+    if (nt > 0) issue(lds, 0);
     Rows kf, vf;
     T::rows(kf, base(p.k, b, hk), p.k.t, kk, len, lane, p.d);
     T::rows(vf, base(p.v, b, hk), p.v.t, kk, len, lane, p.d);
@@ -1117,7 +1123,7 @@ struct AttnOp {
   // 32 keys a workgroup: its waves take every fourth block of 32 queries, of
   // every head of the group, with tiles of their own.  MODE SINK: the sinks among
   // the keys, for the queries of a chunk that see them as such.
-  static constexpr int KOWN = OWN + 3072;
+  static constexpr int KOWN = OWN + (T::DIRECT ? 0 : 3072);
   template <int MODE, bool FINE>
   static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk) {
     const int lane = threadIdx.x & 63;
@@ -1160,7 +1166,7 @@ struct AttnOp {
       auto issue = [&](int it) {
         const int row0 = (t0 + it) * 32;
         T::copy_own(own, qs, lane, row0, len, p.d);
-        T::copy_own(own + TILE / 2, ds, lane, row0, len, p.d);
+        T::copy_own(own + T::OWN, ds, lane, row0, len, p.d);
         T::vec(own + OWN, p.m + rows + row0, lane, 32);
         T::vec(own + OWN + 1024, p.l + rows + row0, lane, 32);
         T::vec(own + OWN + 2048, p.drow + rows + row0, lane, 32);
@@ -1171,11 +1177,12 @@ struct AttnOp {
         fill_table(p, h, table);
         __syncthreads();
       }
-      const float* vec = (const float*)(own + OWN);
       for (int it = wave; it < nt; it += 4) {
         T::own_landed();
-        dkv_block<MODE, FINE>(dk, dv, kf, vf, own, own + TILE / 2, 0, vec, vec + 256, vec + 512, of, (t0 + it) * 32,
-                              k0, kk, lane, len, table, p);
+        const int row0 = (t0 + it) * 32;
+        dkv_block<MODE, FINE>(dk, dv, kf, vf, T::block(qs, own, row0, len, p.d), T::block(ds, own + T::OWN, row0, len, p.d),
+                              0, T::vec_of(own + OWN, p.m + rows + row0), T::vec_of(own + OWN + 1024, p.l + rows + row0),
+                              T::vec_of(own + OWN + 2048, p.drow + rows + row0), of, row0, k0, kk, lane, len, table, p);
         T::own_read();
         if (it + 4 < nt) issue(it + 4);
       }
@@ -1224,11 +1231,11 @@ struct AttnOp {
   // LDS of the kernels.
   static size_t table_bytes(const AttnOpArgs& a) { return BIAS ? 4 * (size_t)table_len(a) : 0; }
   static size_t fwd_lds(const AttnOpArgs& a, bool split) {
-    return (split ? 4 * OWN + 2048 : STAGES * STAGE) + table_bytes(a);
+    return (split ? 4 * OWN + 2048 : 2 * STAGE) + table_bytes(a);
   }
-  static size_t dq_lds(const AttnOpArgs& a, bool split) { return (split ? 4 * OWN : STAGES * STAGE) + 5 * table_bytes(a); }
+  static size_t dq_lds(const AttnOpArgs& a, bool split) { return (split ? 4 * OWN : 2 * STAGE) + 5 * table_bytes(a); }
   static size_t dkv_lds(const AttnOpArgs& a, bool split) {
-    const size_t both = 4 * KOWN, whole = STAGES * KSTAGE;
+    const size_t both = 4 * KOWN, whole = 2 * KSTAGE;
     return (split ? both : a.chunks && both > whole ? both : whole) + table_bytes(a);
   }
 };
@@ -1271,7 +1278,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T
   AttnOp<T, BIAS>::template fwd<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS, bool FINE>
-__global__ __launch_bounds__(256) void attn_op_fwd32_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::FWAVES))) void attn_op_fwd32_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::template fwd32<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS>
@@ -1280,7 +1287,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T
   AttnOp<T, BIAS>::dq(p, attn_op_lds);
 }
 template <class T, bool BIAS, bool FINE>
-__global__ __launch_bounds__(256) void attn_op_dq32_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::QWAVES))) void attn_op_dq32_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::template dq32<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS>
@@ -1288,7 +1295,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::KWAVES, 
   AttnOp<T, BIAS>::dkv(p, attn_op_lds);
 }
 template <class T, bool BIAS, bool FINE>
-__global__ __launch_bounds__(256) void attn_op_dkv32_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::DWAVES))) void attn_op_dkv32_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::template dkv_split<FINE>(p, attn_op_lds);
 }
 
@@ -1302,14 +1309,15 @@ constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 192);
 template <class T, bool BIAS, bool FINE>
 hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
   using K = AttnOp<T, BIAS>;
-  static_assert(4 * K::OWN + 2048 + kTableMost <= kLds && K::STAGES * K::STAGE + 5 * kTableMost <= kLds &&
-                    4 * K::KOWN + kTableMost <= kLds && K::STAGES * K::KSTAGE + kTableMost <= kLds,
+  static_assert(4 * K::OWN + 5 * kTableMost <= kLds && 2 * K::STAGE + 5 * kTableMost <= kLds &&
+                    4 * K::KOWN + kTableMost <= kLds && 2 * K::KSTAGE + kTableMost <= kLds,
                 "LDS at the largest table");
-  const long rows = a.split_f ? 32 : 128;
+  const bool split = T::DIRECT || a.split_f;
+  const long rows = split ? 32 : 128;
   const dim3 grid((unsigned)((a.s + rows - 1) / rows * a.batch * a.heads));
-  if (a.split_f)
+  if (split)
     hipLaunchKernelGGL((attn_op_fwd32_k<T, BIAS, FINE>), grid, dim3(256), K::fwd_lds(a, true), st, a);
-  else
+  else if constexpr (!T::DIRECT)
     hipLaunchKernelGGL((attn_op_fwd_k<T, BIAS, FINE>), grid, dim3(256), K::fwd_lds(a, false), st, a);
   return hipGetLastError();
 }
@@ -1318,8 +1326,7 @@ template <class T, bool BIAS>
 hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
   AttnOpArgs a = args;
   using K = AttnOp<T, BIAS>;
-  // (the one form that does not always fit: five tables of a far bias next to the tiles of fp32 heads of 128)
-  const bool sq = a.split_q && K::dq_lds(a, true) <= kLds, sk = a.split_k;
+  const bool sq = T::DIRECT || a.split_q, sk = T::DIRECT || a.split_k;
   const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
   const dim3 gq((unsigned)(nq * a.batch * a.heads));
   const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
@@ -1329,7 +1336,7 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
     hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, T::REST>), gq, dim3(256), K::dq_lds(a, true), st, a);
   else if (sq)
     hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, false>), gq, dim3(256), K::dq_lds(a, true), st, a);
-  else
+  else if constexpr (!T::DIRECT)
     hipLaunchKernelGGL((attn_op_dq_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, false), st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -1337,7 +1344,7 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
     hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, T::REST>), gk, dim3(256), K::dkv_lds(a, true), st, a);
   else if (sk)
     hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, false>), gk, dim3(256), K::dkv_lds(a, true), st, a);
-  else
+  else if constexpr (!T::DIRECT)
     hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, false), st, a);
   e = hipGetLastError();
   if (e != hipSuccess || !a.chunks) return e;

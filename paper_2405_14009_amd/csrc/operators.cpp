@@ -49,7 +49,7 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   a.scale = c.scale;
   a.buckets = c.buckets;
   a.bias_f32 = c.bias_dtype == RC_FP32;
-  attn_op_plan(a, c.window, c.max_distance);
+  attn_op_plan(a, c.dtype == RC_FP32 ? 4 : 2, c.window, c.max_distance);
   // workgroups a batch and head: of the kernels over queries, over keys, and over the sinks' rows
   const long units = std::max((a.s + 127) / 128 + (long)a.sink_rows / 32 * a.chunks, (std::min(a.sinks, a.s) + 7L) / 8);
   if (units * a.batch > (ATTN_OP_MAX_GROUPS - a.heads) / a.heads)
@@ -111,6 +111,8 @@ rc_status view_args(const rc_view* v, const char* name, const rc_attention* c, i
     return fail(RC_ERR_INVALID_ARG, std::string(name) + ": negative stride");
   if (elt == 2 && v->token_stride > (0x7fffffffL / 2 - c->head_dim) / std::max(1, c->seq_len - 1))
     return fail(RC_ERR_UNSUPPORTED, std::string(name) + ": a head's tokens span 2^31 bytes or more");
+  if (elt == 4 && c->seq_len > 1 && v->token_stride >= 1L << 24)
+    return fail(RC_ERR_UNSUPPORTED, std::string(name) + ": a token_stride of 2^24 elements or more");
   if (output) {
     std::pair<int64_t, int64_t> dims[3] = {
         {v->batch_stride, c->batch}, {v->token_stride, c->seq_len}, {v->head_stride, heads}};
@@ -162,7 +164,7 @@ rc_status rc_attention_memory(const rc_attention* c, size_t* saved_bytes, size_t
     AttnOpArgs a;
     TRY(attention_args(c, a));
     *saved_bytes = attn_op_saved_bytes(a, elt_of(c->dtype));
-    *work_bytes = attn_op_work_bytes(a, elt_of(c->dtype));
+    *work_bytes = attn_op_work_bytes(a);
     return RC_OK;
   });
 }

@@ -293,7 +293,7 @@ rc_status make_layout(const rc_stage_config* c, Layout& y, const rc_stage_option
   y.off_S = take(y.flash || y.op ? 0 : ss * 4);
   y.off_dS = take(y.flash || y.op ? 0 : ss * E);
   y.off_dO = take(T * h * E);
-  y.off_dv = take(y.op ? attn_op_work_bytes(y.attn, y.elt) : y.flash ? rows * 4 : 0);
+  y.off_dv = take(y.op ? attn_op_work_bytes(y.attn) : y.flash ? rows * 4 : 0);
   y.off_check = take(8 * GRAD_CHECK_BLOCKS);
   // Logical stash bytes per micro-batch (tensor sizes, no alignment padding):
   // from F to B_input the forward-written part of the weight-pass slot (X, A,

@@ -135,6 +135,8 @@ def test_attention_refuses_tensors_before_any_device_work():
     assert forward(saved=128) == bad and b"256" in lib.rc_last_error()
     big = 8 * ((2 ** 31 // 2) // 299 // 8 + 1)
     assert forward(q=view(b=0, t=big)) == L.RC_ERR_UNSUPPORTED and b"2^31" in lib.rc_last_error()
+    f32 = config(dtype=L.RC_FP32)
+    assert forward(c=f32, q=view(b=0, t=1 << 24)) == L.RC_ERR_UNSUPPORTED and b"token_stride" in lib.rc_last_error()
     assert backward(dq=view(at)) == bad and b"inputs" in lib.rc_last_error()
     assert backward(dk=view(6 * at, b=300 * 128, t=128)) == bad and b"share" in lib.rc_last_error()
     assert backward(dq=view(4 * at, b=8)) == bad and b"overlap" in lib.rc_last_error()
