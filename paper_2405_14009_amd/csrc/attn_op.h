@@ -50,6 +50,10 @@ struct AttnOpArgs {
   // the sinks' own block visits every query.)
   float* spart;
   int sink_rows, chunks, chunk_len;
+  // The heads of a key head in `parts` workgroups of the dk and dv kernel where
+  // that has few: their shares [batch, kv_heads, parts, 2, part_rows, columns].
+  float* gpart;
+  int parts, part_rows;
   unsigned short first[ATTN_OP_MAX_BUCKETS];  // first distance of each bucket of a side
   unsigned char bucket[ATTN_OP_MAX_FAR];      // of distances below `far`, one side
 };

@@ -1,5 +1,6 @@
 // Host side of the attention operator: scratch memory, buckets, launches; and
 // the sum of several calls' bias gradients.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -65,6 +66,15 @@ size_t bias_bytes(const AttnOpArgs& a) {
   return align256(4 * (size_t)a.batch * a.heads * ((a.s + 31) / 32) * a.buckets);
 }
 
+size_t part_bytes(const AttnOpArgs& a) {
+  return a.parts > 1 ? align256(4 * (size_t)a.batch * a.kv_heads * a.parts * 2 * a.part_rows * columns(a.d)) : 0;
+}
+size_t sink_bytes(const AttnOpArgs& a) {
+  return a.sinks ? align256(4 * (size_t)a.batch * a.kv_heads * (1 + sink_chunks(a) * a.parts) * 2 * a.sink_rows *
+                            columns(a.d))
+                 : 0;
+}
+
 }  // namespace
 
 // Fills what follows from the sizes: the window, buckets and the chunks of sink blocks.
@@ -99,6 +109,20 @@ void attn_op_plan(AttnOpArgs& a, int elt, int window, int max_distance) {
   // of 512, 122 by 128; bf16, 2 sequences of 2048, 16 heads of 128, window 512: 72 and 79)
   a.chunk_len = elt == 4 ? 128 : 512;
   while ((long)a.chunk_len * 64 < a.s) a.chunk_len *= 2;
+  // Parts of the heads of a key head: a workgroup visits the queries of all of
+  // them, and few workgroups leave compute units empty (256 of them; not the
+  // device's number, as the memory depends on it).  us of dk and dv with and without
+  // parts, a bias: blocks of 128 keys, 7 sequences of 4128, 4 / 1 heads of 40 (231 blocks):
+  // 188, 465; 7 of 1827, 6 / 3 heads of 128 (315): 95, 144; 2 of 4096, 16 / 8 heads
+  // of 128 (512): 434, 396.  Blocks of 32, 2 of 512, 8 / 1 heads of 64 (32): 15, 35;
+  // 1 of 1024, 32 / 8 heads of 128, window 256 (256): 44, 31; fp32, 1 of 1604,
+  // 4 / 1 heads of 96 (51): 103, 365.
+  const bool whole = elt == 2 && blocks * a.kv_heads > 256;
+  const long keys = whole ? 128 : 32, units = (a.s + keys - 1) / keys * a.batch * a.kv_heads;
+  const long most = !whole ? (elt == 4 ? 512 : 256) : units < 384 ? 1024 : units;
+  const long span = std::min((long)a.s, (long)a.left + a.right + keys);
+  a.parts = span * a.group >= 512 ? (int)std::max(1L, std::min((long)a.group, most / units)) : 1;
+  a.part_rows = (a.s + 127) / 128 * 128;
   a.chunks = a.sinks && !(a.split_k && a.s <= a.chunk_len) ? sink_chunks(a) : 0;
 }
 
@@ -107,9 +131,7 @@ size_t attn_op_saved_bytes(const AttnOpArgs& a, int elt) {
 }
 
 size_t attn_op_work_bytes(const AttnOpArgs& a) {
-  return align256(4 * rows(a)) + bias_bytes(a) +
-         align256(4 * (size_t)a.batch * a.kv_heads * (a.sinks ? 1 + sink_chunks(a) : 0) * 2 * a.sink_rows *
-                  columns(a.d));
+  return align256(4 * rows(a)) + bias_bytes(a) + sink_bytes(a) + part_bytes(a);
 }
 
 namespace {
@@ -148,6 +170,8 @@ hipError_t attn_op_backward(AttnOpArgs a, int elt, const void* saved, void* work
   a.bpart = (float*)w;
   w += bias_bytes(a);
   a.spart = (float*)w;
+  w += sink_bytes(a);
+  a.gpart = (float*)w;
   const int c = columns(a.d);
   if (elt == 4)
     return c == 32   ? attn_op_bwd_f32_32(a, st)

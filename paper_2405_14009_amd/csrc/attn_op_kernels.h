@@ -1004,9 +1004,17 @@ struct AttnOp {
     T::template outer<FINE>(dk, qt, j, dp, of, lane);
   }
 
-  // This wave's rows k0.. of dk or dv as share `n` of the sinks' rows.
+  // This wave's rows k0.. of dk or dv as share `n` of the sinks' rows, or as the
+  // share of a part of the heads.
   static __device__ __forceinline__ float* share(const AttnOpArgs& p, int z, int n, int which, int k0) {
-    return p.spart + ((((long)z * (1 + p.chunks) + n) * 2 + which) * p.sink_rows + k0) * HD;
+    return p.spart + ((((long)z * (1 + p.chunks * p.parts) + n) * 2 + which) * p.sink_rows + k0) * HD;
+  }
+  static __device__ __forceinline__ float* part_share(const AttnOpArgs& p, int z, int part, int which, int k0) {
+    return p.gpart + ((((long)z * p.parts + part) * 2 + which) * p.part_rows + k0) * HD;
+  }
+  // The heads [first, second) of a part.
+  static __device__ __forceinline__ int2 heads_of(const AttnOpArgs& p, int hk, int part) {
+    return make_int2(hk * p.group + part * p.group / p.parts, hk * p.group + (part + 1) * p.group / p.parts);
   }
   static __device__ __forceinline__ void store_share(const f32x16& a, float* to, int i, int lane) {
     to += (lane & 31) * HD + 32 * i + 4 * (lane >> 5);
@@ -1043,16 +1051,18 @@ struct AttnOp {
 
   static __device__ __forceinline__ void dkv(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
-    const int nkb = (p.s + 127) / 128, units = nkb + p.sink_rows / 32 * p.chunks;
+    const int nkb = (p.s + 127) / 128 * p.parts, units = nkb + p.sink_rows / 32 * p.chunks * p.parts;
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
-    if (kb >= nkb) return dkv32<SINK, false>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
+    if (kb >= nkb) return dkv_sinks<false>(p, lds, z, kb - nkb);
+    const int part = kb % p.parts;
     float* const table = (float*)(lds + 2 * KSTAGE);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = z / p.kv_heads, hk = z % p.kv_heads;
     const int len = length(p, b);
-    const int K0 = kb * 128, k0 = K0 + 32 * wave, kk = k0 + (lane & 31);
+    const int2 heads = heads_of(p, hk, part);
+    const int K0 = kb / p.parts * 128, k0 = K0 + 32 * wave, kk = k0 + (lane & 31);
     // the queries whose windows hold these keys
     const int qlo = (int)max(0L, (long)K0 - p.right);
     const int qhi = K0 < len ? (int)min((long)len - 1, (long)K0 + 127 + p.left) : -1;
@@ -1062,7 +1072,7 @@ struct AttnOp {
     // computed in order, so both count along
     int gi = 0, ti = 0, gc = 0, tc = 0;
     auto issue = [&](char* t, int) {
-      const int h = hk * p.group + gi, row0 = (t0 + ti) * 64;
+      const int h = heads.x + gi, row0 = (t0 + ti) * 64;
       if (ti == 0) {
         qs.set(base(p.q, b, h), p.q.t, len);
         ds.set(base(p.dout, b, h), p.dout.t, len);
@@ -1086,10 +1096,10 @@ struct AttnOp {
       zero(dk[i]);
       zero(dv[i]);
     }
-    pipeline(nt * p.group, lds, KSTAGE, issue, [&](char* cur, int) {
+    pipeline(nt * (heads.y - heads.x), lds, KSTAGE, issue, [&](char* cur, int) {
       if constexpr (BIAS) {
         if (tc == 0) {  // the first tile of a head: its bias
-          fill_table(p, hk * p.group + gc, table);
+          fill_table(p, heads.x + gc, table);
           __syncthreads();
         }
       }
@@ -1107,11 +1117,13 @@ struct AttnOp {
         zero(dv[i]);
       }
     }
-    if (p.chunks && k0 < p.sink_rows) {
+    if (p.parts > 1 || (p.chunks && k0 < p.sink_rows)) {
+      float* const to_k = p.parts > 1 ? part_share(p, z, part, 0, k0) : share(p, z, 0, 0, k0);
+      float* const to_v = p.parts > 1 ? part_share(p, z, part, 1, k0) : share(p, z, 0, 1, k0);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        store_share(dk[i], share(p, z, 0, 0, k0), i, lane);
-        store_share(dv[i], share(p, z, 0, 1, k0), i, lane);
+        store_share(dk[i], to_k, i, lane);
+        store_share(dv[i], to_v, i, lane);
       }
       return;
     }
@@ -1125,7 +1137,7 @@ struct AttnOp {
   // the keys, for the queries of a chunk that see them as such.
   static constexpr int KOWN = OWN + (T::DIRECT ? 0 : 3072);
   template <int MODE, bool FINE>
-  static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk) {
+  static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk, int part) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     char* const own = lds + wave * KOWN;
@@ -1157,8 +1169,8 @@ struct AttnOp {
       zero(dk[i]);
       zero(dv[i]);
     }
-    for (int g = 0; g < p.group; ++g) {
-      const int h = hk * p.group + g;
+    const int2 heads = heads_of(p, hk, part);
+    for (int h = heads.x; h < heads.y; ++h) {
       Src qs, ds;
       qs.set(base(p.q, b, h), p.q.t, len);
       ds.set(base(p.dout, b, h), p.dout.t, len);
@@ -1197,7 +1209,7 @@ struct AttnOp {
         put<NB>(dk, own, lane);
       __syncthreads();
       const AttnOpView& view = which ? p.dv : p.dk;
-      const int n = MODE == SINK ? 1 + chunk : 0;
+      const int n = MODE == SINK ? 1 + chunk * p.parts + part : 0;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         if (i % 4 != wave) continue;
@@ -1207,25 +1219,33 @@ struct AttnOp {
 #pragma unroll
           for (int u = 0; u < 4; ++u) add_scaled(a, lds + u * KOWN, i, lane, 1.0f);
         }
-        if (p.chunks && k0 < p.sink_rows)
+        if (MODE != SINK && p.parts > 1)
+          store_share(a, part_share(p, z, part, which, k0), i, lane);
+        else if (p.chunks && k0 < p.sink_rows)
           store_share(a, share(p, z, n, which, k0), i, lane);
         else
           T::store_cols(a, out(view, b, hk), view.t, k0, p.s, i, lane, which ? 1.0f : p.scale, p.d);
       }
     }
   }
+  // Unit u of the sinks' workgroups: 32 keys, a chunk of queries, a part of the heads.
+  template <bool FINE>
+  static __device__ __forceinline__ void dkv_sinks(const AttnOpArgs& p, char* lds, int z, int u) {
+    const int n = p.chunks * p.parts;
+    dkv32<SINK, FINE>(p, lds, z, u / n * 32, u % n / p.parts, u % p.parts);
+  }
   template <bool FINE>
   static __device__ __forceinline__ void dkv_split(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
-    const int nkb = (p.s + 31) / 32, units = nkb + p.sink_rows / 32 * p.chunks;
+    const int nkb = (p.s + 31) / 32 * p.parts, units = nkb + p.sink_rows / 32 * p.chunks * p.parts;
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
     if (kb >= nkb)
-      dkv32<SINK, FINE>(p, lds, z, (kb - nkb) / p.chunks * 32, (kb - nkb) % p.chunks);
+      dkv_sinks<FINE>(p, lds, z, kb - nkb);
     else if (p.chunks)
-      dkv32<WINDOW, FINE>(p, lds, z, kb * 32, 0);
+      dkv32<WINDOW, FINE>(p, lds, z, kb / p.parts * 32, 0, kb % p.parts);
     else
-      dkv32<BOTH, FINE>(p, lds, z, kb * 32, 0);
+      dkv32<BOTH, FINE>(p, lds, z, kb / p.parts * 32, 0, kb % p.parts);
   }
 
   // LDS of the kernels.
@@ -1240,10 +1260,11 @@ struct AttnOp {
   }
 };
 
-// The sinks' rows of dk and dv from their shares, in order.  One workgroup per
-// sequence, key head and 8 keys; a thread sums 4 columns.
+// Rows of dk and dv from their shares, in order: all rows where the heads are taken
+// in parts, the sinks' otherwise.  One workgroup per sequence, key head and 8
+// keys; a thread sums 4 columns.
 template <class T>
-__global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
+__global__ __launch_bounds__(256) void attn_op_sum_k(AttnOpArgs p) {
   constexpr int HD = T::HD, C4 = HD / 4;
   using E = typename T::E;
   const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, r8 = blockIdx.x / bk;
@@ -1251,15 +1272,23 @@ __global__ __launch_bounds__(256) void attn_op_sinks_k(AttnOpArgs p) {
   for (int i = threadIdx.x; i < 8 * 2 * C4; i += 256) {
     const int c = 4 * (i % C4), which = i / C4 % 2, row = 8 * r8 + i / (2 * C4);
     if (row >= p.s || c >= p.d) continue;
-    const float* src = p.spart + (((long)z * (1 + p.chunks) * 2 + which) * p.sink_rows + row) * HD + c;
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float* src, int n, long step) {
 #pragma unroll 8
-    for (int n = 0; n <= p.chunks; ++n) {
-      const float4 v = *(const float4*)(src + (long)n * 2 * p.sink_rows * HD);
-      t.x += v.x;
-      t.y += v.y;
-      t.z += v.z;
-      t.w += v.w;
+      for (int k = 0; k < n; ++k) {
+        const float4 v = *(const float4*)(src + k * step);
+        t.x += v.x;
+        t.y += v.y;
+        t.z += v.z;
+        t.w += v.w;
+      }
+    };
+    if (p.parts > 1)
+      add(p.gpart + (((long)z * p.parts * 2 + which) * p.part_rows + row) * HD + c, p.parts, 2L * p.part_rows * HD);
+    if (p.chunks && row < p.sink_rows) {
+      const int first = p.parts > 1 ? 1 : 0, all = 1 + p.chunks * p.parts;
+      add(p.spart + ((((long)z * all + first) * 2 + which) * p.sink_rows + row) * HD + c, all - first,
+          2L * p.sink_rows * HD);
     }
     const float mul = which ? 1.0f : p.scale;
     const AttnOpView& v = which ? p.dv : p.dk;
@@ -1329,7 +1358,8 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
   const bool sq = T::DIRECT || a.split_q, sk = T::DIRECT || a.split_k;
   const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
   const dim3 gq((unsigned)(nq * a.batch * a.heads));
-  const dim3 gk((unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
+  const dim3 gk(
+      (unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.parts * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
   a.bias_blocks = (int)nq;
   const bool fine = T::REST && a.seen <= kSeenBackward;
   if (sq && fine)
@@ -1347,9 +1377,9 @@ hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
   else if constexpr (!T::DIRECT)
     hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, false), st, a);
   e = hipGetLastError();
-  if (e != hipSuccess || !a.chunks) return e;
-  const long rows = a.sink_rows < a.s ? a.sink_rows : a.s;
-  hipLaunchKernelGGL((attn_op_sinks_k<T>), dim3((unsigned)((rows + 7) / 8 * a.batch * a.kv_heads)), dim3(256), 0, st, a);
+  if (e != hipSuccess || (!a.chunks && a.parts == 1)) return e;
+  const long rows = a.parts > 1 || a.sink_rows > a.s ? a.s : a.sink_rows;
+  hipLaunchKernelGGL((attn_op_sum_k<T>), dim3((unsigned)((rows + 7) / 8 * a.batch * a.kv_heads)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -105,7 +105,7 @@ def kernel_class(name: str) -> str:
         return "attn_fwd"
     if "attn_op_add_dbias" in name:
         return "reduce"
-    if "attn_op_" in name:            # dq, dk and dv, the sinks' shares
+    if "attn_op_" in name:            # dq, dk and dv, the sums of shares
         return "attn_bwd"
     if re.search(r"ln_(fwd|bwd)(_wave)?_k", name):
         return "layernorm"

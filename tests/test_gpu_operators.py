@@ -113,6 +113,23 @@ def test_attention(case, kind):
     compare(t, do, run(t, do, **how), **how)
 
 
+# Few workgroups of dk and dv, and many heads for each of them: taken in parts.
+PARTS = [
+    (1, 1100, 8, 1, 40, True, 0, 0, 16, 100, None),       # blocks of 32 keys; 7 parts of 8 heads
+    (2, 530, 6, 2, 128, False, 0, 0, 0, 0, (530, 301)),
+    (1, 700, 6, 2, 24, True, 100, 40, 8, 30, None),       # with the sinks' own workgroups
+    (1, 400, 12, 2, 64, True, 90, 7, 0, 0, (333,)),       # and without
+    (6, 1500, 3, 1, 48, True, 300, 40, 8, 20, (1500, 0, 1400, 77, 1, 1000)),   # blocks of 128 keys
+    (6, 1500, 3, 1, 72, False, 0, 0, 0, 0, None),
+]
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", PARTS, ids=lambda c: "-".join(str(x) for x in c[:10]))
+def test_heads_in_parts(case, kind):
+    test_attention(case, kind)
+
+
 # -- layouts, streams, graphs ----------------------------------------------------
 
 MASKED = dict(causal=False, window=40, sinks=3, max_distance=50)

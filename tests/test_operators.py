@@ -90,6 +90,17 @@ def test_attention_refusals(kw, status, word):
     assert word in lib.rc_last_error()
 
 
+@pytest.mark.parametrize("bf16,sinks", [(True, 0), (False, 0), (True, 9), (False, 9)])
+def test_attention_memory_holds_the_shares_of_parts(bf16, sinks):
+    """4 heads a key head and 16 blocks of 32 keys: four parts, of the keys and of the sinks' chunks."""
+    L, _ = lib_or_skip()
+    size = dict(dtype=L.RC_BF16 if bf16 else L.RC_FP32, batch=1, seq_len=500, heads=4, kv_heads=1, head_dim=72)
+    if sinks:
+        size.update(window=300, sinks=sinks)
+    shares = 4 * 2 * 500 + (4 * 2 * 32 if sinks else 0)
+    assert memory(**size)[2] >= up(4 * 4 * 512) + 4 * 96 * shares
+
+
 def test_attention_takes_the_most_blocks_of_a_launch():
     assert memory(seq_len=128, batch=(1 << 24) - 2, heads=1, kv_heads=1)[0] == 0
 
@@ -279,7 +290,7 @@ def test_moment_formats():
     ("void (anonymous namespace)::attn_op_fwd32_k<(anonymous namespace)::TileF32<64>, false>(AttnOpArgs)", "attn_fwd"),
     ("void (anonymous namespace)::attn_op_dq_k<(anonymous namespace)::TileB16<64>, true>(AttnOpArgs)", "attn_bwd"),
     ("void (anonymous namespace)::attn_op_dkv32_k<(anonymous namespace)::TileB16<64>, true>(AttnOpArgs)", "attn_bwd"),
-    ("void (anonymous namespace)::attn_op_sinks_k<(anonymous namespace)::TileB16<64> >(AttnOpArgs)", "attn_bwd"),
+    ("void (anonymous namespace)::attn_op_sum_k<(anonymous namespace)::TileB16<64> >(AttnOpArgs)", "attn_bwd"),
     ("(anonymous namespace)::attn_op_add_dbias_k(AttnOpShares, int, long, float*, int)", "reduce"),
     ("void (anonymous namespace)::adamw_tensors_k<8, 1>((anonymous namespace)::Args)", "adamw"),
 ])
