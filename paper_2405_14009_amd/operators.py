@@ -293,18 +293,19 @@ class AdamW:
             out = [[torch.empty(p.numel(), dtype=torch.float32, device=p.device) for p in self.params]
                    for _ in range(2)]
         n = len(self.params)
+        index, f32, Tensor = self.device.index if n else None, torch.float32, torch.Tensor
         arrays = []
         for name, tensors in zip(("exp_avg", "exp_avg_sq"), out):
             if len(tensors) != n:
                 raise ValueError(f"{name} must have {n} entries")
-            pointers = (ctypes.c_void_p * max(1, n))()
-            for i, (t, count) in enumerate(zip(tensors, self._counts)):
-                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != self.device.index:
+            wrong = [i for i, (t, count) in enumerate(zip(tensors, self._counts))
+                     if not isinstance(t, Tensor) or t.get_device() != index or t.dtype is not f32
+                     or t.numel() != count or not t.is_contiguous()]
+            for i in wrong:
+                if not isinstance(tensors[i], Tensor) or tensors[i].get_device() != index:
                     raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
-                if t.dtype is not torch.float32 or t.numel() != count or not t.is_contiguous():
-                    raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {count} elements")
-                pointers[i] = t.data_ptr()
-            arrays.append(pointers)
+                raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {self._counts[i]} elements")
+            arrays.append((ctypes.c_void_p * max(1, n))(*[t.data_ptr() for t in tensors]))
         if n:
             on, stream = _on(self.device)
             _call(on, self._lib.rc_adamw_read, self._tensors, n, self.state_bits, *arrays, stream)
