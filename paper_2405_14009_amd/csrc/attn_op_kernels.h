@@ -1024,7 +1024,7 @@ struct AttnOp {
   }
 
   // A stage: a Q tile, a dO tile and the row vectors m, l, D of 64 queries.
-  static constexpr int KSTAGE = 2 * TILE + 3072;
+  static constexpr int KSTAGE = 2 * TILE + 3 * 1024;
 
   // dbias[h, c] = sum of the query blocks' shares in the order of (sequence,
   // block): 256 / buckets groups of threads take every g-th share, then add up.
@@ -1135,7 +1135,7 @@ struct AttnOp {
   // 32 keys a workgroup: its waves take every fourth block of 32 queries, of
   // every head of the group, with tiles of their own.  MODE SINK: the sinks among
   // the keys, for the queries of a chunk that see them as such.
-  static constexpr int KOWN = OWN + (T::DIRECT ? 0 : 3072);
+  static constexpr int KOWN = OWN + (T::DIRECT ? 0 : 3 * 1024);
   template <int MODE, bool FINE>
   static __device__ __forceinline__ void dkv32(const AttnOpArgs& p, char* lds, int z, int k0, int chunk, int part) {
     const int lane = threadIdx.x & 63;
