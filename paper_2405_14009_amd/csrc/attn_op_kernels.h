@@ -314,7 +314,7 @@ struct AttnOp {
   // with a DPP operand) into the sum of its distance: to[0], to[16] for what
   // leaves the row of lanes and for rows 16 and on, to[32] for both.  30
   // additions and three LDS atomics a half for 16 elements (us, dq of 40 heads of 128, s
-  // 4096, window 2048, 64 buckets: 469, against 821 with sixteen atomics).
+  // 4096, window 2048, 64 buckets: 334, against 639 with sixteen atomics).
   template <int R>
   static __device__ __forceinline__ void shift_in(float& stays, float& leaves, const f32x16& x) {
     constexpr int b = row_of(R) % 16;
@@ -536,7 +536,7 @@ struct AttnOp {
   // gradient sums it over the far bucket, which holds most of a long row
   // (2133 tokens, both directions, 8 buckets: 4.1e-3, against 1.7e-3).  There the
   // forward also adds what the rounding drops (FINE; us, 32 heads of 128, s 2048, with
-  // a bias: 64 -> 75).
+  // a bias: 68 -> 79).
   template <bool FINE>
   static __device__ __forceinline__ void fwd_tile(Fwd& st, const Rows& qf, const char* kt, const char* vt, const Offs& of,
                                                   int k0, int q0, int qq, int lane, int len, const float* table,
