@@ -32,8 +32,9 @@ struct AttnOpArgs {
   // the last bucket of their side
   const void* bias;
   int bias_f32, buckets, far;
-  // row statistics [batch, heads, spad]: reference score and log2 of the sum of
-  // exponentials relative to it (base 2), and (bf16) what the rounding of o drops
+  // row statistics [batch, heads, spad]: reference score (q.k, or with a bias in base 2)
+  // and log2 of the sum of exponentials relative to it, and (bf16) what the rounding of
+  // o drops
   float *m, *l;
   void* rest;
   float* drow;   // [batch, heads, spad] rowsum(dO o O)

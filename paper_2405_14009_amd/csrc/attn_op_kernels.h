@@ -25,8 +25,9 @@
 // every sum has a fixed order); far blocks add up in registers.  The tables are summed by buckets
 // when the workgroup ends, and over workgroups by the next kernel (dk and dv).
 //
-// D is formed by the same chain of matrix instructions as do.v: where a row
-// sees one token only, dS is exactly zero.
+// Exponents are taken of score differences, and D is formed by the same chain of
+// matrix instructions as do.v: where a row sees one token only, its probability
+// is exactly one and dS exactly zero.
 //
 // us, forward / dq / dk and dv: 32 heads of 128, s 2048, causal, 32 buckets: 77 /
 // 104 / 114; 32 and 8 heads of 128, s 8192, window 1024: 191 / 260 / 395; 16 heads
@@ -481,6 +482,13 @@ struct AttnOp {
   }
 
   // -- forward -----------------------------------------------------------------
+  // Scores and the reference m are in base 2 with a bias, and as the products give
+  // them without.  Exponents come from their difference: at a row's only visible
+  // token it is zero, so its probability is exactly one, o its value and dS zero.
+  // (The rounded product of a score with sl2, less that of m, is not zero.  us of the
+  // forward with that and with differences: 32 / 8 heads of 128, s 8192, window 1024:
+  // 191, 197; 16 heads of 64, s 16384, window 256: 64, 66.)
+  static __device__ __forceinline__ float base2(float x, const AttnOpArgs& p) { return BIAS ? x : x * p.sl2; }
   struct Fwd {
     f32x16 o[NB];
     float m, l;
@@ -514,12 +522,11 @@ struct AttnOp {
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[j][r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    if constexpr (!BIAS) mx *= p.sl2;
     // the reference moves when a row's maximum exceeds it by more than 2^8
-    const bool grow = mx > st.m + 8.f;
+    const bool grow = base2(mx - st.m, p) > 8.f;
     if (__any(grow)) {
       const float m_new = grow ? mx : st.m;
-      const float alpha = __builtin_amdgcn_exp2f(st.m - m_new);
+      const float alpha = __builtin_amdgcn_exp2f(base2(st.m - m_new, p));
       st.m = m_new;
       st.l *= alpha;
 #pragma unroll
@@ -532,7 +539,7 @@ struct AttnOp {
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float e = __builtin_amdgcn_exp2f(BIAS ? sc[j][r] - st.m : fmaf(sc[j][r], p.sl2, -st.m));
+        const float e = __builtin_amdgcn_exp2f(base2(sc[j][r] - st.m, p));
         sc[j][r] = e;
         ls += e;
       }
@@ -654,7 +661,7 @@ struct AttnOp {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const float2 t = stats[u * 64 + lane];
-      scale[u] = __builtin_amdgcn_exp2f(t.x - m);
+      scale[u] = __builtin_amdgcn_exp2f(base2(t.x - m, p));
       l += scale[u] * t.y;
     }
     st.m = m;
@@ -739,11 +746,11 @@ struct AttnOp {
   }
 
   // -- dq, dbias and D -----------------------------------------------------------
-  // A wave's 32 queries: rows of q and dout, the reference score, and what turns
-  // do.v into dS / 2^(x - m) = do.v / sum - D / sum.
+  // A wave's 32 queries: rows of q and dout, and the statistics.  With a bias
+  // what turns do.v into dS / 2^(x - m) = do.v / sum - D / sum: inv, and D times it.
   struct Queries {
     Rows q, d;
-    float m, inv, D;
+    float m, l, inv, D;
   };
   static __device__ __forceinline__ void load_queries(Queries& w, const AttnOpArgs& p, int b, int h, int qq, int len,
                                                       int lane, bool write) {
@@ -771,8 +778,9 @@ struct AttnOp {
     D += __shfl_xor(D, 32, 64);
     if (write && lane < 32 && qq < p.spad) p.drow[row] = qq < len ? D : 0.f;
     w.m = qq < p.s ? p.m[row] : 0.f;
-    w.inv = qq < p.s ? __builtin_amdgcn_exp2f(-p.l[row]) : 0.f;
-    w.D = D * w.inv;
+    w.l = qq < p.s ? p.l[row] : 0.f;
+    w.inv = qq < p.s ? __builtin_amdgcn_exp2f(-w.l) : 0.f;
+    w.D = BIAS ? D * w.inv : D;
   }
 
   // Sums of dS by distance: this wave's table of near ones, far ones on either side.
@@ -840,10 +848,10 @@ struct AttnOp {
       add_bias<1>(sc, table, e, c, near, p);
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - w.m : fmaf(sc[r], p.sl2, -w.m));
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - w.m : fmaf(sc[r] - w.m, p.sl2, -w.l));
     if (wave_uniform(!all_visible<32, 32>(p, q0, k, len))) mask_keys(sc, k, qq, lane, 0.f, len, p);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * fmaf(dp[r], w.inv, -w.D);
+    for (int r = 0; r < 16; ++r) dp[r] = sc[r] * (BIAS ? fmaf(dp[r], w.inv, -w.D) : dp[r] - w.D);
     if constexpr (BIAS) {
       if (near) {
         add_diagonals(sums.near + e, dp, lane);
@@ -995,16 +1003,11 @@ struct AttnOp {
     const int at = 4 * (lane >> 5);
     f32x16 row;  // a statistic of the block's queries
     load_rows16(row, m + at);
-    if constexpr (BIAS) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] -= row[r];
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = fmaf(sc[r], p.sl2, -row[r]);
-    }
+    for (int r = 0; r < 16; ++r) sc[r] -= row[r];
     load_rows16(row, l + at);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(sc[r] - row[r]);
+    for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - row[r] : fmaf(sc[r], p.sl2, -row[r]));
     load_rows16(row, D + at);
     if (wave_uniform(!all_of<MODE>(p, q, k0, len))) mask_queries<MODE>(sc, q, kk, lane, len, p);
 #pragma unroll

@@ -248,6 +248,48 @@ def test_one_visible_token(kind):
         assert float(got[n].abs().max()) == 0.0, n
 
 
+# b, s, heads, kv heads, d, causal, window, lengths
+ALONE = [
+    (2, 150, 4, 2, 64, True, 1, None),
+    (1, 130, 3, 3, 128, False, 1, None),
+    (3, 1, 4, 1, 16, True, 0, None),
+    (1, 1, 2, 2, 80, False, 0, None),
+    (3, 70, 2, 2, 96, False, 0, (1, 0, 1)),              # one token in a padded sequence
+    (1, 500, 32, 1, 40, True, 1, None),                  # the heads of dk and dv in parts
+    (300, 1, 1, 1, 64, False, 0, None),                  # grids of more than 256 blocks of 32 tokens
+    (5, 300, 12, 6, 128, True, 1, (300, 299, 1, 0, 40)),
+    (3, 700, 16, 16, 80, False, 1, None),
+]
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", ALONE, ids=lambda c: "-".join(str(x) for x in c[:7]))
+def test_one_visible_token_without_a_bias(case, kind):
+    """The probability is one whatever the score: o is the value, and no gradient reaches the scores."""
+    b, s, h, kv, d, causal, window, lengths = case
+    t, do = inputs(b, s, h, kv, d, kind)
+    how = dict(causal=causal, window=window)
+    n = torch.tensor([s] * b if lengths is None else lengths, dtype=torch.int32, device="cuda")
+    if lengths is not None:
+        how["lengths"] = n
+    got = run(t, do, **how)
+    real = (torch.arange(s, device="cuda") < n[:, None])[:, :, None, None]
+    assert torch.equal(got["o"], torch.where(real, t["v"].repeat_interleave(h // kv, 2), 0.0).to(kind))
+    for x in ("dq", "dk"):
+        assert int(torch.count_nonzero(got[x])) == 0, (x, float(got[x].abs().max()))
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("b,s,h,kv,d", [(2, 100, 4, 2, 64), (2, 700, 12, 12, 128)])
+def test_the_first_token_of_a_causal_sequence(b, s, h, kv, d, kind):
+    """The one row that sees a single token, next to rows that see more."""
+    t, do = inputs(b, s, h, kv, d, kind)
+    got = run(t, do)
+    assert torch.equal(got["o"][:, 0], t["v"][:, 0].repeat_interleave(h // kv, 1))
+    assert int(torch.count_nonzero(got["dq"][:, 0])) == 0
+    assert int(torch.count_nonzero(got["dq"][:, 1])) > 0
+
+
 @pytest.mark.parametrize("low", [-math.inf, "lowest"])
 @pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
 def test_bias_that_hides(kind, low):
