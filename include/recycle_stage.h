@@ -458,9 +458,10 @@ typedef struct rc_view {
  *
  * Requirements (otherwise RC_ERR_UNSUPPORTED): head_dim a multiple of 8, at
  * most 128; buckets at most 128, max_distance at most 1024; seq_len at most
- * 2^24; batch heads ceil(seq_len / 128) below 2^24, and with a window batch
- * heads ceil(sinks / 8) too; in every tensor a head's tokens span less than
- * 2^31 bytes (bf16) or token strides are below 2^24 elements (fp32). */
+ * 2^24; heads (batch n + 1) below 2^24, where n = ceil(seq_len / 128) (fp32:
+ * ceil(seq_len / 32)), more with sinks (each 32 of them for each chunk of
+ * queries, or ceil(sinks / 8) where that is more); in every tensor a head's tokens
+ * span less than 2^31 bytes (bf16) or token strides are below 2^24 elements (fp32). */
 typedef struct rc_attention {
   int32_t dtype;        /* rc_dtype of q, k, v, o and their gradients */
   int32_t batch, seq_len, heads, kv_heads, head_dim;

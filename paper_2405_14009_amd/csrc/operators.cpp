@@ -51,9 +51,12 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   a.bias_f32 = c.bias_dtype == RC_FP32;
   attn_op_plan(a, c.dtype == RC_FP32 ? 4 : 2, c.window, c.max_distance);
   // workgroups a batch and head: of the kernels over queries, over keys, and over the sinks' rows
-  const long units = std::max((a.s + 127) / 128 + (long)a.sink_rows / 32 * a.chunks, (std::min(a.sinks, a.s) + 7L) / 8);
+  // (bf16 grids take 32 tokens a workgroup only where that is few workgroups)
+  const int rows = c.dtype == RC_FP32 ? 32 : 128;
+  const long units =
+      std::max((a.s + rows - 1) / rows + (long)a.sink_rows / 32 * a.chunks, (std::min(a.sinks, a.s) + 7L) / 8);
   if (units * a.batch > (ATTN_OP_MAX_GROUPS - a.heads) / a.heads)
-    return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^24 - 1 blocks of 128 tokens of a head");
+    return rc_set_error(RC_ERR_UNSUPPORTED, "more than 2^24 - 1 blocks of " + std::to_string(rows) + " tokens of a head");
   return RC_OK;
 }
 

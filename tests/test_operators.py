@@ -105,6 +105,31 @@ def test_attention_takes_the_most_blocks_of_a_launch():
     assert memory(seq_len=128, batch=(1 << 24) - 2, heads=1, kv_heads=1)[0] == 0
 
 
+@pytest.mark.parametrize("seq,heads,batch,masks", [
+    (1, 1, (1 << 24) - 2, {}),
+    (32, 2, (1 << 23) - 2, {}),      # a launch may have a workgroup more per head (the bias gradient)
+    (33, 1, (1 << 23) - 1, {}),
+    (64, 1, (1 << 23) - 1, {}),
+    (128, 1, (1 << 22) - 1, {}),
+    (128, 4, (1 << 20) - 1, dict(window=8)),
+    (1 << 24, 31, 1, dict(window=16)),
+])
+def test_fp32_attention_takes_the_most_blocks_of_a_launch(seq, heads, batch, masks):
+    """fp32 kernels take 32 tokens a workgroup: the largest batches whose launches are
+    below 2^24 workgroups, and the next ones, which are refused up front."""
+    L, lib = lib_or_skip()
+    size = dict(dtype=L.RC_FP32, seq_len=seq, heads=heads, kv_heads=heads, head_dim=8, **masks)
+    assert memory(**size, batch=batch)[0] == L.RC_OK
+    more = dict(heads=heads + 1, kv_heads=heads + 1, batch=batch) if batch == 1 else dict(batch=batch + 1)
+    assert memory(**{**size, **more})[0] == L.RC_ERR_UNSUPPORTED and b"blocks" in lib.rc_last_error()
+
+
+def test_a_stage_refuses_launches_beyond_the_most_blocks():
+    L, lib = lib_or_skip()
+    cfg = dict(hidden=8, heads=1, ffn=8, seq_len=64, micro_batch=1 << 23, dtype=L.RC_FP32)
+    assert stage_memory(cfg, window=2)[0] == L.RC_ERR_UNSUPPORTED and b"blocks" in lib.rc_last_error()
+
+
 def test_attention_refuses_tensors_before_any_device_work():
     """Null, misaligned, overlapping and oversized tensors (host addresses that are
     never touched)."""
