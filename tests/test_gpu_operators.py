@@ -588,3 +588,63 @@ def test_refusals_of_the_python_calls():
         with pytest.raises(ValueError):
             opt.moments(out)
     assert float(x.abs().sum()) == 0.0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_follows_its_tensors(bits):
+    """Parameters and gradients that have other memory, or are other tensors, than at the
+    last step: the step takes the new ones and leaves the old ones alone."""
+    sizes = [300, 17, 129]
+    p, g = adamw_set(sizes, bits, F32)
+    opt = ops().AdamW(p, g, state_bits=bits)
+    opt.step()
+    old = [x.detach() for x in p] + [x.detach() for x in g]    # the same memory
+    kept = [x.clone() for x in old]
+    p[0].data = p[0].detach() + 1.0
+    g[1].data = g[1].detach() * 2.0
+    opt.grads[2] = (g[2] * 3.0).bfloat16()
+    opt.exp_avg[1] = opt.exp_avg[1].clone()
+    opt.decay[0] = False
+    before, grads = state(opt), [x.double().cpu().numpy() for x in opt.grads]
+    opt.step(0.5)
+    check_adamw(opt, before, grads, 0.5, 2)
+    changed = [not torch.equal(a, b) for a, b in zip(old, kept)]
+    assert changed == [False, True, True, False, False, False]
+    # another tensor between the step and the reading of the moments
+    opt.exp_avg[0] = opt.exp_avg[0] * 1
+    m, v = opt.moments()
+    for i, (_, wm, wv) in enumerate(state(opt)):
+        assert np.array_equal(m[i].cpu().numpy(), wm.astype(np.float32)), i
+        assert np.array_equal(v[i].cpu().numpy(), wv.astype(np.float32)), i
+
+
+def test_adamw_refuses_what_its_tensors_became():
+    """Tensors that no longer fit are refused by the next step, which changes nothing; put right, it runs."""
+    p, g = adamw_set([60, 40], 32, F32)
+    opt = ops().AdamW(p, g)
+    opt.step()
+    kept = [x.clone() for x in p]
+    p[0].data, was = p[0].detach()[:50], p[0].detach()
+    for _ in range(2):
+        with pytest.raises(ValueError):
+            opt.step()
+    p[0].data = was.view(6, 10).t()
+    with pytest.raises(ValueError):
+        opt.step()
+    p[0].data = was
+    for lists, error, entry in ((opt.grads, TypeError, None), (opt.grads, ValueError, g[0]), (opt.params, TypeError, p[1].cpu()),
+                                (opt.exp_avg, ValueError, opt.exp_avg[0]), (opt.params, ValueError, p[0]),
+                                (opt.copies, ValueError, p[1])):
+        right, lists[1] = lists[1], entry
+        with pytest.raises(error):
+            opt.step()
+        lists[1] = right
+    opt.params.append(p[0])
+    for call in (opt.step, opt.moments):
+        with pytest.raises(ValueError):
+            call()
+    opt.params.pop()
+    assert opt.steps == 1 and all(torch.equal(a, b) for a, b in zip(p, kept))
+    before, grads = state(opt), [x.cpu().double().numpy() for x in g]
+    opt.step()
+    check_adamw(opt, before, grads, 1.0, 2)
