@@ -535,7 +535,8 @@ rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam
 /* The moments of n tensors as fp32 values (a checkpoint, a resumed run with
  * 32-bit moments): exp_avg[i] and exp_avg_sq[i] are device arrays of
  * tensors[i].count floats, host arrays of n pointers.  Only the moments, scales
- * and counts of the tensors are looked at.
+ * and counts of the tensors are looked at.  The destinations overlap neither each
+ * other nor the moments.
  * Errors: RC_ERR_INVALID_ARG, RC_ERR_HIP. */
 rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state_bits,
                         float* const* exp_avg, float* const* exp_avg_sq, void* hip_stream);

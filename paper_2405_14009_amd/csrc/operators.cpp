@@ -6,6 +6,7 @@
 #include <exception>
 #include <string>
 #include <utility>
+#include <vector>
 
 #include "adamw_op.h"
 #include "attn_op.h"
@@ -157,6 +158,31 @@ rc_status moment_args(const rc_adamw_tensor& t, int state_bits, const std::strin
   return RC_OK;
 }
 
+// Whether the destinations of the moments overlap each other or the moments.
+bool read_overlaps(const rc_adamw_tensor* t, int n, int state_bits, float* const* m, float* const* v) {
+  using Span = std::pair<uintptr_t, uintptr_t>;
+  std::vector<Span> out;
+  out.reserve(2 * (size_t)n);
+  for (int i = 0; i < n; ++i)
+    for (const float* p : {m[i], v[i]})
+      if (t[i].count) out.emplace_back((uintptr_t)p, (uintptr_t)(p + t[i].count));
+  std::sort(out.begin(), out.end());
+  for (size_t i = 1; i < out.size(); ++i)
+    if (out[i].first < out[i - 1].second) return true;
+  auto meets = [&](const void* p, int64_t bytes) {
+    const uintptr_t at = (uintptr_t)p;
+    const auto next = std::upper_bound(out.begin(), out.end(), Span(at, UINTPTR_MAX));
+    return (next != out.end() && next->first < at + bytes) || (next != out.begin() && next[-1].second > at);
+  };
+  for (int i = 0; i < n; ++i) {
+    if (!t[i].count) continue;
+    const int64_t bytes = t[i].count * (state_bits / 8), blocks = (t[i].count + ADAMW_BLOCK - 1) / ADAMW_BLOCK;
+    if (meets(t[i].exp_avg, bytes) || meets(t[i].exp_avg_sq, bytes)) return true;
+    if (state_bits == 8 && (meets(t[i].exp_avg_scale, blocks) || meets(t[i].exp_avg_sq_scale, blocks))) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -269,6 +295,8 @@ rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state
       if (!exp_avg[i] || !exp_avg_sq[i] || ((uintptr_t)exp_avg[i] | (uintptr_t)exp_avg_sq[i]) % 4)
         return fail(RC_ERR_INVALID_ARG, name + "null or misaligned destination");
     }
+    if (read_overlaps(tensors, n, state_bits, exp_avg, exp_avg_sq))
+      return fail(RC_ERR_INVALID_ARG, "destinations overlap each other or the moments");
     OnDevice on((hipStream_t)hip_stream);
     if (on.err != hipSuccess) return hip_result(on.err, "device of the stream");
     return hip_result(adamw_read(tensors, n, state_bits, exp_avg, exp_avg_sq, (hipStream_t)hip_stream), "AdamW read");

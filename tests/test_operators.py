@@ -212,6 +212,31 @@ def test_adamw_refusals():
     assert lib.rc_adamw_read(t, 1, 32, out, None, None) == bad
 
 
+def test_adamw_read_refuses_destinations_that_overlap():
+    """Two destinations in one place, partly so, or a destination among the moments (host
+    addresses that are never touched); empty tensors have none."""
+    L, lib = lib_or_skip()
+
+    def read(m, v, bits=32, counts=(100, 50)):
+        kw = [dict(exp_avg=4096, exp_avg_sq=8192), dict(exp_avg=12288, exp_avg_sq=16384)]
+        if bits == 8:
+            kw = [dict(k, exp_avg_scale=20480 + 64 * i, exp_avg_sq_scale=24576 + 64 * i) for i, k in enumerate(kw)]
+        t = (L.RcAdamwTensor * 2)(*[L.RcAdamwTensor(count=c, **k) for c, k in zip(counts, kw)])
+        P = ctypes.c_void_p * 2
+        return lib.rc_adamw_read(t, 2, bits, P(*m), P(*v), None)
+
+    at = 1 << 20
+    for bits in (32, 8):
+        for m, v in (((at, 2 * at), (at, 3 * at)), ((at, 2 * at), (3 * at, 2 * at + 196)), ((at, at + 396), (2 * at, 3 * at)),
+                     ((at, 2 * at), (2 * at - 396, 3 * at)), ((at, 4096), (2 * at, 3 * at)), ((4096, at), (2 * at, 3 * at)),
+                     ((at, 2 * at), (16384 - 396, 3 * at))):
+            assert read(m, v, bits) == L.RC_ERR_INVALID_ARG, (bits, m, v)
+            assert b"overlap" in lib.rc_last_error()
+    for m, v in (((24576, at), (2 * at, 3 * at)), ((at, 20480 + 64), (2 * at, 3 * at))):
+        assert read(m, v, 8) == L.RC_ERR_INVALID_ARG and b"overlap" in lib.rc_last_error()
+    assert read((at, 4096), (2 * at, 4096), counts=(0, 0)) == L.RC_OK
+
+
 def stage_memory(cfg_kw=None, **options):
     L, lib = lib_or_skip()
     base = dict(num_layers=2, hidden=256, heads=4, ffn=1024, seq_len=128, micro_batch=2, causal=1, dtype=L.RC_BF16,
