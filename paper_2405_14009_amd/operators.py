@@ -47,8 +47,8 @@ def _view(t, name, q, shape):
         if not isinstance(t, torch.Tensor) or t.dtype is not q.dtype or t.get_device() != q.get_device():
             _kind(t, name)
             raise ValueError(f"{name} must have the type and device of q")
-        if t.shape != shape:
-            raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     b, s, h, d = t.stride()
     if d != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the elements of a head must be contiguous")

@@ -648,3 +648,14 @@ def test_adamw_refuses_what_its_tensors_became():
     before, grads = state(opt), [x.cpu().double().numpy() for x in g]
     opt.step()
     check_adamw(opt, before, grads, 1.0, 2)
+
+
+def test_q_itself_as_another_tensor():
+    """q given as k and v is read as such; as v next to fewer key heads it has the wrong shape."""
+    q, do = normal(1, 2, 40, 4, 64), normal(2, 2, 40, 4, 64, std=0.1)
+    t = dict(q=q, k=q, v=q)
+    compare(t, do, run(t, do, window=9), window=9)
+    k = normal(3, 2, 40, 2, 64)
+    for kv in ((k, q), (q, k)):
+        with pytest.raises(ValueError):
+            ops().attention_forward(q, *kv)
