@@ -96,6 +96,14 @@ class RcAdamwTensor(ctypes.Structure):
                 ("count", ctypes.c_int64), ("grad_dtype", ctypes.c_int32), ("decay", ctypes.c_int32)]
 
 
+def whole(name: str, x, bits: int = 32) -> int:
+    """x as a whole number that a signed field of the library holds (ctypes would cut it off)."""
+    n = int(x)
+    if n != x or not -1 << (bits - 1) <= n < 1 << (bits - 1):
+        raise ValueError(f"{name} must be a whole number of {bits} bits, not {x}")
+    return n
+
+
 class RcError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"[{_NAMES.get(status, status)}] {msg}")

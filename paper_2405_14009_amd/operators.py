@@ -86,8 +86,9 @@ def _call(on, function, *args):
 @functools.lru_cache(maxsize=256)
 def _config(kind, batch, seq, heads, kv, d, causal, window, sinks, buckets, max_distance, bias_kind, scale):
     """A checked configuration, with the bytes of its saved and work memory."""
-    c = L.RcAttention(kind, batch, seq, heads, kv, d, causal, window, sinks, buckets, max_distance, bias_kind,
-                      scale)
+    names = ("batch", "seq_len", "heads", "kv_heads", "head_dim", "causal", "window", "sinks", "buckets", "max_distance")
+    sizes = [L.whole(*x) for x in zip(names, (batch, seq, heads, kv, d, causal, window, sinks, buckets, max_distance))]
+    c = L.RcAttention(kind, *sizes, bias_kind, scale)
     saved, work = ctypes.c_size_t(), ctypes.c_size_t()
     L.check(L.load().rc_attention_memory(ctypes.byref(c), ctypes.byref(saved), ctypes.byref(work)))
     return c, saved.value, work.value
@@ -127,9 +128,13 @@ class _Call:
             self.lengths = lengths.data_ptr()
         if scale is None:
             scale = 1.0 / math.sqrt(d) if d else 0.0
+        far = max_distance if buckets else 0
+        masks = int(window), int(sinks), int(far)
+        if masks != (window, sinks, far):
+            raise ValueError("window, sinks and max_distance must be whole numbers")
         self.c, self.saved_bytes, self.work_bytes = _config(
-            kind, batch, seq, heads, kv, d, 1 if causal else 0, int(window), int(sinks), buckets,
-            int(max_distance) if buckets else 0, bias_kind, float(scale))
+            kind, batch, seq, heads, kv, d, 1 if causal else 0, masks[0], masks[1], buckets, masks[2], bias_kind,
+            float(scale))
         self.q = _view(q, "q", q, shape)
         self.k, self.v = _view(k, "k", q, self.kv_shape), _view(v, "v", q, self.kv_shape)
         self.lib = L.load()
@@ -329,7 +334,7 @@ class AdamW:
     def step(self, grad_scale: float = 1.0, *, step: Optional[int] = None) -> None:
         """One step with grad_scale * grads, as step number `step` (by default one
         more than the last).  A captured step replays its own number."""
-        number = self.steps + 1 if step is None else int(step)
+        number = self.steps + 1 if step is None else L.whole("step", step, 64)
         self._refresh()
         if not self.params:
             self.steps = number

@@ -66,8 +66,10 @@ class Stage:
                                    ln_eps, max_stashed_mb,
                                    max_inflight_mb if max_inflight_mb is not None else max_stashed_mb)
         self.adam = L.RcAdamConfig(lr, beta1, beta2, eps, weight_decay)
-        self.options = L.RcStageOptions(window, sinks, rel_buckets, rel_max_distance if rel_buckets else 0,
-                                        adam_state_bits, 1 if static_work and not dry_run else 0)
+        self.options = L.RcStageOptions(
+            L.whole("window", window), L.whole("sinks", sinks), L.whole("rel_buckets", rel_buckets),
+            L.whole("rel_max_distance", rel_max_distance) if rel_buckets else 0,
+            L.whole("adam_state_bits", adam_state_bits), 1 if static_work and not dry_run else 0)
         self._rel_bias = (heads, rel_buckets)
         st, sh, wk = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
         L.check(self._lib.rc_stage_memory_requirements_with(

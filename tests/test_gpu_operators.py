@@ -659,3 +659,18 @@ def test_q_itself_as_another_tensor():
     for kv in ((k, q), (q, k)):
         with pytest.raises(ValueError):
             ops().attention_forward(q, *kv)
+
+
+def test_numbers_that_are_not_whole_or_too_large():
+    pkg, q = ops(), normal(1, 1, 40, 2, 32)
+    for kw in (dict(window=2.5), dict(window=7, sinks=0.5), dict(window=(1 << 32) + 5), dict(window=5, sinks=1 << 32),
+               dict(rel_bias=normal(2, 2, 8), max_distance=(1 << 32) + 64),
+               dict(rel_bias=normal(2, 2, 8), max_distance=64.5)):
+        with pytest.raises(ValueError):
+            pkg.attention_forward(q, q, q, **kw)
+    p = torch.zeros(8, device="cuda")
+    opt = pkg.AdamW([p], [torch.ones_like(p)])
+    for step in (2.5, (1 << 64) + 1, 1 << 63):
+        with pytest.raises(ValueError):
+            opt.step(step=step)
+    assert opt.steps == 0 and float(p.abs().sum()) == 0.0

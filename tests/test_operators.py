@@ -292,6 +292,30 @@ def test_stage_options_on_a_dry_run():
         plain.read(RC_READ_PARAM, 0, 12)
 
 
+@pytest.mark.parametrize("option", ["window", "sinks", "rel_buckets", "rel_max_distance", "adam_state_bits"])
+@pytest.mark.parametrize("beyond", [1 << 32, -(1 << 32), 1 << 31])
+def test_numbers_beyond_32_bits_are_refused(option, beyond):
+    """A number that the library's 32 bits would hold as another one."""
+    from paper_2405_14009_amd import Stage
+    kw = dict(num_layers=1, hidden=256, heads=4, ffn=1024, seq_len=128, micro_batch=2, dry_run=True)
+    good = dict(window=40, sinks=2, rel_buckets=16, rel_max_distance=50, adam_state_bits=8)
+    Stage(**kw, **good)
+    with pytest.raises(ValueError, match=option):
+        Stage(**kw, **{**good, option: good[option] + beyond})
+
+
+def test_attention_sizes_beyond_32_bits_are_refused():
+    from paper_2405_14009_amd import operators
+    L, _ = lib_or_skip()
+    names = ("batch", "seq_len", "heads", "kv_heads", "head_dim", "causal", "window", "sinks", "buckets", "max_distance")
+    good = (2, 300, 4, 2, 64, 1, 40, 3, 16, 50)
+    call = lambda sizes: operators._config(L.RC_BF16, *sizes, L.RC_FP32, 0.125)   # noqa: E731
+    assert call(good)[1] > 0
+    for i, name in enumerate(names):
+        with pytest.raises(ValueError, match=name):
+            call(good[:i] + (good[i] + (1 << 32),) + good[i + 1:])
+
+
 def test_buckets_by_their_definition():
     """The test's own bucket against the logarithms, away from their ties, and at the ties."""
     for causal, buckets, far in ((True, 32, 128), (False, 32, 128), (True, 16, 40), (False, 64, 512), (True, 2, 2)):
