@@ -6,7 +6,7 @@ Argument marshalling only: every step runs in the HIP library.  The calls
 enqueue on PyTorch's current stream of the tensors' device and take their
 outputs and scratch memory from PyTorch, so they may be captured into a graph.
 Autograd does not record them: a backward pass is a call of its own, as it is
-for a stage.
+for a stage, and a forward pass that autograd would have to record is refused.
 """
 from __future__ import annotations
 
@@ -152,7 +152,16 @@ def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: i
     `window` away (0: no window).  rel_bias: [heads, buckets], added to the
     scores by the bucket of the distance (the last one from about max_distance
     on).  scale: 1 / sqrt(d) unless given.  saved: what attention_backward needs,
-    None with save=False.  out: a tensor for o."""
+    None with save=False.  out: a tensor for o.
+
+    Tensors that require gradients are taken where autograd is off (no_grad, or
+    the forward of an autograd function): o has no graph."""
+    _import()
+    if torch.is_grad_enabled():
+        for name, t in (("q", q), ("k", k), ("v", v), ("rel_bias", rel_bias), ("out", out)):
+            if t is not None and getattr(t, "requires_grad", False):
+                raise RuntimeError(f"{name} requires gradients, which autograd does not pass through this call; "
+                                   "call it under torch.no_grad(), and attention_backward for them")
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
     on, stream = _on(q.device)
     o, ov = _new(q) if out is None else (out, _view(out, "out", q, c.shape))

@@ -674,3 +674,39 @@ def test_numbers_that_are_not_whole_or_too_large():
         with pytest.raises(ValueError):
             opt.step(step=step)
     assert opt.steps == 0 and float(p.abs().sum()) == 0.0
+
+
+def test_autograd_is_not_cut_silently():
+    """A call that autograd would have to record is refused; with autograd off, and in a
+    function of its own that calls the backward, it runs."""
+    t, do = inputs(1, 40, 2, 2, 32)
+    bias = normal(9, 2, 8)
+    how = dict(window=9, max_distance=16)
+    want = run(t, do, rel_bias=bias, **how)
+    leaves = [x.clone().requires_grad_() for x in (t["q"], t["k"], t["v"], bias)]
+    for i in range(4):
+        x = [leaf if i == j else leaf.detach() for j, leaf in enumerate(leaves)]
+        with pytest.raises(RuntimeError, match="gradients"):
+            ops().attention_forward(*x[:3], rel_bias=x[3], **how)
+    with pytest.raises(RuntimeError, match="out"):
+        ops().attention_forward(t["q"], t["k"], t["v"], out=torch.empty_like(t["q"]).requires_grad_())
+    with torch.no_grad():
+        o, _ = ops().attention_forward(*leaves[:3], rel_bias=leaves[3], **how)
+    assert torch.equal(o, want["o"]) and not o.requires_grad
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v, b):
+            o, saved = ops().attention_forward(q, k, v, rel_bias=b, **how)
+            ctx.save_for_backward(q, k, v, b, o, saved)
+            return o
+
+        @staticmethod
+        def backward(ctx, g):
+            q, k, v, b, o, saved = ctx.saved_tensors
+            return ops().attention_backward(g, q, k, v, o, saved, rel_bias=b, **how)
+
+    o = Attention.apply(*leaves)
+    got = torch.autograd.grad(o, leaves, do)
+    assert torch.equal(o, want["o"])
+    assert all(torch.equal(a, want[n]) for a, n in zip(got, ("dq", "dk", "dv", "dbias")))
