@@ -180,7 +180,8 @@ def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: 
     same arguments; dq, dk, dv: tensors for the gradients (all of their elements
     are written)."""
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
-    if not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device:
+    if (not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device
+            or saved.dtype is not torch.uint8 or not saved.is_contiguous()):
         raise ValueError("saved must be what attention_forward returned for these arguments")
     ov, dov = _view(o, "o", q, c.shape), _view(dout, "dout", q, c.shape)
     on, stream = _on(q.device)

@@ -710,3 +710,17 @@ def test_autograd_is_not_cut_silently():
     got = torch.autograd.grad(o, leaves, do)
     assert torch.equal(o, want["o"])
     assert all(torch.equal(a, want[n]) for a, n in zip(got, ("dq", "dk", "dv", "dbias")))
+
+
+def test_saved_is_what_the_forward_returned():
+    """As many elements of another type, or strided ones, are not those bytes."""
+    t, do = inputs(1, 40, 2, 2, 32)
+    o, saved = ops().attention_forward(t["q"], t["k"], t["v"])
+    wide = torch.empty(2 * saved.numel(), dtype=torch.uint8, device="cuda")
+    for bad in (saved.bool(), saved[:1].expand(saved.numel()), wide[::2], saved[:-1], saved.cpu()):
+        with pytest.raises(ValueError):
+            ops().attention_backward(do, t["q"], t["k"], t["v"], o, bad)
+    # a copy is (as a checkpointed activation is one)
+    a = ops().attention_backward(do, t["q"], t["k"], t["v"], o, saved)
+    b = ops().attention_backward(do, t["q"], t["k"], t["v"], o, saved.clone())
+    assert all(torch.equal(x, y) for x, y in zip(a[:3], b[:3]))
