@@ -827,9 +827,9 @@ struct AttnOp {
     }
   }
 
-  // acc += dS times the 32 keys from k (rows j of the tiles).  FINE (small grids,
-  // rows of few tokens): with what the rounding of dS drops, which there costs little
-  // and is not averaged over a row.
+  // acc += dS times the 32 keys from k (rows j of the tiles).  FINE (rows of few
+  // tokens): with what the rounding of dS drops, which there costs little and is not
+  // averaged over a row.
   template <bool FINE>
   static __device__ __forceinline__ void dq_block(f32x16 (&acc)[NB], const Queries& w, const Block& kt, const Block& vt,
                                                   int j, const Offs& of, int k, int q0, int qq, int lane, int len,
@@ -868,6 +868,7 @@ struct AttnOp {
     T::template outer<FINE>(acc, kt, j, dp, of, lane);
   }
 
+  template <bool FINE>
   static __device__ __forceinline__ void dq(const AttnOpArgs& p, char* lds) {
     float* const table = (float*)(lds + 2 * STAGE);
     const int lane = threadIdx.x & 63;
@@ -903,7 +904,7 @@ struct AttnOp {
       const int k0 = steps.tile(it) * 64;
 #pragma unroll 1
       for (int j = 0; j < 2; ++j)
-        dq_block<false>(acc, w, cur, cur + TILE, j, of, k0 + 32 * j, q0, qq, lane, len, table, sums, p);
+        dq_block<FINE>(acc, w, cur, cur + TILE, j, of, k0 + 32 * j, q0, qq, lane, len, table, sums, p);
     });
     if (qq >= len) {
 #pragma unroll
@@ -1061,12 +1062,13 @@ struct AttnOp {
       ((bf16*)p.dbias)[at] = (bf16)t;
   }
 
+  template <bool FINE>
   static __device__ __forceinline__ void dkv(const AttnOpArgs& p, char* lds) {
     const int bk = p.batch * p.kv_heads, z = blockIdx.x % bk, kb = blockIdx.x / bk;
     const int nkb = (p.s + 127) / 128 * p.parts, units = nkb + p.sink_rows / 32 * p.chunks * p.parts;
     if constexpr (BIAS)
       if (kb >= units) return dbias(p, blockIdx.x - units * bk, (float*)lds);
-    if (kb >= nkb) return dkv_sinks<false>(p, lds, z, kb - nkb);
+    if (kb >= nkb) return dkv_sinks<FINE>(p, lds, z, kb - nkb);
     const int part = kb % p.parts;
     float* const table = (float*)(lds + 2 * KSTAGE);
     const int lane = threadIdx.x & 63;
@@ -1118,7 +1120,7 @@ struct AttnOp {
       const float* vec = (const float*)(cur + 2 * TILE);
 #pragma unroll 1
       for (int j = 0; j < 2; ++j)
-        dkv_block<WINDOW, false>(dk, dv, kf, vf, cur, cur + TILE, j, vec + 32 * j, vec + 256 + 32 * j, vec + 512 + 32 * j, of,
+        dkv_block<WINDOW, FINE>(dk, dv, kf, vf, cur, cur + TILE, j, vec + 32 * j, vec + 256 + 32 * j, vec + 512 + 32 * j, of,
                           (t0 + tc) * 64 + 32 * j, k0, kk, lane, len, table, p);
       if (++tc == nt) tc = 0, ++gc;
     });
@@ -1322,18 +1324,18 @@ template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::FWAVES))) void attn_op_fwd32_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::template fwd32<FINE>(p, attn_op_lds);
 }
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::WAVES, T::WAVES))) void attn_op_dq_k(
     AttnOpArgs p) {
-  AttnOp<T, BIAS>::dq(p, attn_op_lds);
+  AttnOp<T, BIAS>::template dq<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::QWAVES))) void attn_op_dq32_k(AttnOpArgs p) {
   AttnOp<T, BIAS>::template dq32<FINE>(p, attn_op_lds);
 }
-template <class T, bool BIAS>
+template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::KWAVES, T::KWAVES))) void attn_op_dkv_k(AttnOpArgs p) {
-  AttnOp<T, BIAS>::dkv(p, attn_op_lds);
+  AttnOp<T, BIAS>::template dkv<FINE>(p, attn_op_lds);
 }
 template <class T, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::DWAVES))) void attn_op_dkv32_k(AttnOpArgs p) {
@@ -1341,9 +1343,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T::DWAVES))
 }
 
 constexpr size_t kLds = 160 * 1024;  // of a compute unit
-// Rows of so few tokens take the FINE kernels (rel-L2 of dq over that of its own
-// rounding, 142 tokens: 1.50 with the coarse forward, 1.46 with the fine one; 4
-// tokens: 1.9 with the coarse backward).
+// Rows of so few tokens, by the masks (sequences' lengths are on the device), take
+// the FINE kernels (rel-L2 of dq over that of its own rounding, 142 tokens: 1.50 with
+// the coarse forward, 1.46 with the fine one; 4 tokens: 1.4 to 1.9 with the coarse
+// backward, 1.0 with the fine one; us of dq and of dk and dv, coarse and fine: 4096
+// tokens, 32 heads of 128, window 4: 49, 51 and 62, 68; window 64: 50, 53 and 65, 73).
 constexpr int kSeenForward = 160, kSeenBackward = 64;
 constexpr size_t kTableMost = 4 * (2 * ATTN_OP_MAX_FAR + 192);
 
@@ -1363,32 +1367,36 @@ hipError_t attn_op_fwd_launch(const AttnOpArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <class T, bool BIAS, bool FINE>
+hipError_t attn_op_bwd_grids(const AttnOpArgs& a, bool sq, dim3 gq, bool sk, dim3 gk, hipStream_t st) {
+  using K = AttnOp<T, BIAS>;
+  if (sq)
+    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, FINE>), gq, dim3(256), K::dq_lds(a, true), st, a);
+  else if constexpr (!T::DIRECT)
+    hipLaunchKernelGGL((attn_op_dq_k<T, BIAS, FINE>), gq, dim3(256), K::dq_lds(a, false), st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (sk)
+    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, FINE>), gk, dim3(256), K::dkv_lds(a, true), st, a);
+  else if constexpr (!T::DIRECT)
+    hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS, FINE>), gk, dim3(256), K::dkv_lds(a, false), st, a);
+  return hipGetLastError();
+}
+
 template <class T, bool BIAS>
 hipError_t attn_op_bwd_launch(const AttnOpArgs& args, hipStream_t st) {
   AttnOpArgs a = args;
-  using K = AttnOp<T, BIAS>;
   const bool sq = T::DIRECT || a.split_q, sk = T::DIRECT || a.split_k;
   const long nq = (a.s + (sq ? 31 : 127)) / (sq ? 32 : 128), nk = (a.s + (sk ? 31 : 127)) / (sk ? 32 : 128);
   const dim3 gq((unsigned)(nq * a.batch * a.heads));
   const dim3 gk(
       (unsigned)((nk + (long)a.sink_rows / 32 * a.chunks) * a.parts * a.batch * a.kv_heads + (BIAS ? a.heads : 0)));
   a.bias_blocks = (int)nq;
-  const bool fine = T::REST && a.seen <= kSeenBackward;
-  if (sq && fine)
-    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, T::REST>), gq, dim3(256), K::dq_lds(a, true), st, a);
-  else if (sq)
-    hipLaunchKernelGGL((attn_op_dq32_k<T, BIAS, false>), gq, dim3(256), K::dq_lds(a, true), st, a);
-  else if constexpr (!T::DIRECT)
-    hipLaunchKernelGGL((attn_op_dq_k<T, BIAS>), gq, dim3(256), K::dq_lds(a, false), st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (sk && fine)
-    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, T::REST>), gk, dim3(256), K::dkv_lds(a, true), st, a);
-  else if (sk)
-    hipLaunchKernelGGL((attn_op_dkv32_k<T, BIAS, false>), gk, dim3(256), K::dkv_lds(a, true), st, a);
-  else if constexpr (!T::DIRECT)
-    hipLaunchKernelGGL((attn_op_dkv_k<T, BIAS>), gk, dim3(256), K::dkv_lds(a, false), st, a);
-  e = hipGetLastError();
+  hipError_t e;
+  if (T::REST && a.seen <= kSeenBackward)
+    e = attn_op_bwd_grids<T, BIAS, T::REST>(a, sq, gq, sk, gk, st);
+  else
+    e = attn_op_bwd_grids<T, BIAS, false>(a, sq, gq, sk, gk, st);
   if (e != hipSuccess || (!a.chunks && a.parts == 1)) return e;
   const long rows = a.parts > 1 || a.sink_rows > a.s ? a.s : a.sink_rows;
   hipLaunchKernelGGL((attn_op_sum_k<T>), dim3((unsigned)((rows + 7) / 8 * a.batch * a.kv_heads)), dim3(256), 0, st, a);
