@@ -472,8 +472,9 @@ typedef struct rc_attention {
 } rc_attention;
 
 /* Bytes of `saved` (written by the forward for the backward: row statistics
- * and, bf16, what the rounding of o drops) and of the backward's `work`; both
- * are 256-byte aligned.  Host only.  Errors: RC_ERR_INVALID_ARG, RC_ERR_UNSUPPORTED. */
+ * and, bf16, what the rounding of o drops) and of the backward's `work` (row
+ * terms, and fp32 shares: of dk and dv where few workgroups form them, of the
+ * sinks' rows of dk and dv, of the bias gradient); both are 256-byte aligned.  Host only.  Errors: RC_ERR_INVALID_ARG, RC_ERR_UNSUPPORTED. */
 rc_status rc_attention_memory(const rc_attention* a, size_t* saved_bytes, size_t* work_bytes);
 
 /* o = attention(q, k, v).  bias: device [heads, buckets] (NULL without).

@@ -123,6 +123,12 @@ void attn_op_plan(AttnOpArgs& a, int elt, int window, int max_distance) {
   const long span = std::min((long)a.s, (long)a.left + a.right + keys);
   a.parts = span * a.group >= 512 ? (int)std::max(1L, std::min((long)a.group, most / units)) : 1;
   a.part_rows = (a.s + 127) / 128 * 128;
+  // No more chunks than 1024 workgroups take: each writes a share of dk and dv of its
+  // rows.  (us of dk and dv and their shares' sum, and bytes of work memory, with 16 chunks
+  // whatever the sinks and so: 8192 tokens, 32 heads of 128, window 512, 512 sinks:
+  // 737 and 0.29 GB, 502 and 0.05; 8000 sinks: 5767 and 4.46 GB, 2080 and 0.53.)
+  const long sink_units = (long)a.sink_rows / 32 * a.batch * a.kv_heads * a.parts;
+  while (a.chunk_len < a.s && sink_units * sink_chunks(a) > 1024) a.chunk_len *= 2;
   a.chunks = a.sinks && !(a.split_k && a.s <= a.chunk_len) ? sink_chunks(a) : 0;
 }
 

@@ -745,3 +745,18 @@ def test_rows_of_few_tokens(b, s, h, kv, d, causal, window, buckets):
                            max_distance=16)
     share = {n: float((got[n].cpu().double() - out[n]).norm() / (out[n].to(BF16).double() - out[n]).norm()) for n in got}
     assert all(x < 1.1 for x in share.values()), share
+
+
+# Sinks whose workgroups are many: their queries in fewer chunks, or in one.
+MANY_SINKS = [
+    (7, 600, 8, 8, 32, True, 50, 300, 0, 0, None),
+    (2, 1100, 8, 8, 64, True, 70, 700, 8, 30, (1100, 801)),
+    (2, 1100, 8, 8, 128, False, 40, 700, 0, 0, None),
+    (7, 600, 16, 8, 40, False, 50, 500, 0, 0, (600, 550, 480, 1, 0, 64, 333)),
+]
+
+
+@pytest.mark.parametrize("kind", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", MANY_SINKS, ids=lambda c: "-".join(str(x) for x in c[:10]))
+def test_many_sinks(case, kind):
+    test_attention(case, kind)

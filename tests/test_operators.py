@@ -105,6 +105,20 @@ def test_attention_takes_the_most_blocks_of_a_launch():
     assert memory(seq_len=128, batch=(1 << 24) - 2, heads=1, kv_heads=1)[0] == 0
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("batch,seq,heads,kv,d", [(1, 8192, 32, 32, 128), (1, 8192, 32, 8, 128), (16, 2048, 16, 16, 64)])
+def test_attention_memory_of_many_sinks(bf16, batch, seq, heads, kv, d):
+    """The shares of the sinks' rows: two of each row, or as many as 1024 workgroups of 32 rows write."""
+    L, _ = lib_or_skip()
+    size = dict(dtype=L.RC_BF16 if bf16 else L.RC_FP32, batch=batch, seq_len=seq, heads=heads, kv_heads=kv, head_dim=d,
+                window=512)
+    plain = memory(**size)[2]
+    for sinks in (1, 4, 33, 512, 1500, seq - 192):
+        rows = -(-sinks // 32) * 32
+        share = memory(**size, sinks=sinks)[2] - plain
+        assert 0 < share <= 4 * 2 * d * (batch * kv * rows + max(1024 * 32, batch * heads * rows)) + 256, (sinks, share)
+
+
 @pytest.mark.parametrize("seq,heads,batch,masks", [
     (1, 1, (1 << 24) - 2, {}),
     (32, 2, (1 << 23) - 2, {}),      # a launch may have a workgroup more per head (the bias gradient)
