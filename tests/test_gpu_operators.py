@@ -760,3 +760,27 @@ MANY_SINKS = [
 @pytest.mark.parametrize("case", MANY_SINKS, ids=lambda c: "-".join(str(x) for x in c[:10]))
 def test_many_sinks(case, kind):
     test_attention(case, kind)
+
+
+@pytest.mark.parametrize("grad_kind", [F32, BF16], ids=["f32", "bf16"])
+def test_adamw_8_bit_codes_bit_by_bit(grad_kind):
+    """Every bit of the codes: second moments have no sign, so 0 and 128, or 127 and 255 (not
+    a number), are not alike; first moments may differ in the sign of a zero alone."""
+    rng = np.random.RandomState(5)
+    g = [rng.randn(1000) * 1e-3, np.ldexp(rng.randn(700), rng.randint(-40, 20, 700)), rng.randn(300) * 1e30,
+         np.where(rng.rand(500) < 0.5, 0.0, rng.randn(500))]
+    g[1][[3, 200, 500]], g[2][7] = (np.nan, np.inf, -np.inf), 0.0
+    grads = [torch.from_numpy(x).float().to(grad_kind).cuda() for x in g]
+    opt = ops().AdamW([torch.zeros(x.size, device="cuda") for x in g], grads, state_bits=8)
+    for step in (1, 2, 3):
+        before = state(opt)
+        opt.step(step=step)
+        for i, (p0, m0, v0) in enumerate(before):
+            with np.errstate(invalid="ignore"):
+                _, m, v = ref.adamw(p0, grads[i].cpu().double().numpy(), m0, v0, step=step, decay=True)
+            (wm, ws), (wv, wvs) = ref.encode_m(m), ref.encode_v(v)
+            assert np.array_equal(opt.exp_avg_sq[i].cpu().numpy(), wv), (step, i)
+            assert np.array_equal(opt.exp_avg_sq_scale[i].cpu().numpy(), wvs), (step, i)
+            assert np.array_equal(opt.exp_avg_scale[i].cpu().numpy(), ws), (step, i)
+            c = opt.exp_avg[i].cpu().numpy()
+            assert np.all((c == wm) | (c | wm == 128)), (step, i)

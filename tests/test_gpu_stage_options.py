@@ -219,3 +219,29 @@ def test_window_stage_in_a_graph():
             eager.optimizer_skip()
             side.synchronize()
             assert torch.equal(y, want_y) and torch.equal(dx, want_dx), turn
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_the_step_after_a_rollback(bits):
+    """Back from a step, a stage computes with the parameters that it reads out (its bf16 copies
+    are theirs), and its next step is that of its state before: the right bank and number."""
+    from paper_2405_14009_amd import RC_READ_ADAM_M, RC_READ_ADAM_V, RC_READ_PARAM
+    cfg = get_config("small_bf16").with_(n_mb=1, layers=1)
+    kw = dict(window=70, sinks=3, rel_max_distance=50, adam_state_bits=bits)
+    st, mbs = make(cfg, 16, **kw), [(0, 0)]
+    for step in (1, 2, 3):
+        train(st, cfg, mbs)
+        st.optimizer_step(0.5)
+        st.optimizer_rollback()
+        before = (st.read_all(RC_READ_PARAM), moments8(st, RC_READ_ADAM_M), moments8(st, RC_READ_ADAM_V))
+        y, dx, grads = train(st, cfg, mbs)
+        other = make(cfg, 16, **kw)
+        other.load_params(before[0])
+        y2, dx2, grads2 = train(other, cfg, mbs)
+        assert np.array_equal(y[mbs[0]], y2[mbs[0]]) and np.array_equal(dx[mbs[0]], dx2[mbs[0]])
+        assert all(np.array_equal(a, b) for a, b in zip(grads[0], grads2[0]))
+        other.close()
+        st.optimizer_step(0.5)
+        if bits == 8:
+            check_step8(st, before, grads, 0.5, step)
+    st.close()
