@@ -282,6 +282,24 @@ class AdamW:
                 and all(map(Tensor.is_contiguous, self.params))):
             self._look()
 
+    def _check_list(self, name, tensors, types, counts, places=None) -> None:
+        """Refuses a list that is not one of contiguous tensors of these types and sizes (all of
+        them at once, which takes a third of the time of one by one).  places: their numbers."""
+        Tensor = torch.Tensor
+        if len(tensors) != len(counts):
+            raise ValueError(f"{name} must have {len(counts)} entries")
+        if (all(issubclass(x, Tensor) for x in set(map(type, tensors)))
+                and set(map(Tensor.get_device, tensors)) <= {self._index}
+                and {t.dtype for t in tensors} <= set(types) and list(map(Tensor.numel, tensors)) == counts
+                and all(map(Tensor.is_contiguous, tensors))):
+            return
+        for i, t, count in zip(places or range(len(counts)), tensors, counts):
+            if not isinstance(t, Tensor) or t.device != self.device:
+                raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
+            if t.dtype not in types or t.numel() != count or not t.is_contiguous():
+                raise ValueError(f"{name}[{i}] must be a contiguous tensor of {count} elements of "
+                                 f"{' or '.join(str(x) for x in types)}")
+
     def _look(self) -> None:
         """Checks the tensors and writes their addresses down."""
         n, state_bits = len(self.params), self.state_bits
@@ -291,54 +309,48 @@ class AdamW:
         self.device = self.params[0].device if n else None
         self._index = self.device.index if n else None
         self._counts = [p.numel() for p in self.params]
-
-        def pointer(lists, i, name, types, count):
-            if len(lists) != n:
-                raise ValueError(f"{name} must have {n} entries")
-            t = lists[i]
-            if not isinstance(t, torch.Tensor) or t.device != self.device:
-                raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
-            if t.dtype not in types or t.numel() != count or not t.is_contiguous():
-                raise ValueError(f"{name}[{i}] must be a contiguous tensor of {count} elements of "
-                                 f"{' or '.join(str(x) for x in types)}")
-            return t.data_ptr()
-
         if len(self.decay) != n or len(self.copies) != n or len(self.grads) != n:
             raise ValueError(f"grads, decay and copies must have {n} entries")
-        self._tensors = (L.RcAdamwTensor * max(1, n))()
         f32, bf16 = torch.float32, torch.bfloat16
-        for i in range(n):
-            t, count = self._tensors[i], self.params[i].numel()
-            t.param = pointer(self.params, i, "params", (f32,), count)
-            t.grad = pointer(self.grads, i, "grads", (f32, bf16), count)
-            t.exp_avg = pointer(self.exp_avg, i, "exp_avg", (kind,), count)
-            t.exp_avg_sq = pointer(self.exp_avg_sq, i, "exp_avg_sq", (kind,), count)
-            if state_bits == 8:
-                t.exp_avg_scale = pointer(self.exp_avg_scale, i, "exp_avg_scale", (kind,), _blocks(count))
-                t.exp_avg_sq_scale = pointer(self.exp_avg_sq_scale, i, "exp_avg_sq_scale", (kind,), _blocks(count))
-            if self.copies[i] is not None:
-                t.copy = pointer(self.copies, i, "copies", (bf16,), count)
-            t.count, t.decay = count, bool(self.decay[i])
-            t.grad_dtype = L.RC_BF16 if self.grads[i].dtype == bf16 else L.RC_FP32
-        written = (self.params, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale or (), self.exp_avg_sq_scale or (),
-                   self.copies)
-        # (first byte, byte behind the last one, whether a step writes them)
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w)
-                       for w, lists in ((True, written), (False, (self.grads,)))
-                       for tensors in lists for t in tensors if t is not None and t.numel())
+        each, at = self._counts, [i for i in range(n) if self.copies[i] is not None]
+        blocks = [_blocks(count) for count in each] if state_bits == 8 else []
+        # per list: tensors, their types and sizes, whether a step writes them
+        lists = {"params": (self.params, (f32,), each, True), "grads": (self.grads, (f32, bf16), each, False),
+                 "exp_avg": (self.exp_avg, (kind,), each, True), "exp_avg_sq": (self.exp_avg_sq, (kind,), each, True),
+                 "copies": ([self.copies[i] for i in at], (bf16,), [each[i] for i in at], True)}
+        if state_bits == 8:
+            lists["exp_avg_scale"] = (self.exp_avg_scale, (kind,), blocks, True)
+            lists["exp_avg_sq_scale"] = (self.exp_avg_sq_scale, (kind,), blocks, True)
+        addresses, spans = {}, []
+        for name, (tensors, types, counts, w) in lists.items():
+            self._check_list(name, tensors, types, counts, at if name == "copies" else None)
+            addresses[name] = first = list(map(torch.Tensor.data_ptr, tensors))
+            sizes = map(torch.Tensor.element_size, tensors)
+            # (first byte, byte behind the last one, whether a step writes them)
+            spans += [(x, x + c * e, w) for x, c, e in zip(first, counts, sizes) if c]
+        spans.sort()
         end, write_end = 0, 0
         for first, last, w in spans:
             if first < (end if w else write_end):
                 raise ValueError("a tensor that a step writes is listed twice or overlaps another one")
-            end = max(end, last)
-            write_end = max(write_end, last) if w else write_end
+            if last > end:
+                end = last
+            if w and last > write_end:
+                write_end = last
+        scales = zip(addresses["exp_avg_scale"], addresses["exp_avg_sq_scale"]) if state_bits == 8 else ((None, None),) * n
+        copies = dict(zip(at, addresses["copies"]))
+        self._tensors = (L.RcAdamwTensor * max(1, n))(*[
+            (p, g, m, v, ms, vs, copies.get(i), count, L.RC_BF16 if grad.dtype is bf16 else L.RC_FP32, bool(decay))
+            for i, (p, g, m, v, (ms, vs), count, grad, decay) in enumerate(zip(
+                addresses["params"], addresses["grads"], addresses["exp_avg"], addresses["exp_avg_sq"], scales, each,
+                self.grads, self.decay))])
         self._decay, self._no_copy = list(self.decay), [c is None for c in self.copies]
         self._seen = self._others()
-        self._addresses = [t.data_ptr() for t in self._seen]
+        self._addresses = list(map(torch.Tensor.data_ptr, self._seen))
         # a tensor of our own for each storage that holds moments: it stays while we write to it
         moments = self._moments()
         self._kept = list({t.untyped_storage().data_ptr(): t.detach() for t in moments if t.numel()}.values())
-        self._kept_at = [t.data_ptr() for t in self._kept]
+        self._kept_at = list(map(torch.Tensor.data_ptr, self._kept))
         self._seen_moments = moments
 
     def step(self, grad_scale: float = 1.0, *, step: Optional[int] = None) -> None:
@@ -354,15 +366,6 @@ class AdamW:
               self.state_bits, number, float(grad_scale), stream)
         self.steps = number
 
-    def _are_values(self, tensors, count=None) -> bool:
-        """Whether moments can be written to them (all at once: a third of the time of one by one)."""
-        f32, Tensor = torch.float32, torch.Tensor
-        return (all(issubclass(x, Tensor) for x in set(map(type, tensors)))
-                and set(map(Tensor.get_device, tensors)) <= {self._index}
-                and [t.dtype for t in tensors].count(f32) == len(tensors)
-                and list(map(Tensor.numel, tensors)) == (self._counts if count is None else [count])
-                and all(map(Tensor.is_contiguous, tensors)))
-
     def moments(self, out=None):
         """The moments as fp32 values: (exp_avg, exp_avg_sq), lists of tensors, by
         tensor.  out: two such lists to fill (contiguous fp32 tensors of the sizes)."""
@@ -374,14 +377,7 @@ class AdamW:
         n = len(self._counts)
         arrays = []
         for name, tensors in zip(("exp_avg", "exp_avg_sq"), out):
-            if len(tensors) != n:
-                raise ValueError(f"{name} must have {n} entries")
-            if not self._are_values(tensors):
-                for i, (t, count) in enumerate(zip(tensors, self._counts)):
-                    if not isinstance(t, torch.Tensor) or t.device != self.device:
-                        raise TypeError(f"{name}[{i}] must be a tensor on {self.device}")
-                    if not self._are_values([t], count):
-                        raise ValueError(f"{name}[{i}] must be a contiguous float32 tensor of {count} elements")
+            self._check_list(name, tensors, (torch.float32,), self._counts)
             arrays.append((ctypes.c_void_p * max(1, n))(*map(torch.Tensor.data_ptr, tensors)))
         if n:
             on, stream = _on(self.device)
