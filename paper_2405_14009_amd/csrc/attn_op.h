@@ -47,8 +47,8 @@ struct AttnOpArgs {
   // Every query sees the sinks.  Their keys (sink_rows: up to a multiple of 32)
   // are handled twice: with the other keys for the queries whose window holds
   // them, and by workgroups of 32 keys and chunk_len queries for the others; the
-  // shares of dK and dV are added up afterwards.  (chunks 0: short sequences;
-  // the sinks' own block visits every query.)
+  // shares of dK and dV are added up afterwards.  (chunks 0: one chunk would do and
+  // blocks are of 32 keys; the sinks' own block visits every query.)
   float* spart;
   int sink_rows, chunks, chunk_len;
   // The heads of a key head in `parts` workgroups of the dk and dv kernel where

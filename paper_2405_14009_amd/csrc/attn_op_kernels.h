@@ -30,11 +30,13 @@
 // is exactly one and dS exactly zero.
 //
 // us, forward / dq / dk and dv: 32 heads of 128, s 2048, causal, 32 buckets: 77 /
-// 104 / 114; 32 and 8 heads of 128, s 8192, window 1024: 191 / 260 / 395; 16 heads
+// 104 / 114; 32 and 8 heads of 128, s 8192, window 1024: 197 / 263 / 393; 16 heads
 // of 64, 8 sequences of 512, both directions, 32 buckets: 26 / 41 / 29.  The matrix cores are busy
-// for 26 to 42 % of the cycles: LDS reads (transposed ones run at half the rate)
-// and vector work take as long, and dk and dv at 128 columns have one wave a SIMD
-// to overlap them (two waves, with half of the columns each, read LDS twice: 518).
+// for 26 to 43 % of the cycles, vector instructions issue in 18 to 32 % of a wave's
+// cycles and LDS ones in 4 to 9 %: no unit is full.  The rest goes to waits (for LDS data,
+// of which transposed reads come at half the rate, and for tiles at the barriers)
+// that one or two waves a SIMD do not cover; dk and dv at 128 columns have one
+// (two, with half of the columns each, read LDS twice: 518).
 // Blocks of 128 rows on one side keep the other side's reads from memory small;
 // grids that would leave compute units empty split further (attn_op.h).
 #pragma once
@@ -552,7 +554,7 @@ struct AttnOp {
   // gradient sums it over the far bucket, which holds most of a long row
   // (2133 tokens, both directions, 8 buckets: 4.1e-3, against 1.7e-3).  There the
   // forward also adds what the rounding drops (FINE; us, 32 heads of 128, s 2048, with
-  // a bias: 68 -> 79).
+  // a bias: 65 -> 78).
   template <bool FINE>
   static __device__ __forceinline__ void fwd_tile(Fwd& st, const Rows& qf, const char* kt, const char* vt, const Offs& of,
                                                   int k0, int q0, int qq, int lane, int len, const float* table,
