@@ -542,6 +542,134 @@ rc_status rc_adamw_step(const rc_adamw_tensor* tensors, int32_t n, const rc_adam
 rc_status rc_adamw_read(const rc_adamw_tensor* tensors, int32_t n, int32_t state_bits,
                         float* const* exp_avg, float* const* exp_avg_sq, void* hip_stream);
 
+/* ---- The other operators of a layer ------------------------------------- */
+
+/* A [rows, cols] matrix: columns contiguous, rows row_stride elements apart (an
+ * input's rows may share their memory).  data and row_stride need only the
+ * alignment of their elements, unless an operator says more.  Where an operator
+ * takes a matrix or leaves it out, NULL or a null data leaves it out. */
+typedef struct rc_matrix {
+  void* data;
+  int64_t row_stride;
+} rc_matrix;
+
+/* Dropout, D below.  Element (row, column) of a call is kept when its 16-bit
+ * number is at least t = p 2^16 (rounded to nearest), and then multiplied by
+ * 2^16 / (2^16 - t); the others become 0, whatever they held.  (So p counts in
+ * steps of 2^-16, and the expected value is kept exactly.)  The numbers of columns
+ * 8 g .. 8 g + 7 are the halves, low ones first, of the four words that
+ * Philox4x32-10 makes of the counter (g, row, low and high word of the offset)
+ * under the key (low, high word of seed): no mask is stored, and calls with the
+ * same seed and offset draw the same one.  A program gives each use of its own an
+ * offset of its own (step times uses a step, plus the use), and its backward pass
+ * the same.  step: a device pointer to a number that is added to offset when the
+ * kernel runs (a captured graph then draws another mask at each replay), or NULL. */
+typedef struct rc_dropout {
+  float p;              /* 0 .. 1 */
+  int32_t reserved;     /* 0 */
+  uint64_t seed, offset;
+  const uint64_t* step;
+} rc_dropout;
+
+/* The sizes and types of a call over rows.  rows 0 .. 2^31 - 1, cols 1 .. 2^30. */
+typedef struct rc_rows {
+  int32_t dtype;        /* rc_dtype of the matrices */
+  int32_t param_dtype;  /* rc_dtype of the vectors of parameters; their gradients are fp32 */
+  int64_t rows, cols;
+} rc_rows;
+
+/* For all calls of this section: sums, statistics and gradients of parameters
+ * are fp32, summed in a fixed order (results are bitwise reproducible); each
+ * output is rounded once.  accumulate = 1 adds a parameter's gradient to what is
+ * there (several micro-batches, a deferred weight pass), 0 overwrites it.  No
+ * output overlaps another tensor of the call.  work: device memory of the bytes
+ * that the operator's _memory call names, 256-byte aligned (NULL for 0 bytes). */
+
+/* y = residual + D(x + bias); bias [cols] and residual may be NULL. */
+rc_status rc_dropout_forward(const rc_rows* r, const rc_dropout* drop, const rc_matrix* x,
+                             const void* bias, const rc_matrix* residual, const rc_matrix* y,
+                             void* hip_stream);
+
+/* dx = D(dy) * derivative (NULL: 1; the stored derivative of an activation that
+ * the elements went through before the dropout, see rc_linear_forward), and, if
+ * dbias is given, dbias[cols] = its column sums, before rounding.  With p = 0 this
+ * is the gradient of an activation or of a bias alone.  dx may be NULL (the sums
+ * alone).  The gradient of residual is dy. */
+rc_status rc_dropout_memory(const rc_rows* r, size_t* work_bytes);
+rc_status rc_dropout_backward(const rc_rows* r, const rc_dropout* drop, const rc_matrix* dy,
+                              const rc_matrix* derivative, const rc_matrix* dx, float* dbias,
+                              int32_t accumulate, void* work, void* hip_stream);
+
+/* Layer norm of total = residual + D(x + in_bias), rounded to its type:
+ * y = (total - mean) / sqrt(variance + eps) * weight + bias, over each row.
+ * in_bias, drop, residual, weight and bias may be NULL; where none of the first
+ * three is given, total is x and must be NULL.  stats: fp32 [2][rows] for the
+ * backward pass (means, then 1 / sqrt(variance + eps)), or NULL.  cols at most
+ * 16384 (otherwise RC_ERR_UNSUPPORTED). */
+rc_status rc_layer_norm_forward(const rc_rows* r, float eps, const rc_dropout* drop,
+                                const rc_matrix* x, const void* in_bias, const rc_matrix* residual,
+                                const void* weight, const void* bias, const rc_matrix* total,
+                                const rc_matrix* y, float* stats, void* hip_stream);
+
+/* Gradients from dy and, where total goes on (as the next residual), dtotal_in
+ * (NULL: none): dtotal = dtotal_in + the norm's gradient, which is also that of
+ * residual, dx = D(dtotal), and the sums dweight, dbias and din_bias (of the
+ * unrounded dx).  total is the forward's (x where there was none).  Each output
+ * may be NULL: a call for dtotal and dx alone and one for the parameters alone,
+ * later, give what one call for all of them gives.  Without drop, dx is dtotal. */
+rc_status rc_layer_norm_memory(const rc_rows* r, size_t* work_bytes);
+rc_status rc_layer_norm_backward(const rc_rows* r, const rc_dropout* drop, const rc_matrix* dy,
+                                 const rc_matrix* dtotal_in, const rc_matrix* total,
+                                 const float* stats, const void* weight, const rc_matrix* dtotal,
+                                 const rc_matrix* dx, float* dweight, float* dbias, float* din_bias,
+                                 int32_t accumulate, void* work, void* hip_stream);
+
+/* Activations of a linear layer; GELU is its tanh form. */
+enum { RC_ACT_NONE = 0, RC_ACT_GELU = 1, RC_ACT_RELU = 2, RC_ACT_SILU = 3 };
+
+/* A linear layer y = act(x W + bias) + residual on the matrix cores (fp32: fp32
+ * products).  weight is stored [in, out] (by_out 0) or [out, in] (by_out 1); its
+ * gradient has the same layout, without gaps.  Its backward pass comes in two
+ * calls, as a stage's does: the input's gradient, and the parameters', which may
+ * be deferred.
+ *
+ * Requirements (otherwise RC_ERR_UNSUPPORTED): in and out multiples of 8; bf16: the
+ * weight spans less than 2^31 bytes, row strides below 2^21 elements.  data and row strides of all matrices are
+ * multiples of 16 bytes, dweight is 16-byte aligned. */
+typedef struct rc_linear {
+  int32_t dtype;        /* rc_dtype of the matrices */
+  int32_t bias_dtype;   /* rc_dtype of bias; gradients of weight and bias are fp32 */
+  int64_t rows;         /* 0 .. 2^31 - 1 */
+  int32_t in, out;
+  int32_t activation;   /* RC_ACT_* */
+  int32_t by_out;
+} rc_linear;
+
+/* Work memory of the three calls (an output may be NULL; weight_work is for a
+ * call with a bias gradient). */
+rc_status rc_linear_memory(const rc_linear* l, size_t* forward_work, size_t* input_work,
+                           size_t* weight_work);
+
+/* bias and residual may be NULL.  derivative: [rows, out], the activation's at
+ * x W + bias, for the backward pass, or NULL (always without an activation). */
+rc_status rc_linear_forward(const rc_linear* l, const rc_matrix* x, const rc_matrix* weight,
+                            const void* bias, const rc_matrix* residual, const rc_matrix* y,
+                            const rc_matrix* derivative, void* work, void* hip_stream);
+
+/* dx = (dy W^T) * before.  dy is the gradient at x W + bias: with an activation,
+ * its gradient times the stored derivative, which the call of the layer that took
+ * y as its input has formed already if that derivative was its `before`
+ * (rc_dropout_backward forms it elsewhere).  before: the derivative of the
+ * activation that made x, or NULL. */
+rc_status rc_linear_backward_input(const rc_linear* l, const rc_matrix* dy, const rc_matrix* weight,
+                                   const rc_matrix* before, const rc_matrix* dx, void* work,
+                                   void* hip_stream);
+
+/* dweight = x^T dy (or its transpose, by_out), and dbias = column sums of dy (NULL: not formed). */
+rc_status rc_linear_backward_weight(const rc_linear* l, const rc_matrix* x, const rc_matrix* dy,
+                                    float* dweight, float* dbias, int32_t accumulate, void* work,
+                                    void* hip_stream);
+
 /* ---- Schedule side (host only, no device work) ------------------------- */
 
 /* Failure Normalization (section 4.2.1, Algorithm 1): assign `failures`

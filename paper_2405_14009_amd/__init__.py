@@ -11,4 +11,8 @@ from ._lib import (  # noqa: F401
     RC_READ_PARAM, LIB_PATH, load,
 )
 from .operators import AdamW, attention_backward, attention_forward  # noqa: F401
+from .layer_operators import (  # noqa: F401
+    Dropout, NormGradients, dropout_backward, dropout_forward, layer_norm_backward, layer_norm_forward,
+    linear_backward_input, linear_backward_weight, linear_forward,
+)
 from .stage import PARAM_NAMES, Stage, param_shape  # noqa: F401

@@ -17,6 +17,7 @@ RC_OP_F, RC_OP_B, RC_OP_W, RC_OP_STEP, RC_OP_SKIP, RC_OP_ROLLBACK = 0, 1, 2, 3, 
 RC_READ_PARAM, RC_READ_GRAD, RC_READ_ADAM_M, RC_READ_ADAM_V = 0, 1, 2, 3
 RC_NUM_PARAMS, RC_P_REL_BIAS = 12, 12
 RC_ATTN_MATERIALISED, RC_ATTN_BLOCK, RC_ATTN_PAIRED, RC_ATTN_SPLIT, RC_ATTN_OPERATOR = 0, 1, 2, 3, 4
+RC_ACT_NONE, RC_ACT_GELU, RC_ACT_RELU, RC_ACT_SILU = 0, 1, 2, 3
 RC_STATIC_WORK_BYTES = 96 * 1024 * 1024
 
 # Every symbol the header declares, for load checks.
@@ -30,6 +31,9 @@ EXPORTED = (
     "rc_stage_synchronize", "rc_stage_profile_enable", "rc_stage_profile_read", "rc_last_error",
     "rc_failure_normalization", "rc_schedule_simulate",
     "rc_attention_memory", "rc_attention_forward", "rc_attention_backward", "rc_adamw_step",
+    "rc_dropout_memory", "rc_dropout_forward", "rc_dropout_backward", "rc_layer_norm_memory",
+    "rc_layer_norm_forward", "rc_layer_norm_backward", "rc_linear_memory", "rc_linear_forward",
+    "rc_linear_backward_input", "rc_linear_backward_weight",
     "rc_adamw_read", "rc_stage_memory_requirements_with", "rc_stage_create_with",
 )
 
@@ -96,6 +100,26 @@ class RcAdamwTensor(ctypes.Structure):
                 ("count", ctypes.c_int64), ("grad_dtype", ctypes.c_int32), ("decay", ctypes.c_int32)]
 
 
+class RcMatrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class RcDropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("reserved", ctypes.c_int32), ("seed", ctypes.c_uint64),
+                ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class RcRows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("param_dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64)]
+
+
+class RcLinear(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("bias_dtype", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("in_", ctypes.c_int32), ("out", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("by_out", ctypes.c_int32)]
+
+
 def whole(name: str, x, bits: int = 32) -> int:
     """x as a whole number that a signed field of the library holds (ctypes would cut it off)."""
     n = int(x)
@@ -139,6 +163,8 @@ def load() -> ctypes.CDLL:
     cfgp = ctypes.POINTER(RcStageConfig)
     sz = ctypes.POINTER(ctypes.c_size_t)
     view = ctypes.POINTER(RcView)
+    mat, drop = ctypes.POINTER(RcMatrix), ctypes.POINTER(RcDropout)
+    rows, lin = ctypes.POINTER(RcRows), ctypes.POINTER(RcLinear)
     sig = {
         "rc_stage_memory_requirements": [cfgp, sz, sz, sz],
         "rc_stage_create": [cfgp, ctypes.POINTER(RcAdamConfig), I32, I32, P, P, P, P,
@@ -175,6 +201,16 @@ def load() -> ctypes.CDLL:
         "rc_stage_memory_requirements_with": [cfgp, ctypes.POINTER(RcStageOptions), sz, sz, sz],
         "rc_stage_create_with": [cfgp, ctypes.POINTER(RcStageOptions), ctypes.POINTER(RcAdamConfig), I32, I32, P,
                                  P, P, P, ctypes.POINTER(P)],
+        "rc_dropout_memory": [rows, sz],
+        "rc_dropout_forward": [rows, drop, mat, P, mat, mat, P],
+        "rc_dropout_backward": [rows, drop, mat, mat, mat, P, I32, P, P],
+        "rc_layer_norm_memory": [rows, sz],
+        "rc_layer_norm_forward": [rows, F32, drop, mat, P, mat, P, P, mat, mat, P, P],
+        "rc_layer_norm_backward": [rows, drop, mat, mat, mat, P, P, mat, mat, P, P, P, I32, P, P],
+        "rc_linear_memory": [lin, sz, sz, sz],
+        "rc_linear_forward": [lin, mat, mat, P, mat, mat, mat, P, P],
+        "rc_linear_backward_input": [lin, mat, mat, mat, mat, P, P],
+        "rc_linear_backward_weight": [lin, mat, mat, P, P, I32, P, P],
         "rc_adamw_read": [ctypes.POINTER(RcAdamwTensor), I32, I32, ctypes.POINTER(P), ctypes.POINTER(P), P],
         "rc_adamw_step": [ctypes.POINTER(RcAdamwTensor), I32, ctypes.POINTER(RcAdamConfig), I32,
                           ctypes.c_int64, F32, P],

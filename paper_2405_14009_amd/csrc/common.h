@@ -33,6 +33,38 @@ __device__ __forceinline__ float gelu_grad_s(float u, float s) {
 
 __device__ __forceinline__ float gelu_grad_f(float u) { return gelu_grad_s(u, gelu_sig(u)); }
 
+// Activations of the linear operator.
+enum Act { ACT_NONE = 0, ACT_GELU = 1, ACT_RELU = 2, ACT_SILU = 3 };
+
+// 1 / (1 + exp(-z)): the hardware's exponential and reciprocal where the result
+// is rounded to bf16 (they are off by 2^-21 or so at |z| = 16), the exact ones for fp32.
+template <class E>
+__device__ __forceinline__ float logistic(float z) {
+  if constexpr (sizeof(E) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  else return 1.0f / (1.0f + expf(-z));
+}
+
+// act(u) and its derivative.  Where the logistic has run into 0 or 1 both take
+// their limits (the products there would be 0 times infinity).
+template <class E>
+__device__ __forceinline__ void act_both(int act, float u, float& value, float& slope) {
+  if (act == ACT_GELU || act == ACT_SILU) {
+    const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi): the tanh form, as a logistic
+    const bool gelu = act == ACT_GELU;
+    const float u2 = u * u;
+    const float s = logistic<E>(gelu ? c * (u + 0.044715f * u2 * u) : u);
+    const float bend = s * (1.0f - s);
+    value = s == 0.f ? 0.f : u * s;
+    slope = bend == 0.f ? s : s + u * bend * (gelu ? c * (1.0f + 0.134145f * u2) : 1.0f);
+  } else if (act == ACT_RELU) {
+    value = u < 0.f ? 0.f : u;
+    slope = u > 0.f ? 1.f : 0.f;
+  } else {
+    value = u;
+    slope = 1.f;
+  }
+}
+
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);

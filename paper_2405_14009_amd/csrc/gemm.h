@@ -22,7 +22,8 @@ enum EpiKind {
   EPI_BIAS_GELU = 3,   // u = acc + bias[n];  C = gelu'(u), C2 = gelu(u)
   EPI_GELU_BWD = 4,    // C = acc * aux[m, n]   (aux: the stored gelu'(u))
   EPI_F32_ACC = 5,     // C32 = (accumulate ? C32 : 0) + acc     (fp32 gradient buffers)
-  EPI_F32_STORE = 6    // C32 = acc                              (fp32 scores)
+  EPI_F32_STORE = 6,   // C32 = acc                              (fp32 scores)
+  EPI_LINEAR = 7       // u = acc + bias[n];  C = act(u) + resid[m, n], C2 = act'(u)  (bias, resid, C2: where given)
 };
 
 enum KRange {
@@ -44,6 +45,7 @@ struct GemmParams {
   int epi;          // EpiKind
   void* C; long ldc;
   const float* bias;
+  int bias_bf16, act;  // EPI_LINEAR: bias holds bf16 values; Act
   const void* resid; long ld_resid;
   const void* aux; long ld_aux;
   void* C2; long ldc2;
@@ -98,7 +100,8 @@ hipError_t gemm_f32(const GemmParams& p, hipStream_t s);
 // these loads in flight instead of one load round trip per output group.
 template <int EPI>
 struct EpiIn {
-  static constexpr bool kHas = EPI == EPI_BIAS_RESID || EPI == EPI_GELU_BWD || EPI == EPI_F32_ACC;
+  static constexpr bool kHas = EPI == EPI_BIAS_RESID || EPI == EPI_GELU_BWD || EPI == EPI_F32_ACC ||
+                               EPI == EPI_LINEAR;
   uint4 raw;
 };
 
@@ -116,6 +119,8 @@ __device__ __forceinline__ EpiIn<EPI> epi_fetch4(const GemmParams& p, const void
   };
   if constexpr (EPI == EPI_BIAS_RESID) {
     r.raw = ld((const E*)p.resid + (long)m * p.ld_resid + n);
+  } else if constexpr (EPI == EPI_LINEAR) {
+    if (p.resid) r.raw = ld((const E*)p.resid + (long)m * p.ld_resid + n);
   } else if constexpr (EPI == EPI_GELU_BWD) {
     r.raw = ld((const E*)p.aux + (long)m * p.ld_aux + n);
   } else if constexpr (EPI == EPI_F32_ACC) {
@@ -125,7 +130,22 @@ __device__ __forceinline__ EpiIn<EPI> epi_fetch4(const GemmParams& p, const void
 }
 
 constexpr bool epi_has_bias(int epi) {
-  return epi == EPI_BIAS || epi == EPI_BIAS_RESID || epi == EPI_BIAS_GELU;
+  return epi == EPI_BIAS || epi == EPI_BIAS_RESID || epi == EPI_BIAS_GELU || epi == EPI_LINEAR;
+}
+
+// bias[n .. n + 3] of an epilogue that has one.
+template <int EPI>
+__device__ __forceinline__ float4 epi_bias4(const GemmParams& p, int n) {
+  if constexpr (EPI == EPI_LINEAR) {
+    if (!p.bias) return make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p.bias_bf16) {
+      const bf16* b = (const bf16*)p.bias + n;   // aligned to its elements only
+      return make_float4((float)b[0], (float)b[1], (float)b[2], (float)b[3]);
+    }
+    return make_float4(p.bias[n], p.bias[n + 1], p.bias[n + 2], p.bias[n + 3]);
+  } else {
+    return *(const float4*)(p.bias + n);
+  }
 }
 
 // The epilogue on 4 consecutive columns n..n+3 (n % 4 == 0, all in range)
@@ -172,6 +192,18 @@ __device__ __forceinline__ void epi_finish4(const GemmParams& p, void* Cv, int m
     if constexpr (EPI == EPI_GELU_BWD) {
       const float4 d = cvt4(in.raw);
       v.x *= d.x; v.y *= d.y; v.z *= d.z; v.w *= d.w;
+    }
+    if constexpr (EPI == EPI_LINEAR) {
+      if (p.act != ACT_NONE) {
+        float4 d;
+        act_both<E>(p.act, v.x, v.x, d.x);
+        act_both<E>(p.act, v.y, v.y, d.y);
+        act_both<E>(p.act, v.z, v.z, d.z);
+        act_both<E>(p.act, v.w, v.w, d.w);
+        if (p.C2) st4((E*)p.C2 + (long)m * p.ldc2 + n, d);
+      }
+      const float4 r = cvt4(in.raw);
+      v.x += r.x; v.y += r.y; v.z += r.z; v.w += r.w;
     }
     if constexpr (EPI == EPI_BIAS_GELU) {
       const float4 sg = make_float4(gelu_sig(v.x), gelu_sig(v.y), gelu_sig(v.z), gelu_sig(v.w));

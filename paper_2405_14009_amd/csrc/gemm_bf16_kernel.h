@@ -321,7 +321,7 @@ __device__ __forceinline__ void epilogue(const GemmParams& p, f32x16 (&acc)[TM][
   float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
   if constexpr (epi_has_bias(EPI)) {
     const int n = n0 + 4 * (lane % (COLS / 4));
-    if (n < p.N) bias = *(const float4*)(p.bias + n);
+    if (n < p.N) bias = epi_bias4<EPI>(p, n);
   }
   EpiIn<EPI> in[2][NQ];
   auto fetch = [&](int i, EpiIn<EPI>(&dst)[NQ]) {

@@ -4,6 +4,7 @@
 
 hipError_t gemm_bf16_nt(const GemmParams& p, hipStream_t s);
 hipError_t gemm_bf16_tn(const GemmParams& p, hipStream_t s);
+hipError_t gemm_bf16_linear_nn(const GemmParams& p, hipStream_t s);
 
 static hipError_t gemm_bf16_nn(const GemmParams& p, hipStream_t s) {
   switch (p.epi) {
@@ -11,7 +12,7 @@ static hipError_t gemm_bf16_nn(const GemmParams& p, hipStream_t s) {
     case EPI_BIAS: return launch_bf16<true, false, EPI_BIAS>(p, s);
     case EPI_BIAS_RESID: return launch_bf16<true, false, EPI_BIAS_RESID>(p, s);
     case EPI_BIAS_GELU: return launch_bf16<true, false, EPI_BIAS_GELU>(p, s);
-    default: return hipErrorInvalidValue;
+    default: return gemm_bf16_linear_nn(p, s);
   }
 }
 

@@ -258,6 +258,8 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
         const int m = mb + 8 * (r >> 2) + (r & 3);
         in[r] = 0.f;
         if (n < p.N && m < p.M) {
+          if constexpr (EPI == EPI_LINEAR)
+            if (p.resid) in[r] = ((const float*)p.resid)[(long)m * p.ld_resid + n];
           if constexpr (EPI == EPI_BIAS_RESID) in[r] = ((const float*)p.resid)[(long)m * p.ld_resid + n];
           if constexpr (EPI == EPI_GELU_BWD) in[r] = ((const float*)p.aux)[(long)m * p.ld_aux + n];
           if constexpr (EPI == EPI_F32_ACC)
@@ -265,14 +267,24 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
         }
       }
       float bias = 0.f;
-      if constexpr (epi_has_bias(EPI))
+      if constexpr (EPI == EPI_LINEAR) {
+        if (n < p.N && p.bias) bias = p.bias_bf16 ? (float)((const bf16*)p.bias)[n] : p.bias[n];
+      } else if constexpr (epi_has_bias(EPI)) {
         if (n < p.N) bias = p.bias[n];
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int m = mb + 8 * (r >> 2) + (r & 3);
         if (n < p.N && m < p.M) {
           const long o = (long)m * p.ldc + n;
-          if constexpr (EPI == EPI_BIAS) {
+          if constexpr (EPI == EPI_LINEAR) {
+            float u = v[r] + bias, slope;
+            if (p.act != ACT_NONE) {
+              act_both<float>(p.act, u, u, slope);
+              if (p.C2) ((float*)p.C2)[(long)m * p.ldc2 + n] = slope;
+            }
+            C[o] = u + in[r];
+          } else if constexpr (EPI == EPI_BIAS) {
             C[o] = v[r] + bias;
           } else if constexpr (EPI == EPI_BIAS_RESID) {
             C[o] = v[r] + bias + in[r];
@@ -338,6 +350,7 @@ hipError_t launch_epi(const GemmParams& p, hipStream_t s) {
     case EPI_BIAS_GELU: return launch<AK, BKC, EPI_BIAS_GELU>(p, pl, s);
     case EPI_GELU_BWD: return launch<AK, BKC, EPI_GELU_BWD>(p, pl, s);
     case EPI_F32_ACC: return launch<AK, BKC, EPI_F32_ACC>(p, pl, s);
+    case EPI_LINEAR: return launch<AK, BKC, EPI_LINEAR>(p, pl, s);
     default: return launch<AK, BKC, EPI_F32_STORE>(p, pl, s);
   }
 }

@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256) void gemm_small_kernel(GemmParams p) {
     void* C = (OutT*)p.C + c_off;
     const EpiIn<EPI> in = epi_fetch4<EPI, E>(p, C, m, n);
     float4 bias = make_float4(0.f, 0.f, 0.f, 0.f);
-    if constexpr (epi_has_bias(EPI)) bias = *(const float4*)(p.bias + n);
+    if constexpr (epi_has_bias(EPI)) bias = epi_bias4<EPI>(p, n);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {

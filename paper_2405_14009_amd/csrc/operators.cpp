@@ -3,16 +3,13 @@
 
 #include <algorithm>
 #include <cmath>
-#include <exception>
 #include <string>
 #include <utility>
 #include <vector>
 
 #include "adamw_op.h"
 #include "attn_op.h"
-#include "recycle_stage.h"
-
-rc_status rc_set_error(rc_status s, const std::string& msg);
+#include "operators_common.h"
 
 rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
   if (c.dtype != RC_FP32 && c.dtype != RC_BF16) return rc_set_error(RC_ERR_INVALID_ARG, "unknown dtype");
@@ -63,43 +60,6 @@ rc_status attn_op_check(const rc_attention& c, AttnOpArgs& a) {
 
 namespace {
 
-rc_status fail(rc_status s, const std::string& msg) { return rc_set_error(s, msg); }
-
-// No exception leaves a C entry.
-template <class F>
-rc_status guarded(F f) {
-  try {
-    return f();
-  } catch (const std::exception& e) {
-    return fail(RC_ERR_HIP, std::string("host: ") + e.what());
-  }
-}
-
-// The stream's device as the current one, while in scope (kernels start on the current one).
-struct OnDevice {
-  int back = -1;
-  hipError_t err = hipSuccess;
-  explicit OnDevice(hipStream_t s) {
-    if (!s) return;
-    int cur = 0;
-    err = hipGetDevice(&cur);
-    const int dev = hipGetStreamDeviceId(s);
-    if (err != hipSuccess || dev < 0 || dev == cur) return;
-    err = hipSetDevice(dev);
-    if (err == hipSuccess) back = cur;
-  }
-  ~OnDevice() {
-    if (back >= 0) (void)hipSetDevice(back);
-  }
-};
-
-rc_status hip_result(hipError_t e, const char* what) {
-  if (e == hipSuccess) return RC_OK;
-  return fail(RC_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
-
-int elt_of(int dtype) { return dtype == RC_BF16 ? 2 : 4; }
-
 rc_status attention_args(const rc_attention* c, AttnOpArgs& a) {
   if (!c) return fail(RC_ERR_INVALID_ARG, "null attention");
   return attn_op_check(*c, a);
@@ -131,12 +91,6 @@ rc_status view_args(const rc_view* v, const char* name, const rc_attention* c, i
   to = {v->data, (long)v->batch_stride, (long)v->token_stride, (long)v->head_stride};
   return RC_OK;
 }
-
-#define TRY(expr)                  \
-  do {                             \
-    const rc_status r_ = (expr);   \
-    if (r_ != RC_OK) return r_;    \
-  } while (0)
 
 rc_status bias_args(const rc_attention* c, const void* bias, const int32_t* lengths, AttnOpArgs& a) {
   if ((c->buckets != 0) != (bias != nullptr))

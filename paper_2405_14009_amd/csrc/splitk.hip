@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256) void splitk_finish_k(GemmParams p) {
   const int m = (int)(i / nc), n = 4 * (int)(i % nc);
   const EpiIn<EPI> in = epi_fetch4<EPI, E>(p, p.C, m, n);
   float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-  if constexpr (epi_has_bias(EPI)) b = *(const float4*)(p.bias + n);
+  if constexpr (epi_has_bias(EPI)) b = epi_bias4<EPI>(p, n);
   const long mn = (long)p.M * p.N;
   const float* src = p.split_work + (long)m * p.N + n;
   float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -50,6 +50,7 @@ hipError_t finish(const GemmParams& p, hipStream_t s) {
     case EPI_BIAS_RESID: hipLaunchKernelGGL((splitk_finish_k<EPI_BIAS_RESID, E>), grid, dim3(256), 0, s, p); break;
     case EPI_BIAS_GELU: hipLaunchKernelGGL((splitk_finish_k<EPI_BIAS_GELU, E>), grid, dim3(256), 0, s, p); break;
     case EPI_GELU_BWD: hipLaunchKernelGGL((splitk_finish_k<EPI_GELU_BWD, E>), grid, dim3(256), 0, s, p); break;
+    case EPI_LINEAR: hipLaunchKernelGGL((splitk_finish_k<EPI_LINEAR, E>), grid, dim3(256), 0, s, p); break;
     case EPI_F32_ACC: hipLaunchKernelGGL((splitk_finish_k<EPI_F32_ACC, E>), grid, dim3(256), 0, s, p); break;
     default: hipLaunchKernelGGL((splitk_finish_k<EPI_F32_STORE, E>), grid, dim3(256), 0, s, p); break;
   }
