@@ -571,7 +571,7 @@ typedef struct rc_dropout {
   const uint64_t* step;
 } rc_dropout;
 
-/* The sizes and types of a call over rows.  rows 0 .. 2^31 - 1, cols 1 .. 2^30. */
+/* The sizes and types of a call over rows.  rows 0 .. 2^31 - 1, cols 1 .. 2^29. */
 typedef struct rc_rows {
   int32_t dtype;        /* rc_dtype of the matrices */
   int32_t param_dtype;  /* rc_dtype of the vectors of parameters; their gradients are fp32 */

@@ -36,38 +36,72 @@ __device__ __forceinline__ float gelu_grad_f(float u) { return gelu_grad_s(u, ge
 // Activations of the linear operator.
 enum Act { ACT_NONE = 0, ACT_GELU = 1, ACT_RELU = 2, ACT_SILU = 3 };
 
-// 1 / (1 + exp(-z)): the hardware's exponential and reciprocal where the result
-// is rounded to bf16 (they are off by 2^-21 or so at |z| = 16), the exact ones for fp32.
+// 1 / (1 + 2^x): the hardware's exponential and reciprocal where the result is
+// rounded to bf16 (they are off by 2^-20 or so at |x| = 16), the exact ones for fp32.
 template <class E>
-__device__ __forceinline__ float logistic(float z) {
-  if constexpr (sizeof(E) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-  else return 1.0f / (1.0f + expf(-z));
+__device__ __forceinline__ float logistic2(float x) {
+  if constexpr (sizeof(E) == 2) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x));
+  else return 1.0f / (1.0f + exp2f(x));
 }
 
-// act(u) and its derivative.  Where the logistic has run into 0 or 1 both take
-// their limits (the products there would be 0 times infinity).
-template <class E>
-__device__ __forceinline__ void act_both(int act, float u, float& value, float& slope) {
-  if (act == ACT_GELU || act == ACT_SILU) {
-    const float c = 1.5957691216057308f;  // 2 sqrt(2 / pi): the tanh form, as a logistic
-    const bool gelu = act == ACT_GELU;
-    const float u2 = u * u;
-    const float s = logistic<E>(gelu ? c * (u + 0.044715f * u2 * u) : u);
-    const float bend = s * (1.0f - s);
-    value = s == 0.f ? 0.f : u * s;
-    slope = bend == 0.f ? s : s + u * bend * (gelu ? c * (1.0f + 0.134145f * u2) : 1.0f);
-  } else if (act == ACT_RELU) {
-    value = u < 0.f ? 0.f : u;
-    slope = u > 0.f ? 1.f : 0.f;
-  } else {
-    value = u;
-    slope = 1.f;
+// v = act(v) and, with SLOPE, its derivative, of N values.  The order of the
+// products keeps 0 times infinity out of finite arguments' derivatives: where s has
+// run into 1, 1 - s is 0 before it meets a large factor.  (An epilogue's time is
+// its operations: GELU and its derivative take 18 of the quarter-rate exponential
+// and reciprocal counted as four.)
+template <class E, bool SLOPE, int N>
+__device__ __forceinline__ void act_values(int act, float (&v)[N], float (&d)[N]) {
+  if (act == ACT_GELU) {
+    // the tanh form as a logistic of 2 sqrt(2 / pi) (u + 0.044715 u^3), in base 2
+    constexpr float C = 1.5957691216057308f, A = -2.3022081984f, B = -0.1029432396f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float u = v[i], u2 = fminf(u * u, 1e30f);
+      const float s = logistic2<E>(u * (A + B * u2));
+      v[i] = u * s;
+      if constexpr (SLOPE) d[i] = s + (v[i] * (1.0f - s)) * (C + (0.134145f * C) * u2);
+    }
+  } else if (act == ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float u = v[i], s = logistic2<E>(-1.4426950408889634f * u);
+      v[i] = u * s;
+      if constexpr (SLOPE) d[i] = s + v[i] * (1.0f - s);
+    }
+  } else {  // ACT_RELU
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (SLOPE) d[i] = v[i] > 0.f ? 1.f : 0.f;
+      v[i] = v[i] < 0.f ? 0.f : v[i];
+    }
   }
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// Sum over groups of N consecutive lanes (a power of two from 4), in registers: the
+// lanes of a row of 16 by data-parallel moves, rows and halves of a wave by swaps.
+// (A shuffle goes through LDS, at ten times the latency of a step here.)  Every
+// lane of a group gets the same sum.
+template <int N>
+__device__ __forceinline__ float lane_sum(float v) {
+  auto add = [&](int moved) { v += __int_as_float(moved); };
+  add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));                       // lane ^ 1
+  add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));                       // lane ^ 2
+  if constexpr (N > 4) add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));  // 7 - lane of 8
+  if constexpr (N > 8) add(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xf, 0xf, true));  // 15 - lane of 16
+  if constexpr (N > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = __int_as_float(r[0]) + __int_as_float(r[1]);
+  }
+  if constexpr (N > 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = __int_as_float(r[0]) + __int_as_float(r[1]);
+  }
   return v;
 }
 

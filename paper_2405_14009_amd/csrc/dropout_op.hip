@@ -19,7 +19,9 @@ struct Grid {
 };
 
 // Rows of a workgroup: enough workgroups to fill the card eight times over, or,
-// where column sums are kept, twice (each stores a row of them).
+// where column sums are kept, twice (each stores a row of them).  Sums of few rows
+// are one workgroup's down, which stores them itself (128 x 256 fp32: 5 us, where
+// the second launch alone takes the host 3.5).
 Grid grid_of(long rows, int cols, bool sums) {
   Grid g;
   const int groups = (cols + 7) / 8;
@@ -27,8 +29,8 @@ Grid grid_of(long rows, int cols, bool sums) {
   while (g.lanes < NT && g.lanes < groups) g.lanes *= 2;
   g.wide = (groups + g.lanes - 1) / g.lanes;
   const long step = NT / g.lanes;   // rows side by side
-  const long want = std::max(1L, (sums ? 512L : 2048L) / g.wide);
   const long steps = std::max(1L, (rows + step - 1) / step);
+  const long want = sums && steps <= 16 ? 1 : std::max(1L, (sums ? 512L : 2048L) / g.wide);
   g.rows = (steps + want - 1) / want * step;
   g.deep = (int)std::max(1L, (rows + g.rows - 1) / g.rows);
   return g;
@@ -92,7 +94,11 @@ __global__ __launch_bounds__(NT) void dropout_k(DropoutArgs a, int lanes, long r
       float t = 0.f;
       for (int q = 0; q < step; ++q) t += red[q * lanes + (i >> 3)][i & 7];
       const int c = 8 * (int)blockIdx.x * lanes + i;
-      if (c < stride) a.work[(long)blockIdx.y * stride + c] = t;
+      if (gridDim.y > 1) {
+        if (c < stride) a.work[(long)blockIdx.y * stride + c] = t;
+      } else if (c < a.cols) {
+        a.sums[c] = a.accumulate ? a.sums[c] + t : t;
+      }
     }
   }
 }
@@ -110,7 +116,7 @@ hipError_t launch(const DropoutArgs& a, hipStream_t s) {
   else DROPOUT(false, false);
 #undef DROPOUT
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !sums) return e;
+  if (e != hipSuccess || !sums || g.deep == 1) return e;
   return rows_finish(a.work, g.deep, 1, stride, a.cols, &a.sums, a.accumulate, s);
 }
 

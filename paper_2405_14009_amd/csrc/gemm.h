@@ -195,12 +195,14 @@ __device__ __forceinline__ void epi_finish4(const GemmParams& p, void* Cv, int m
     }
     if constexpr (EPI == EPI_LINEAR) {
       if (p.act != ACT_NONE) {
-        float4 d;
-        act_both<E>(p.act, v.x, v.x, d.x);
-        act_both<E>(p.act, v.y, v.y, d.y);
-        act_both<E>(p.act, v.z, v.z, d.z);
-        act_both<E>(p.act, v.w, v.w, d.w);
-        if (p.C2) st4((E*)p.C2 + (long)m * p.ldc2 + n, d);
+        float f[4] = {v.x, v.y, v.z, v.w}, d[4];
+        if (p.C2) {
+          act_values<E, true>(p.act, f, d);
+          st4((E*)p.C2 + (long)m * p.ldc2 + n, make_float4(d[0], d[1], d[2], d[3]));
+        } else {
+          act_values<E, false>(p.act, f, d);
+        }
+        v = make_float4(f[0], f[1], f[2], f[3]);
       }
       const float4 r = cvt4(in.raw);
       v.x += r.x; v.y += r.y; v.z += r.z; v.w += r.w;

@@ -278,12 +278,12 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
         if (n < p.N && m < p.M) {
           const long o = (long)m * p.ldc + n;
           if constexpr (EPI == EPI_LINEAR) {
-            float u = v[r] + bias, slope;
+            float u[1] = {v[r] + bias}, slope[1];
             if (p.act != ACT_NONE) {
-              act_both<float>(p.act, u, u, slope);
-              if (p.C2) ((float*)p.C2)[(long)m * p.ldc2 + n] = slope;
+              act_values<float, true>(p.act, u, slope);
+              if (p.C2) ((float*)p.C2)[(long)m * p.ldc2 + n] = slope[0];
             }
-            C[o] = u + in[r];
+            C[o] = u[0] + in[r];
           } else if constexpr (EPI == EPI_BIAS) {
             C[o] = v[r] + bias;
           } else if constexpr (EPI == EPI_BIAS_RESID) {

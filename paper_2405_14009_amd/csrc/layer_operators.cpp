@@ -15,7 +15,7 @@ namespace {
 
 static_assert((int)RC_ACT_GELU == ACT_GELU && (int)RC_ACT_RELU == ACT_RELU && (int)RC_ACT_SILU == ACT_SILU, "activations");
 
-constexpr int64_t MAX_ROWS = 0x7fffffff, MAX_COLS = 1 << 30, MAX_ELEMENTS = 1LL << 46;
+constexpr int64_t MAX_ROWS = 0x7fffffff, MAX_COLS = 1 << 29, MAX_ELEMENTS = 1LL << 46;
 
 bool known(int dtype) { return dtype == RC_FP32 || dtype == RC_BF16; }
 
@@ -92,7 +92,7 @@ rc_status rows_args(const rc_rows* r) {
   if (!known(r->dtype)) return fail(RC_ERR_INVALID_ARG, "unknown dtype");
   if (!known(r->param_dtype)) return fail(RC_ERR_INVALID_ARG, "unknown param_dtype");
   if (r->rows < 0 || r->rows > MAX_ROWS || r->cols < 1 || r->cols > MAX_COLS)
-    return fail(RC_ERR_INVALID_ARG, "rows must lie in 0 .. 2^31 - 1, cols in 1 .. 2^30");
+    return fail(RC_ERR_INVALID_ARG, "rows must lie in 0 .. 2^31 - 1, cols in 1 .. 2^29");
   return RC_OK;
 }
 
@@ -243,7 +243,7 @@ rc_status rc_layer_norm_memory(const rc_rows* r, size_t* work_bytes) {
     NormArgs a;
     if (!work_bytes) return fail(RC_ERR_INVALID_ARG, "null output pointer");
     TRY(norm_args(r, nullptr, a));
-    *work_bytes = norm_work_bytes(a.rows, a.cols, elt_of(r->dtype));
+    *work_bytes = norm_work_bytes(a.rows, a.cols);
     return RC_OK;
   });
 }
@@ -302,7 +302,7 @@ rc_status rc_layer_norm_backward(const rc_rows* r, const rc_dropout* drop, const
     TRY(t.vector(dweight, "dweight", 4, r->cols, true, 4));
     TRY(t.vector(dbias, "dbias", 4, r->cols, true, 4));
     TRY(t.vector(din_bias, "din_bias", 4, r->cols, true, 4));
-    if (sums) TRY(t.work(work, norm_work_bytes(a.rows, a.cols, elt)));
+    if (sums) TRY(t.work(work, norm_work_bytes(a.rows, a.cols)));
     TRY(t.overlap());
     a.weight = weight;
     a.stats = const_cast<float*>(stats);

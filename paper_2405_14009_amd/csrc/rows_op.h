@@ -51,9 +51,16 @@ struct NormArgs {
   float* work;
 };
 
+// How a matrix is shared out: lanes a row (0: whole waves), groups a lane, waves a
+// row, rows side by side, workgroups.
+struct NormPlan {
+  int lpr, cpl, waves, slots, threads;
+  long groups;
+};
+
 // Bytes of work memory for the column sums of a call.
 size_t dropout_work_bytes(long rows, int cols);
-size_t norm_work_bytes(long rows, int cols, int elt);
+size_t norm_work_bytes(long rows, int cols);
 hipError_t dropout_rows(const DropoutArgs& a, int elt, hipStream_t s);
 hipError_t norm_forward(const NormArgs& a, int elt, hipStream_t s);
 hipError_t norm_backward(const NormArgs& a, int elt, hipStream_t s);

@@ -33,18 +33,18 @@ template <class E, bool TAIL>
 struct Columns {
   __device__ __forceinline__ static Raw8<E> load(const E* row, int group, int cols) {
     Raw8<E> r;
-    int c = 8 * group;
+    uint32_t c = 8u * (uint32_t)group;   // (32 bits, unsigned: a lane's offset from its row's address)
     if constexpr (TAIL) {
       if (cols < 8) {
         E t[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = c + e < cols ? row[c + e] : (E)0.f;
+        for (int e = 0; e < 8; ++e) t[e] = (int)c + e < cols ? row[c + e] : (E)0.f;
         __builtin_memcpy(&r, t, sizeof(r));
         return r;
       }
-      c = min(c, cols - 8);
+      c = min(c, (uint32_t)cols - 8u);
     }
-    __builtin_memcpy(&r, row + c, sizeof(r));
+    __builtin_memcpy(&r, (const char*)row + c * (uint32_t)sizeof(E), sizeof(r));
     return r;
   }
   // the loaded group as numbers
@@ -65,7 +65,7 @@ struct Columns {
 #pragma unroll
     for (int e = 0; e < 8; ++e) t[e] = from_f32<E>(f[e]);
     if (!TAIL || 8 * group + 8 <= cols) {
-      __builtin_memcpy(row + 8 * group, t, sizeof(t));
+      __builtin_memcpy((char*)row + 8u * (uint32_t)group * (uint32_t)sizeof(E), t, sizeof(t));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -120,14 +120,18 @@ struct Philox {
     c2 = (uint32_t)o;
     c3 = (uint32_t)(o >> 32);
   }
+  // (one operation; 0x96 is the truth table of a ^ b ^ c)
+  __device__ __forceinline__ static uint32_t xor3(uint32_t x, uint32_t y, uint32_t z) {
+    return __builtin_amdgcn_bitop3_b32(x, y, z, 0x96);
+  }
   __device__ __forceinline__ void words(uint32_t group, uint32_t row, uint32_t (&w)[4]) const {
     uint32_t x0 = group, x1 = row, x2 = c2, x3 = c3, a = k0, b = k1;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
       const uint64_t p = (uint64_t)x0 * 0xD2511F53u, q = (uint64_t)x2 * 0xCD9E8D57u;
-      x0 = (uint32_t)(q >> 32) ^ x1 ^ a;
+      x0 = xor3((uint32_t)(q >> 32), x1, a);
       x1 = (uint32_t)q;
-      x2 = (uint32_t)(p >> 32) ^ x3 ^ b;
+      x2 = xor3((uint32_t)(p >> 32), x3, b);
       x3 = (uint32_t)p;
       a += 0x9E3779B9u;
       b += 0xBB67AE85u;

@@ -20,10 +20,17 @@ from typing import NamedTuple, Optional
 
 from . import _lib as L
 from . import operators as _ops
-from .operators import _call, _import, _kind, _on
+from .operators import _kind, _kinds
 
 _ACTIVATIONS = {None: L.RC_ACT_NONE, "gelu": L.RC_ACT_GELU, "relu": L.RC_ACT_RELU, "silu": L.RC_ACT_SILU}
-_ref = ctypes.byref
+_ref, _Matrix = ctypes.byref, L.RcMatrix
+torch = None   # imported with the first call
+
+
+def _import():
+    global torch
+    _ops._import()
+    torch = _ops.torch
 
 
 class Dropout:
@@ -44,8 +51,8 @@ class Dropout:
         for name, x in (("seed", seed), ("offset", offset)):
             if int(x) != x or not 0 <= x < 1 << 64:
                 raise ValueError(f"{name} must be a whole number of 64 bits, not {x}")
-        if step is not None and (not isinstance(step, _ops.torch.Tensor) or not step.is_cuda
-                                 or step.dtype is not _ops.torch.int64 or step.numel() != 1):
+        if step is not None and (not isinstance(step, torch.Tensor) or not step.is_cuda
+                                 or step.dtype is not torch.int64 or step.numel() != 1):
             raise TypeError("step must be an int64 device tensor of one number")
         self.p, self.seed, self.offset, self.step = p, int(seed), int(offset), step
         self._c = L.RcDropout(p, 0, self.seed, self.offset, None if step is None else step.data_ptr())
@@ -64,68 +71,61 @@ class NormGradients(NamedTuple):
 def _rows(t, name):
     """Rows and row stride of a tensor [..., columns]."""
     shape, stride = t.shape, t.stride()
-    if not shape:
-        raise ValueError(f"{name} must have a dimension of columns")
-    if shape[-1] > 1 and stride[-1] != 1:
+    if len(shape) == 2:
+        rows, step = shape[0], stride[0]
+    else:
+        if not shape:
+            raise ValueError(f"{name} must have a dimension of columns")
+        rows, step = 1, None
+        for n, s in zip(shape[-2::-1], stride[-2::-1]):
+            if n == 1:
+                continue
+            if step is None:
+                step = s
+            elif s != step * rows and n and rows:
+                raise ValueError(f"{name}: the rows must have one stride between them")
+            rows *= n
+    if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the columns must be contiguous")
-    rows, step = 1, None
-    for n, s in zip(shape[-2::-1], stride[-2::-1]):
-        if n == 1:
-            continue
-        if step is None:
-            step = s
-        elif s != step * rows and n and rows:
-            raise ValueError(f"{name}: the rows must have one stride between them")
-        rows *= n
-    return rows, shape[-1] if step is None else step
+    return rows, shape[-1] if rows == 1 else step
 
 
-def _matrix(t, name, like):
-    """A matrix that goes with `like`."""
-    if t is not like:
-        if (not isinstance(t, _ops.torch.Tensor) or t.dtype is not like.dtype
-                or t.get_device() != like.get_device()):
-            _kind(t, name)
-            raise ValueError(f"{name} must have the type and device of the others")
-        if t.shape != like.shape:
-            raise ValueError(f"{name} must have the shape {tuple(like.shape)}, not {tuple(t.shape)}")
-    return L.RcMatrix(t.data_ptr(), _rows(t, name)[1])
+def _tensor(t, name, dtype, device):
+    """Refuses what is not a tensor of the type and device (its number) of the others."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != device:
+        _kind(t, name)
+        raise ValueError(f"{name} must have the type and device of the others")
 
 
-def _optional(t, name, like):
-    return None if t is None else _ref(_matrix(t, name, like))
+def _matrix(t, name, shape, dtype, device):
+    """A reference to a matrix of this shape."""
+    _tensor(t, name, dtype, device)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    return _ref(_Matrix(t.data_ptr(), _rows(t, name)[1]))
 
 
-def _new(like, columns=None):
-    """A contiguous tensor like another one, or with another number of columns."""
-    if columns is None:
-        return _ops.torch.empty_like(like, memory_format=_ops.torch.contiguous_format)
-    return like.new_empty((*like.shape[:-1], columns))
-
-
-def _output(t, name, like):
-    """An output like another tensor (the caller's, or a new one) and its matrix."""
+def _output(t, name, like, shape, dtype, device):
+    """An output like another tensor (the caller's, or a new one), and a reference to its matrix."""
     if t is None:
-        t = _new(like)
-        return t, L.RcMatrix(t.data_ptr(), t.shape[-1])
-    return t, _matrix(t, name, like)
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
+        return t, _ref(_Matrix(t.data_ptr(), shape[-1]))
+    return t, _matrix(t, name, shape, dtype, device)
 
 
-def _vectors(n, like, **vectors):
-    """The type of the vectors of parameters that are given, and their addresses."""
-    kind, places = None, []
-    for name, t in vectors.items():
-        if t is None:
-            places.append(None)
-            continue
+def _vector(t, name, n, device, kind):
+    """The address of a vector of parameters, and its type, which is that of those before it."""
+    if t is None:
+        return None, kind
+    this = _kinds.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if this is None or t.get_device() != device:
         this = _kind(t, name)
-        if kind is not None and this != kind:
-            raise ValueError(f"{name} must have the type of the other vectors")
-        kind = this
-        if t.shape != (n,) or not t.is_contiguous() or t.get_device() != like.get_device():
-            raise ValueError(f"{name} must be a contiguous vector of {n} on the device of the matrices")
-        places.append(t.data_ptr())
-    return L.RC_FP32 if kind is None else kind, places
+        raise ValueError(f"{name} must be on the device of the matrices")
+    if kind is not None and this != kind:
+        raise ValueError(f"{name} must have the type of the other vectors")
+    if t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous vector of {n}")
+    return t.data_ptr(), this
 
 
 def _gradient(want, name, shape, like):
@@ -133,8 +133,8 @@ def _gradient(want, name, shape, like):
     if want is None or want is False:
         return None
     if want is True:
-        return _ops.torch.empty(shape, dtype=_ops.torch.float32, device=like.device)
-    if (not isinstance(want, _ops.torch.Tensor) or want.dtype is not _ops.torch.float32
+        return torch.empty(shape, dtype=torch.float32, device=like.device)
+    if (not isinstance(want, torch.Tensor) or want.dtype is not torch.float32
             or want.get_device() != like.get_device()):
         raise TypeError(f"{name} must be True, False or an fp32 tensor on the device of the matrices")
     if want.shape != shape or not want.is_contiguous():
@@ -152,62 +152,76 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
-def _no_graph(**tensors):
-    if _ops.torch.is_grad_enabled():
-        for name, t in tensors.items():
+def _no_graph(*tensors):
+    """Refuses (tensor, name, ...) that autograd would have to record."""
+    if torch.is_grad_enabled():
+        for t, name in zip(tensors[::2], tensors[1::2]):
             if t is not None and getattr(t, "requires_grad", False):
                 raise RuntimeError(f"{name} requires gradients, which autograd does not pass through this call; "
                                    "call it under torch.no_grad(), and the operator's backward calls for them")
 
 
-def _dropout(drop, like, needed):
-    if drop is None and not needed:
-        return None
+def _dropout(drop, device):
     if not isinstance(drop, Dropout):
         raise TypeError("drop must be a Dropout")
-    if drop.step is not None and drop.step.get_device() != like.get_device():
-        raise ValueError("the dropout's step must be on the device of the matrices")
+    if drop.step is not None:
+        if drop.step.get_device() != device:
+            raise ValueError("the dropout's step must be on the device of the matrices")
+        drop._c.step = drop.step.data_ptr()
     return _ref(drop._c)
 
 
 def _work(size, like):
-    return _ops.torch.empty(size, dtype=_ops.torch.uint8, device=like.device) if size else None
+    return torch.empty(size, dtype=torch.uint8, device=like.device)
+
+
+def _call(function, device, *args):
+    """The call on PyTorch's current stream of the device."""
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if device == torch._C._cuda_getDevice():
+        status = function(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = function(*args, stream)
+    if status != L.RC_OK:
+        L.check(status)
 
 
 @functools.lru_cache(maxsize=256)
 def _rows_config(kind, params, rows, cols, operator):
     """Checked sizes, with the bytes of the backward pass's work memory."""
-    c = L.RcRows(kind, params, rows, cols)
+    c = L.RcRows(kind, L.RC_FP32 if params is None else params, rows, cols)
     size = ctypes.c_size_t()
     L.check(getattr(L.load(), operator + "_memory")(_ref(c), _ref(size)))
-    return c, size.value
+    return _ref(c), size.value
 
 
 @functools.lru_cache(maxsize=256)
 def _linear_config(kind, bias_kind, rows, fan_in, fan_out, activation, by_out):
     """Checked sizes, with the bytes of the three calls' work memory."""
-    c = L.RcLinear(kind, bias_kind, rows, fan_in, fan_out, activation, by_out)
+    c = L.RcLinear(kind, L.RC_FP32 if bias_kind is None else bias_kind, rows, fan_in, fan_out, activation, by_out)
     sizes = [ctypes.c_size_t() for _ in range(3)]
     L.check(L.load().rc_linear_memory(_ref(c), *map(_ref, sizes)))
-    return c, *(x.value for x in sizes)
+    return _ref(c), *(x.value for x in sizes)
 
 
 def dropout_forward(x, drop: Dropout, *, bias=None, residual=None, out=None):
     """residual + D(x + bias): D keeps and scales elements as `drop` says, or makes
     them 0.  bias: [columns], residual: like x.  out: a tensor for the result, which
     overlaps no input."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(x, "x")
-    _no_graph(x=x, bias=bias, residual=residual, out=out)
-    d = _dropout(drop, x, True)
+    _no_graph(x, "x", bias, "bias", residual, "residual", out, "out")
+    shape, dtype, device = x.shape, x.dtype, x.get_device()
+    d = _dropout(drop, device)
     rows, step = _rows(x, "x")
-    cols = x.shape[-1]
-    params, (b,) = _vectors(cols, x, bias=bias)
+    cols = shape[-1]
+    b, params = _vector(bias, "bias", cols, device, None)
     c, _ = _rows_config(kind, params, rows, cols, "rc_dropout")
-    y, ym = _output(out, "out", x)
-    on, stream = _on(x.device)
-    _call(on, L.load().rc_dropout_forward, _ref(c), d, _ref(L.RcMatrix(x.data_ptr(), step)), b,
-          _optional(residual, "residual", x), _ref(ym), stream)
+    r = None if residual is None else _matrix(residual, "residual", shape, dtype, device)
+    y, ym = _output(out, "out", x, shape, dtype, device)
+    _call(L.load().rc_dropout_forward, device, c, d, _ref(_Matrix(x.data_ptr(), step)), b, r, ym)
     return y
 
 
@@ -217,19 +231,21 @@ def dropout_backward(dy, drop: Dropout, *, derivative=None, bias_grad=False, acc
     what linear_forward stored of an activation that the elements went through
     before the dropout (without a dropout: Dropout(0.0, 0)).  bias_grad: True, or an
     fp32 tensor [columns], which accumulate adds to.  The gradient of the residual is dy."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(dy, "dy")
-    d = _dropout(drop, dy, True)
+    shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
+    d = _dropout(drop, device)
     rows, step = _rows(dy, "dy")
-    cols = dy.shape[-1]
-    c, work_bytes = _rows_config(kind, L.RC_FP32, rows, cols, "rc_dropout")
+    cols = shape[-1]
+    c, work_bytes = _rows_config(kind, None, rows, cols, "rc_dropout")
     more = _accumulates(accumulate, bias_grad)
     dbias = _gradient(bias_grad, "bias_grad", (cols,), dy)
-    dx, dxm = _output(out, "out", dy)
-    work = _work(work_bytes if dbias is not None else 0, dy)
-    on, stream = _on(dy.device)
-    _call(on, L.load().rc_dropout_backward, _ref(c), d, _ref(L.RcMatrix(dy.data_ptr(), step)),
-          _optional(derivative, "derivative", dy), _ref(dxm), _address(dbias), more, _address(work), stream)
+    m = None if derivative is None else _matrix(derivative, "derivative", shape, dtype, device)
+    dx, dxm = _output(out, "out", dy, shape, dtype, device)
+    work = None if dbias is None else _work(work_bytes, dy)
+    _call(L.load().rc_dropout_backward, device, c, d, _ref(_Matrix(dy.data_ptr(), step)), m, dxm, _address(dbias), more,
+          _address(work))
     return dx, dbias
 
 
@@ -239,28 +255,31 @@ def layer_norm_forward(x, weight=None, bias=None, *, eps: float = 1e-5, in_bias=
     where none of the three is given), y = its norm over each row, times weight, plus
     bias (None: 1, 0).  stats: what layer_norm_backward needs, None with save=False.
     out, total: tensors for the results."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(x, "x")
-    _no_graph(x=x, weight=weight, bias=bias, in_bias=in_bias, residual=residual, out=out, total=total)
-    d = _dropout(drop, x, False)
+    _no_graph(x, "x", weight, "weight", bias, "bias", in_bias, "in_bias", residual, "residual", out, "out", total, "total")
+    shape, dtype, device = x.shape, x.dtype, x.get_device()
+    d = None if drop is None else _dropout(drop, device)
     rows, step = _rows(x, "x")
-    cols = x.shape[-1]
-    params, (w, b, ib) = _vectors(cols, x, weight=weight, bias=bias, in_bias=in_bias)
+    cols = shape[-1]
+    w, params = _vector(weight, "weight", cols, device, None)
+    b, params = _vector(bias, "bias", cols, device, params)
+    ib, params = _vector(in_bias, "in_bias", cols, device, params)
     c, _ = _rows_config(kind, params, rows, cols, "rc_layer_norm")
-    rm = _optional(residual, "residual", x)
-    tm = None
-    if d is not None or ib is not None or rm is not None:
-        total, tm = _output(total, "total", x)
-        tm = _ref(tm)
+    r = tm = None
+    if residual is not None:
+        r = _matrix(residual, "residual", shape, dtype, device)
+    if d is not None or ib is not None or r is not None:
+        total, tm = _output(total, "total", x, shape, dtype, device)
     elif total is not None:
         raise ValueError("total without a residual, a dropout or an in_bias is x")
     else:
         total = x
-    y, ym = _output(out, "out", x)
-    stats = _ops.torch.empty((2, rows), dtype=_ops.torch.float32, device=x.device) if save else None
-    on, stream = _on(x.device)
-    _call(on, L.load().rc_layer_norm_forward, _ref(c), float(eps), d, _ref(L.RcMatrix(x.data_ptr(), step)), ib, rm, w,
-          b, tm, _ref(ym), _address(stats), stream)
+    y, ym = _output(out, "out", x, shape, dtype, device)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device) if save else None
+    _call(L.load().rc_layer_norm_forward, device, c, float(eps), d, _ref(_Matrix(x.data_ptr(), step)), ib, r, w, b, tm,
+          ym, _address(stats))
     return y, total, stats
 
 
@@ -274,50 +293,50 @@ def layer_norm_backward(dy, total, stats, weight=None, *, dtotal=None, drop: Opt
     formed; weight_grad, bias_grad, in_bias_grad: True, False or fp32 tensors
     [columns], which accumulate adds to.  The parameters' gradients may so be left to
     a later call."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(dy, "dy")
-    d = _dropout(drop, dy, False)
+    shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
+    d = None if drop is None else _dropout(drop, device)
     rows, step = _rows(dy, "dy")
-    cols = dy.shape[-1]
-    params, (w,) = _vectors(cols, dy, weight=weight)
+    cols = shape[-1]
+    w, params = _vector(weight, "weight", cols, device, None)
     c, work_bytes = _rows_config(kind, params, rows, cols, "rc_layer_norm")
-    if (not isinstance(stats, _ops.torch.Tensor) or stats.dtype is not _ops.torch.float32 or stats.shape != (2, rows)
-            or not stats.is_contiguous() or stats.get_device() != dy.get_device()):
+    if (not isinstance(stats, torch.Tensor) or stats.dtype is not torch.float32 or stats.shape != (2, rows)
+            or not stats.is_contiguous() or stats.get_device() != device):
         raise ValueError("stats must be what layer_norm_forward returned for these rows")
+    t = _matrix(total, "total", shape, dtype, device)
+    din = None if dtotal is None else _matrix(dtotal, "dtotal", shape, dtype, device)
     more = _accumulates(accumulate, weight_grad, bias_grad, in_bias_grad)
-    sums = [_gradient(want, name, (cols,), dy) for name, want in
-            (("weight_grad", weight_grad), ("bias_grad", bias_grad), ("in_bias_grad", in_bias_grad))]
+    vector = (cols,)
+    dw = _gradient(weight_grad, "weight_grad", vector, dy)
+    db = _gradient(bias_grad, "bias_grad", vector, dy)
+    dib = _gradient(in_bias_grad, "in_bias_grad", vector, dy)
+    sums = dw is not None or db is not None or dib is not None
     dt = dx = dtm = dxm = None
     if input_grad:
-        dt = _new(dy)
-        dtm = _ref(L.RcMatrix(dt.data_ptr(), cols))
+        dt, dtm = _output(None, "dtotal", dy, shape, dtype, device)
         dx = dt
         if d is not None:
-            dx = _new(dy)
-            dxm = _ref(L.RcMatrix(dx.data_ptr(), cols))
-    elif not any(s is not None for s in sums):
+            dx, dxm = _output(None, "dx", dy, shape, dtype, device)
+    elif not sums:
         raise ValueError("no gradient is asked for")
-    work = _work(work_bytes if any(s is not None for s in sums) else 0, dy)
-    on, stream = _on(dy.device)
-    _call(on, L.load().rc_layer_norm_backward, _ref(c), d, _ref(L.RcMatrix(dy.data_ptr(), step)),
-          _optional(dtotal, "dtotal", dy), _ref(_matrix(total, "total", dy)), stats.data_ptr(), w, dtm, dxm,
-          *map(_address, sums), more, _address(work), stream)
-    return NormGradients(dx, dt, *sums)
+    work = _work(work_bytes, dy) if sums else None
+    _call(L.load().rc_layer_norm_backward, device, c, d, _ref(_Matrix(dy.data_ptr(), step)), din, t, stats.data_ptr(), w,
+          dtm, dxm, _address(dw), _address(db), _address(dib), more, _address(work))
+    return NormGradients(dx, dt, dw, db, dib)
 
 
-def _weight(weight, like):
+def _weight(weight, dtype, device):
     """A weight [in, out], either dimension contiguous: its matrix, and whether it is stored [out, in]."""
-    if (not isinstance(weight, _ops.torch.Tensor) or weight.dtype is not like.dtype
-            or weight.get_device() != like.get_device()):
-        _kind(weight, "weight")
-        raise ValueError("weight must have the type and device of the matrices")
+    _tensor(weight, "weight", dtype, device)
     if weight.dim() != 2:
         raise ValueError("weight must be [in, out]")
     s0, s1 = weight.stride()
     if s1 == 1:
-        return L.RcMatrix(weight.data_ptr(), s0), 0
+        return _ref(_Matrix(weight.data_ptr(), s0)), 0
     if s0 == 1:
-        return L.RcMatrix(weight.data_ptr(), s1), 1
+        return _ref(_Matrix(weight.data_ptr(), s1)), 1
     raise ValueError("weight: one of its dimensions must be contiguous")
 
 
@@ -335,33 +354,33 @@ def linear_forward(x, weight, bias=None, *, activation: Optional[str] = None, re
     activation: None, "gelu" (its tanh form), "relu" or "silu".  derivative: the
     activation's, for the backward calls (None without an activation or with
     save=False).  in and out are multiples of 8, data and row strides of 16 bytes."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(x, "x")
-    _no_graph(x=x, weight=weight, bias=bias, residual=residual, out=out)
+    _no_graph(x, "x", weight, "weight", bias, "bias", residual, "residual", out, "out")
     act = _activation(activation)
+    dtype, device = x.dtype, x.get_device()
     rows, step = _rows(x, "x")
-    wm, by_out = _weight(weight, x)
+    wm, by_out = _weight(weight, dtype, device)
     fan_in, fan_out = weight.shape
     if x.shape[-1] != fan_in:
         raise ValueError(f"x must have {fan_in} columns, as weight has rows, not {x.shape[-1]}")
-    bias_kind, (b,) = _vectors(fan_out, x, bias=bias)
+    b, bias_kind = _vector(bias, "bias", fan_out, device, None)
     c, work_bytes, _, _ = _linear_config(kind, bias_kind, rows, fan_in, fan_out, act, by_out)
+    shape = (*x.shape[:-1], fan_out)
+    r = sm = None
+    if residual is not None:
+        r = _matrix(residual, "residual", shape, dtype, device)
     if out is None:
-        y = _new(x, fan_out)
-        ym = L.RcMatrix(y.data_ptr(), fan_out)
+        y = x.new_empty(shape)
+        ym = _ref(_Matrix(y.data_ptr(), fan_out))
     else:
-        y = out
-        if not isinstance(y, _ops.torch.Tensor) or y.shape != (*x.shape[:-1], fan_out):
-            raise ValueError(f"out must have the shape {(*x.shape[:-1], fan_out)}")
-        if y.dtype is not x.dtype or y.get_device() != x.get_device():
-            raise ValueError("out must have the type and device of x")
-        ym = _matrix(y, "out", y)
-    slope = _new(y) if act and save else None
-    work = _work(work_bytes, x)
-    on, stream = _on(x.device)
-    _call(on, L.load().rc_linear_forward, _ref(c), _ref(L.RcMatrix(x.data_ptr(), step)), _ref(wm), b,
-          _optional(residual, "residual", y), _ref(ym),
-          None if slope is None else _ref(L.RcMatrix(slope.data_ptr(), fan_out)), _address(work), stream)
+        y, ym = out, _matrix(out, "out", shape, dtype, device)
+    slope = None
+    if act and save:
+        slope, sm = _output(None, "derivative", y, shape, dtype, device)
+    work = _work(work_bytes, x) if work_bytes else None
+    _call(L.load().rc_linear_forward, device, c, _ref(_Matrix(x.data_ptr(), step)), wm, b, r, ym, sm, _address(work))
     return y, slope
 
 
@@ -369,27 +388,26 @@ def linear_backward_input(dy, weight, *, derivative=None, out=None):
     """dx = (dy weight^T) * derivative.  dy: the gradient at x weight + bias.
     derivative: what linear_forward stored of the activation that made x (dx is then
     the gradient before that activation, which that layer's backward calls take)."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(dy, "dy")
+    dtype, device = dy.dtype, dy.get_device()
     rows, step = _rows(dy, "dy")
-    wm, by_out = _weight(weight, dy)
+    wm, by_out = _weight(weight, dtype, device)
     fan_in, fan_out = weight.shape
     if dy.shape[-1] != fan_out:
         raise ValueError(f"dy must have {fan_out} columns, as weight has, not {dy.shape[-1]}")
-    c, _, work_bytes, _ = _linear_config(kind, L.RC_FP32, rows, fan_in, fan_out, L.RC_ACT_NONE, by_out)
+    c, _, work_bytes, _ = _linear_config(kind, None, rows, fan_in, fan_out, L.RC_ACT_NONE, by_out)
     shape = (*dy.shape[:-1], fan_in)
+    s = None if derivative is None else _matrix(derivative, "derivative", shape, dtype, device)
     if out is None:
-        dx = _new(dy, fan_in)
-    elif (not isinstance(out, _ops.torch.Tensor) or out.shape != shape or out.dtype is not dy.dtype
-          or out.get_device() != dy.get_device()):
-        raise ValueError(f"out must have the shape {shape}, and the type and device of dy")
+        out = dy.new_empty(shape)
+        dxm = _ref(_Matrix(out.data_ptr(), fan_in))
     else:
-        dx = out
-    work = _work(work_bytes, dy)
-    on, stream = _on(dy.device)
-    _call(on, L.load().rc_linear_backward_input, _ref(c), _ref(L.RcMatrix(dy.data_ptr(), step)), _ref(wm),
-          _optional(derivative, "derivative", dx), _ref(_matrix(dx, "out", dx)), _address(work), stream)
-    return dx
+        dxm = _matrix(out, "out", shape, dtype, device)
+    work = _work(work_bytes, dy) if work_bytes else None
+    _call(L.load().rc_linear_backward_input, device, c, _ref(_Matrix(dy.data_ptr(), step)), wm, s, dxm, _address(work))
+    return out
 
 
 def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bias_grad=True, accumulate: bool = False):
@@ -397,18 +415,18 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
     without bias_grad).  by_out: dweight is the transpose of a contiguous matrix
     [out, in], for weights stored so.  weight_grad, bias_grad: True, or fp32 tensors,
     which accumulate adds to."""
-    _import()
+    if torch is None:
+        _import()
     kind = _kind(x, "x")
+    dtype, device = x.dtype, x.get_device()
     rows, step = _rows(x, "x")
-    if (not isinstance(dy, _ops.torch.Tensor) or dy.dtype is not x.dtype or dy.get_device() != x.get_device()):
-        _kind(dy, "dy")
-        raise ValueError("dy must have the type and device of x")
-    if dy.shape[:-1] != x.shape[:-1] or not dy.dim():
+    _tensor(dy, "dy", dtype, device)
+    if not dy.dim() or dy.shape[:-1] != x.shape[:-1]:
         raise ValueError(f"dy must have the rows of x, {tuple(x.shape[:-1])}")
     dstep = _rows(dy, "dy")[1]
     fan_in, fan_out = x.shape[-1], dy.shape[-1]
     by_out = 1 if by_out else 0
-    c, _, _, work_bytes = _linear_config(kind, L.RC_FP32, rows, fan_in, fan_out, L.RC_ACT_NONE, by_out)
+    c, _, _, work_bytes = _linear_config(kind, None, rows, fan_in, fan_out, L.RC_ACT_NONE, by_out)
     if weight_grad is None or weight_grad is False:
         raise ValueError("weight_grad must be True or an fp32 tensor")
     more = _accumulates(accumulate, weight_grad, bias_grad)
@@ -418,7 +436,6 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
     dw = _gradient(weight_grad, "weight_grad", shape, x)
     dbias = _gradient(bias_grad, "bias_grad", (fan_out,), x)
     work = _work(work_bytes, x)
-    on, stream = _on(x.device)
-    _call(on, L.load().rc_linear_backward_weight, _ref(c), _ref(L.RcMatrix(x.data_ptr(), step)),
-          _ref(L.RcMatrix(dy.data_ptr(), dstep)), dw.data_ptr(), _address(dbias), more, _address(work), stream)
+    _call(L.load().rc_linear_backward_weight, device, c, _ref(_Matrix(x.data_ptr(), step)),
+          _ref(_Matrix(dy.data_ptr(), dstep)), dw.data_ptr(), _address(dbias), more, _address(work))
     return (dw.t() if by_out else dw), dbias

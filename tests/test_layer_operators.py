@@ -135,7 +135,7 @@ def test_linear_memory(r, i, o, dtype):
 
 BAD_ROWS = [(dict(dtype=9), "INVALID_ARG", b"dtype"), (dict(param_dtype=2), "INVALID_ARG", b"param_dtype"),
             (dict(rows=-1), "INVALID_ARG", b"rows"), (dict(rows=1 << 31), "INVALID_ARG", b"rows"),
-            (dict(cols=0), "INVALID_ARG", b"cols"), (dict(cols=(1 << 30) + 1), "INVALID_ARG", b"cols")]
+            (dict(cols=0), "INVALID_ARG", b"cols"), (dict(cols=(1 << 29) + 1), "INVALID_ARG", b"cols")]
 
 
 @pytest.mark.parametrize("kw,st,word", BAD_ROWS, ids=str)
