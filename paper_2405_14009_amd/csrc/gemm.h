@@ -52,7 +52,9 @@ struct GemmParams {
   int accumulate;
   // Column sums of B over k (bf16 GEMMs with A and B m/n-contiguous): the
   // bias gradient of a linear layer is exactly this sum of its output
-  // gradient, the B operand of its weight-gradient product.  The workgroup of
+  // gradient, the B operand of its weight-gradient product (colsum_a: the A
+  // operand, of weights [out, in]; A and M, tile-columns and tiles_n then take the
+  // place of B and N, tile-rows and tiles_m).  The workgroup of
   // tile-row tm sums the B tiles it stages anyway whose k-tile index t has
   // t mod tiles_m == tm, into row tm of colsum_work ([rows, N] floats of the
   // colsum_floats there; split s of a split reduction into row
@@ -61,6 +63,7 @@ struct GemmParams {
   float* colsum_work;
   long colsum_floats;
   int* colsum_rows;
+  int colsum_a;
   // Split reductions: with splits > 1 (set by the launchers, which also point
   // C at the partials) workgroup row blockIdx.y multiplies k in
   // [y * split_k, (y + 1) * split_k) and stores its fp32 partial of the whole
@@ -87,7 +90,7 @@ hipError_t gemm_bf16(const GemmParams& p, hipStream_t s);
 // Workspace of a product of [M, N] over nseg segments of seg each: floats of
 // split_work that it can make use of, and of colsum_work that column sums need.
 struct GemmWork {
-  long split_floats, colsum_floats;
+  long split_floats, colsum_floats, colsum_a_floats;
 };
 GemmWork gemm_bf16_work(long M, long N, long nseg, long seg, bool tn);  // tn: A and B m/n-contiguous
 GemmWork gemm_f32_work(long M, long N, long nseg, long seg);

@@ -125,30 +125,39 @@ struct Copier {
 };
 
 // Column sums over k of the staged m/n-contiguous B tiles ([BK][BN] bf16,
-// 16-byte chunks swizzled by k-row), accumulated over the k-tiles a
-// workgroup takes part for: thread t (of NTH) owns chunk column t % (BN / 8)
-// and k-rows t / (BN / 8) + R i of every tile (R row groups), 8 fp32 partial
-// sums.  finish() adds the R partials of each column in a fixed order through
-// LDS and stores the workgroup's row of partial sums, so the result is
-// reproducible.
-template <int BN, int BK, int NTH = 512>
+// 16-byte chunks swizzled by k-row), or A tiles, accumulated over the k-tiles a
+// workgroup takes part for: of `ROWS` columns, thread t (of NTH) owns chunk column
+// t % (ROWS / 8) and k-rows t / (ROWS / 8) + R i of every tile (R row groups), 8
+// fp32 partial sums.  finish() adds the R partials of each column in a fixed order
+// through LDS and stores the workgroup's row of partial sums, so the result is
+// reproducible.  Which operand and whether any is uniform to the launch.
+template <int BM, int BN, int BK, int A_BYTES, int NTH = 512>
 struct ColSums {
-  static constexpr int CC = BN / 8, R = NTH / CC, RPT = BK / R;
-  static_assert(BK % R == 0, "row groups");
-  static constexpr int RED_BYTES = R * BN * 4;
+  static constexpr int RED_BYTES = NTH * 8 * 4;
   float s[8];
-  int cc, rg;
-  __device__ __forceinline__ void init(int tid) {
-    cc = tid % CC;
-    rg = tid / CC;
+  bool on, of_a;
+  int next, every, row, c0, n;   // k-tile to sum, step to the one after, row and first column of the partial sums
+  __device__ __forceinline__ void init(const GemmParams& p, bool first, int tm, int tn, int split, int m0, int n0,
+                                       int tid) {
+    on = p.colsum_work != nullptr && first;
+    of_a = p.colsum_a != 0;
+    next = of_a ? tn : tm;
+    every = of_a ? (p.N + BN - 1) / BN : (p.M + BM - 1) / BM;
+    row = split * every + next;
+    c0 = of_a ? m0 : n0;
+    n = of_a ? p.M : p.N;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] = 0.f;
   }
-  __device__ __forceinline__ void tile(const char* tb) {
+  template <int ROWS>
+  __device__ __forceinline__ void add(const char* tb) {
+    constexpr int CC = ROWS / 8, R = NTH / CC, RPT = BK / R;
+    static_assert(BK % R == 0, "row groups");
+    const int cc = threadIdx.x % CC, rg = threadIdx.x / CC;
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       const int k = rg + R * i;
-      const uint4 v = *(const uint4*)(tb + k * (BN * 2) + ((cc ^ swz_mn<BN>(k)) << 4));
+      const uint4 v = *(const uint4*)(tb + k * (ROWS * 2) + ((cc ^ swz_mn<ROWS>(k)) << 4));
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -157,19 +166,41 @@ struct ColSums {
       }
     }
   }
-  // red: RED_BYTES of LDS that no wave touches meanwhile; every wave calls it.
-  __device__ __forceinline__ void finish(float* red, const GemmParams& p, int row, int n0, int tid) {
+  // st: the stage of k-tile t
+  __device__ __forceinline__ void tile(const char* st, int t) {
+    if (!on || t != next) return;
+    if constexpr (BM == BN) {
+      add<BN>(st + (of_a ? 0 : A_BYTES));
+    } else {
+      if (of_a) add<BM>(st);
+      else add<BN>(st + A_BYTES);
+    }
+    next += every;
+  }
+  template <int ROWS>
+  __device__ __forceinline__ void store(float* red, const GemmParams& p, int tid) {
+    constexpr int CC = ROWS / 8, R = NTH / CC;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[rg * BN + 8 * cc + e] = s[e];
+    for (int e = 0; e < 8; ++e) red[(tid / CC) * ROWS + 8 * (tid % CC) + e] = s[e];
     __syncthreads();
-    if (tid < BN) {
+    if (tid < ROWS) {
       float t = 0.f;
 #pragma unroll 8
-      for (int r = 0; r < R; ++r) t += red[r * BN + tid];
-      const int n = n0 + tid;
-      if (n < p.N) p.colsum_work[(long)row * p.N + n] = t;
+      for (int r = 0; r < R; ++r) t += red[r * ROWS + tid];
+      const int c = c0 + tid;
+      if (c < n) p.colsum_work[(long)row * n + c] = t;
     }
     __syncthreads();
+  }
+  // red: RED_BYTES of LDS that no wave touches meanwhile; every wave calls it.
+  __device__ __forceinline__ void finish(float* red, const GemmParams& p, int tid) {
+    if (!on) return;
+    if constexpr (BM == BN) {
+      store<BN>(red, p, tid);
+    } else {
+      if (of_a) store<BM>(red, p, tid);
+      else store<BN>(red, p, tid);
+    }
   }
 };
 
@@ -503,14 +534,12 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // column sums of B (a workgroup-uniform condition)
+  // column sums (a workgroup-uniform condition)
   constexpr bool CS = !AK && !BKC;  // weight-gradient layout only
   // Every tile-row takes part in the column sums for one k-tile in tiles_m, so
   // the extra work spreads evenly over the launch.
-  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
-  int cs_next = tm;  // next k-tile this workgroup sums
-  ColSums<BN, BK> cs;
-  if (cs_on) cs.init(threadIdx.x);
+  ColSums<BM, BN, BK, A_BYTES> cs;
+  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -553,10 +582,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
     if constexpr (CS) {
       // while the tile's MFMAs drain; the stage stays valid until the next barrier
       __builtin_amdgcn_sched_barrier(0);
-      if (cs_on && t == cs_next) {
-        cs.tile(st + A_BYTES);
-        cs_next += tiles_m;
-      }
+      cs.tile(st, t);
     }
     sc = sc + 1 == NST ? 0 : sc + 1;
     si = si + 1 == NST ? 0 : si + 1;
@@ -566,9 +592,9 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
   // LDS is free once every wave is past its last k-tile.
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
-  static_assert(ColSums<BN, BK>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    if (cs_on) cs.finish((float*)lds, p, split * tiles_m + tm, n0, threadIdx.x);
+    cs.finish((float*)lds, p, threadIdx.x);
   }
   float* sm = (float*)(lds + wave * EPI_BYTES);
   epilogue<EPI, TN, 0, TM, true, TM>(p, acc, sm, m0 + wm * (BM / 2), n0 + wn * (BN / WN_), lane, c_off);
@@ -595,7 +621,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
   constexpr int EPI_BYTES = 32 * (32 * TN + 8) * 4;
   constexpr int LDS_BYTES = NST * STAGE > STAGE + NW * EPI_BYTES ? NST * STAGE : STAGE + NW * EPI_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "LDS");
-  static_assert(ColSums<BN, BK>::RED_BYTES <= NW * EPI_BYTES, "column-sum reduction fits above stage 0");
+  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= NW * EPI_BYTES, "column-sum reduction fits above stage 0");
   __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
 
   const int lane = threadIdx.x & 63;
@@ -631,7 +657,6 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     wk.next(p, 0, 0);
   };
   constexpr bool CS = !AK && !BKC;
-  const bool cs_on = CS && p.colsum_work != nullptr;
 
   int i = blockIdx.x >> 3;
   if (i >= nx) return;
@@ -648,9 +673,8 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][j][r] = 0.f;
   while (true) {
-    int cs_next = tm;
-    ColSums<BN, BK> cs;
-    if (cs_on) cs.init(threadIdx.x);
+    ColSums<BM, BN, BK, A_BYTES> cs;
+    if constexpr (CS) cs.init(p, true, tm, n0 / BN, 0, m0, n0, threadIdx.x);
     int sc = 0, si = 1;
     bf16x8 pa[4], pb[TN];  // the deferred last k-step of each k-tile (mma_tile)
     mma_pending_clear<4, TN>(pa, pb);
@@ -670,10 +694,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
       if (refill) wk.next(p, 0, 0);
       if constexpr (CS) {
         __builtin_amdgcn_sched_barrier(0);
-        if (cs_on && t == cs_next) {
-          cs.tile(st + A_BYTES);
-          cs_next += tiles_m;
-        }
+        cs.tile(st, t);
       }
       sc ^= 1;
       si ^= 1;
@@ -681,7 +702,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     if constexpr (DEFER) mma_flush<4, TN>(acc, pa, pb);
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();  // every wave is past the last k-tile: both stages are free
-    const int cm0 = m0, cn0 = n0, ctm = tm;
+    const int cm0 = m0, cn0 = n0;
     const int inext = i + nq;
     if (inext < nx) {
       tile_of(inext, m0, n0, tm);
@@ -691,7 +712,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     }
     char* above = lds + STAGE;
     if constexpr (CS) {
-      if (cs_on) cs.finish((float*)above, p, ctm, cn0, threadIdx.x);
+      cs.finish((float*)above, p, threadIdx.x);
     }
     // (the gradient-accumulating epilogue with its inputs fetched a block-row
     // ahead does not fit the registers next to the next tile's copy state)
@@ -851,14 +872,12 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // column sums of B (a workgroup-uniform condition)
+  // column sums (a workgroup-uniform condition)
   constexpr bool CS = !AK && !BKC;  // weight-gradient layout only
   // Every tile-row takes part in the column sums for one k-tile in tiles_m, so
   // the extra work spreads evenly over the launch.
-  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
-  int cs_next = tm;  // next k-tile this workgroup sums
-  ColSums<BN, BK> cs;
-  if (cs_on) cs.init(threadIdx.x);
+  ColSums<BM, BN, BK, A_BYTES> cs;
+  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -905,10 +924,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
       load_unit<BM, BN, AK, BKC, TN, NKS, BK>(af, bfr, st, st + A_BYTES, fa, fb, u);
       if (refill) ca.issue(wk.a, dst, wave, p.lda, p.M, wk.k, wk.kend);
       if constexpr (CS) {
-        if (u == 0 && cs_on && t == cs_next) {
-          cs.tile(st + A_BYTES);
-          cs_next += tiles_m;
-        }
+        if (u == 0) cs.tile(st, t);
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the unit's fragments are in registers
       if (grp == 1 && u == U - 1) wait_next(t, SPLIT && U == 1);
@@ -928,9 +944,9 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
 
   // LDS is free once every wave is past its last k-tile.
   __syncthreads();
-  static_assert(ColSums<BN, BK>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    if (cs_on) cs.finish((float*)lds, p, split * tiles_m + tm, n0, threadIdx.x);
+    cs.finish((float*)lds, p, threadIdx.x);
   }
   // The partner's slot is read only by this wave, so after the reduction it
   // serves as this wave's epilogue tile.  (The gradient-accumulating

@@ -36,5 +36,6 @@ GemmWork gemm_bf16_work(long M, long N, long nseg, long seg, bool tn) {
   // within that room
   const GemmPlan pl =
       plan_bf16(M, N, nseg * ((seg + 63) / 64) * 64, tn, 1, GEMM_SPLIT_MAX_FLOATS, -1, 256);
-  return {pl.split_floats, std::max(pl.colsum_rows(M), (M + 255) / 256) * N};
+  return {pl.split_floats, std::max(pl.colsum_rows(M), (M + 255) / 256) * N,
+          std::max(pl.colsum_a_rows(N), (N + 255) / 256) * M};
 }

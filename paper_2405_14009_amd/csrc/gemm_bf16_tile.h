@@ -68,13 +68,11 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // Column sums of B (bias gradients): tile-row tm takes the k-tiles t of its
-  // split with t mod tiles_m == tm, into row split * tiles_m + tm.
+  // Column sums (bias gradients): tile-row tm takes the k-tiles t of its split
+  // with t mod tiles_m == tm, into row split * tiles_m + tm.
   constexpr bool CS = !AK && !BKC;
-  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
-  int cs_next = tm;
-  ColSums<BN, BK, 256> cs;
-  if (cs_on) cs.init(threadIdx.x);
+  ColSums<BM, BN, BK, A_BYTES, 256> cs;
+  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -129,10 +127,7 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
     }
     if constexpr (CS) {
       __builtin_amdgcn_sched_barrier(0);
-      if (cs_on && t == cs_next) {
-        cs.tile(st + A_BYTES);
-        cs_next += tiles_m;
-      }
+      cs.tile(st, t);
     }
     sc = sc + 1 == NST ? 0 : sc + 1;
     si = si + 1 == NST ? 0 : si + 1;
@@ -154,9 +149,9 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
   }
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
-  static_assert(ColSums<BN, BK, 256>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<BM, BN, BK, A_BYTES, 256>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    if (cs_on) cs.finish((float*)lds, p, split * tiles_m + tm, n0, threadIdx.x);
+    cs.finish((float*)lds, p, threadIdx.x);
   }
   epilogue<EPI, TN, 0, TM, true, TM>(p, acc, (float*)(lds + wave * EPI_BYTES), m0 + wm * (BM / 2),
                                      n0 + wn * (BN / 2), lane, c_off);
@@ -228,9 +223,12 @@ hipError_t launch_bf16(GemmParams p, hipStream_t s) {
   const bool whole = z == 1 && p.krange == KR_FULL && !p.causal_skip;
   const int cus = device_compute_units();
   const GemmPlan pl = plan_bf16(p.M, p.N, p.K, !AK && !BKC, z, whole && p.split_work ? p.split_floats : 0,
-                                p.colsum_work != nullptr ? p.colsum_floats : -1, cus);
-  if (p.colsum_work != nullptr && pl.colsum_rows(p.M) * p.N > p.colsum_floats) return hipErrorInvalidValue;
-  if (p.colsum_work != nullptr) *p.colsum_rows = (int)pl.colsum_rows(p.M);
+                                p.colsum_work != nullptr ? p.colsum_floats : -1, cus, p.colsum_a);
+  if (p.colsum_work != nullptr) {
+    const long rows = p.colsum_a ? pl.colsum_a_rows(p.N) : pl.colsum_rows(p.M);
+    if (rows * (p.colsum_a ? p.M : p.N) > p.colsum_floats) return hipErrorInvalidValue;
+    *p.colsum_rows = (int)rows;
+  }
   p.splits = 1;
   if (pl.splits == 1) return launch_tiles<AK, BKC, EPI>(p, pl, s);
   GemmParams q = p;

@@ -358,7 +358,7 @@ hipError_t launch_epi(const GemmParams& p, hipStream_t s) {
 }  // namespace
 
 GemmWork gemm_f32_work(long M, long N, long nseg, long seg) {
-  return {plan_f32(M, N, nseg, seg, 1, GEMM_SPLIT_MAX_FLOATS, 256).split_floats, 0};
+  return {plan_f32(M, N, nseg, seg, 1, GEMM_SPLIT_MAX_FLOATS, 256).split_floats, 0, 0};
 }
 
 hipError_t gemm_f32(const GemmParams& p, hipStream_t s) {

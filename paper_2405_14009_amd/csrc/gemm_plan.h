@@ -13,6 +13,7 @@ struct GemmPlan {
   int splits, split_k;  // split_k: k per split, a multiple of 64
   long split_floats;    // partials: splits * M * N
   long colsum_rows(long M) const { return (M + bm - 1) / bm * splits; }
+  long colsum_a_rows(long N) const { return (N + bn - 1) / bn * splits; }   // of sums of A
 };
 
 // A kernel's time: `fix` around its first round of workgroups, `again` around
@@ -63,9 +64,10 @@ inline double split_us(int splits, long M, long N) { return 2.25 + 0.107 * split
 // average 1.1 % / 0.8 % more than the fastest measured one (3.2 % / 3.7 % with
 // fits of fewer shapes, whose partial rounds were too cheap: 1.5 rounds of
 // 256x256 tiles over K 12288 take 551 us, three of 256x128 512).
-// room_floats: split workspace; colsum_floats: what colsum_rows may take (< 0:
-// no column sums).  256x256 tiles unsplit always qualify.
-inline GemmPlan plan_bf16(long M, long N, long K, bool tn, long z, long room_floats, long colsum_floats, int cus) {
+// room_floats: split workspace; colsum_floats: what colsum_rows (colsum_a:
+// colsum_a_rows) may take (< 0: no column sums).  256x256 tiles unsplit always qualify.
+inline GemmPlan plan_bf16(long M, long N, long K, bool tn, long z, long room_floats, long colsum_floats, int cus,
+                          bool colsum_a = false) {
   struct Kind {
     GemmTile t;
     int bm, bn;
@@ -84,12 +86,13 @@ inline GemmPlan plan_bf16(long M, long N, long K, bool tn, long z, long room_flo
   double best_us = 1e30;
   for (const Kind& q : kinds) {
     if (tn && q.t == TILE_192x256) continue;  // whole 64-row blocks of a k-contiguous A only
-    const long rows = (M + q.bm - 1) / q.bm, tiles = rows * ((N + q.bn - 1) / q.bn);
+    const long rows = (M + q.bm - 1) / q.bm, cols = (N + q.bn - 1) / q.bn, tiles = rows * cols;
+    const long sums = colsum_a ? cols * M : rows * N;
     for (int want = 1; want <= (q.t == TILE_32 ? 1 : 32); ++want) {
       const long per = (nk + want - 1) / want;
       if ((nk + per - 1) / per != want) continue;  // a split without a k-tile
       if (want > 1 && (per < 2 || want * M * N > room_floats)) break;
-      if (colsum_floats >= 0 && (q.t != TILE_256 || want > 1) && rows * want * N > colsum_floats) break;
+      if (colsum_floats >= 0 && (q.t != TILE_256 || want > 1) && sums * want > colsum_floats) break;
       // the waves of a 32x32 tile take every fourth k-tile each
       GemmCost c = tn ? q.ctn : q.c;
       if (want > 1) {

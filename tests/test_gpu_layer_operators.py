@@ -331,6 +331,26 @@ def test_linear_larger_tiles(rows, i, o, kind):
     check_linear(rows, i, o, kind, None, by_out=True)
 
 
+@pytest.mark.parametrize("by_out", [False, True])
+@pytest.mark.parametrize("rows,i,o", [(1, 4096, 4096), (100, 256, 200), (640, 1024, 1024), (300, 4096, 4096), (1111, 2048, 8192),
+                                      (2048, 4096, 12288), (9001, 4096, 12288), (20000, 512, 512), (5000, 1536, 768),
+                                      (40, 64, 16384), (3, 16384, 64)])
+def test_bias_gradient_of_every_tile(rows, i, o, by_out):
+    """Sums on the way of the product, whatever tile and split the sizes take; the weight's gradient is
+    that of a call without them."""
+    x, dy = normal(1, rows, i), normal(2, rows, o, std=0.1)
+    dw, db = ops().linear_backward_weight(x, dy, by_out=by_out)
+    ref.close("db", db, *ref.column_sums(ref.wide(dy), 0.0))
+    plain, _ = ops().linear_backward_weight(x, dy, by_out=by_out, bias_grad=False)
+    # in another order at most
+    mag = (rows + 2) * ref.U * (x.float().abs().t() @ dy.float().abs())
+    assert ((dw - plain).abs() <= 2.01 * mag).all()
+    old = torch.ones(o, device="cuda")
+    _, db2 = ops().linear_backward_weight(x, dy, by_out=by_out, weight_grad=torch.zeros_like(dw), bias_grad=old,
+                                          accumulate=True)
+    assert torch.equal(db2, db + 1.0)
+
+
 @KINDS
 def test_linear_of_columns_of_a_wider_matrix(kind):
     for rows in (1, 9, 150):

@@ -3,6 +3,9 @@
 compute call runs here."""
 import ctypes
 import math
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -129,6 +132,41 @@ def test_linear_memory(r, i, o, dtype):
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o, by_out=by_out)), *map(REF, n)) == 0
         assert n[2].value >= 4 * o       # a row of the bias gradient's sums at least
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o)), None, None, None) == 0
+
+
+PLAN = r"""
+#include <cstdio>
+#include "gemm_plan.h"
+int main() {
+  const long dims[] = {8, 24, 40, 64, 136, 256, 264, 640, 1024, 1288, 5120, 16384};
+  const long depths[] = {8, 72, 512, 2048, 6000, 65536};
+  for (long M : dims) for (long N : dims) for (long K : depths) for (long room : {0L, 1L << 20, 16L << 20})
+    for (int cus : {64, 256, 304}) {
+      const long least = (N + 255) / 256 * M;   // what a caller provides at least
+      for (long sums : {least, 4 * least}) {
+        const GemmPlan p = plan_bf16(M, N, K, true, 1, room, sums, cus, true);
+        if (p.colsum_a_rows(N) != (N + p.bn - 1) / p.bn * p.splits || p.colsum_a_rows(N) * M > sums) {
+          std::printf("M %ld N %ld K %ld room %ld cus %d\n", M, N, K, room, cus);
+          return 1;
+        }
+      }
+    }
+  return 0;
+}
+"""
+
+
+def test_plans_leave_room_for_the_left_operand_s_sums(tmp_path):
+    """The choice of tile and split where a product sums its left operand's columns."""
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no host compiler")
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2405_14009_amd", "csrc")
+    (tmp_path / "main.cpp").write_text(PLAN)
+    exe = str(tmp_path / "main")
+    subprocess.run([cxx, "-std=c++17", "-O2", "-I", csrc, str(tmp_path / "main.cpp"), "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stdout
 
 
 # -- refusals ------------------------------------------------------------------------
