@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "gemm.h"
+#include "linear_few.h"
 
 namespace {
 
@@ -67,7 +68,12 @@ bool sums_in_product(const LinearArgs& a) { return a.dbias && a.elt == 2; }
 struct WeightWork {
   long split, sums;
 };
+// Few tokens: no tiles.  (A grid's second dimension holds 2^16 - 1.)
+bool few(const LinearArgs& a) {
+  return a.rows > 0 && a.rows <= few_tokens_most(a.elt) && std::max(a.in, a.out) < 1 << 21;
+}
 WeightWork weight_work(const LinearArgs& a) {
+  if (few(a)) return {0, 0};
   const long each = part_rows(a.elt, a.in, a.out);
   const long m = a.by_out ? a.out : a.in, n = a.by_out ? a.in : a.out;
   const long full = std::max(1L, std::min(a.rows, each)), rest = a.rows > each ? a.rows % each : 0;
@@ -149,6 +155,11 @@ hipError_t linear_backward_input(const LinearArgs& args, hipStream_t s) {
 
 hipError_t linear_backward_weight(const LinearArgs& args, hipStream_t s) {
   LinearArgs a = args;
+  if (few(a)) {
+    const int m = a.by_out ? a.out : a.in, n = a.by_out ? a.in : a.out;
+    return few_tokens({(int)a.rows, m, n, a.by_out ? a.dy : a.x, a.by_out ? a.x : a.dy, a.dw, a.dbias, !a.by_out,
+                       a.accumulate}, a.elt, s);
+  }
   const long each = part_rows(a.elt, a.x.stride, a.dy.stride);
   const WeightWork w = weight_work(a);
   float* const sums = (float*)a.work + w.split;

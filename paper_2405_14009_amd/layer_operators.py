@@ -435,7 +435,7 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
         weight_grad = weight_grad.t()
     dw = _gradient(weight_grad, "weight_grad", shape, x)
     dbias = _gradient(bias_grad, "bias_grad", (fan_out,), x)
-    work = _work(work_bytes, x)
+    work = _work(work_bytes, x) if work_bytes else None
     _call(L.load().rc_linear_backward_weight, device, c, _ref(_Matrix(x.data_ptr(), step)),
           _ref(_Matrix(dy.data_ptr(), dstep)), dw.data_ptr(), _address(dbias), more, _address(work))
     return (dw.t() if by_out else dw), dbias

@@ -262,7 +262,7 @@ def test_no_rows():
 
 # -- linear ------------------------------------------------------------------------
 
-LINEAR = [(1, 8, 8), (1, 256, 1024), (2, 1024, 64), (3, 64, 200), (7, 520, 24), (17, 72, 1000), (31, 136, 136), (32, 8, 512),
+LINEAR = [(1, 8, 8), (1, 256, 1024), (4, 40, 1032), (5, 1032, 40), (8, 24, 2088), (9, 72, 2056), (2, 1024, 64), (3, 64, 200), (7, 520, 24), (17, 72, 1000), (31, 136, 136), (32, 8, 512),
           (33, 64, 64), (65, 1040, 8), (129, 200, 328), (257, 264, 136), (300, 2048, 72), (1000, 24, 16), (70, 8, 4096),
           (513, 520, 520)]
 

@@ -130,7 +130,8 @@ def test_linear_memory(r, i, o, dtype):
     for by_out in (0, 1):
         n = [ctypes.c_size_t() for _ in range(3)]
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o, by_out=by_out)), *map(REF, n)) == 0
-        assert n[2].value >= 4 * o       # a row of the bias gradient's sums at least
+        # a row of the bias gradient's sums at least, but for few tokens, which take none
+        assert n[2].value >= 4 * o or 0 < r <= 32
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o)), None, None, None) == 0
 
 
@@ -315,7 +316,7 @@ def test_linear_refusals():
         refused(fwd(l=big, x=at(0, 8192), work=None), "INVALID_ARG", b"work")
     refused(lib.rc_linear_backward_input(REF(linear()), at(0), at(1), at(2), at(2), W, None), "INVALID_ARG", b"overlaps")
     wt = lambda dw=place(4), db=None, acc=0, work=W: lib.rc_linear_backward_weight(  # noqa: E731
-        REF(linear()), at(0), at(1), dw, db, acc, work, None)
+        REF(linear(rows=40)), at(0), at(1), dw, db, acc, work, None)
     refused(wt(dw=None), "INVALID_ARG", b"null dweight")
     refused(wt(dw=place(4) + 4), "INVALID_ARG", b"16 bytes")
     refused(wt(acc=2), "INVALID_ARG", b"accumulate")
