@@ -40,6 +40,7 @@ struct GemmParams {
   const void* B; long ldb; int b_kcontig;
   int batch, heads;
   long a_bs, a_hs, b_bs, b_hs, c_bs, c_hs;
+  int stream;       // bf16: few rows of A, the plan of a large B that is read once (plan_stream)
   int causal_skip;  // skip output tiles strictly above the diagonal (n0 > m0 + BM - 1)
   int krange;       // KRange
   int epi;          // EpiKind

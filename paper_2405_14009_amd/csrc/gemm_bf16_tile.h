@@ -222,8 +222,10 @@ hipError_t launch_bf16(GemmParams p, hipStream_t s) {
   const long z = (long)p.batch * p.heads;
   const bool whole = z == 1 && p.krange == KR_FULL && !p.causal_skip;
   const int cus = device_compute_units();
-  const GemmPlan pl = plan_bf16(p.M, p.N, p.K, !AK && !BKC, z, whole && p.split_work ? p.split_floats : 0,
-                                p.colsum_work != nullptr ? p.colsum_floats : -1, cus, p.colsum_a);
+  const long room = whole && p.split_work ? p.split_floats : 0;
+  const GemmPlan pl = p.stream ? plan_stream(p.M, p.N, p.K, room, cus)
+                               : plan_bf16(p.M, p.N, p.K, !AK && !BKC, z, room,
+                                           p.colsum_work != nullptr ? p.colsum_floats : -1, cus, p.colsum_a);
   if (p.colsum_work != nullptr) {
     const long rows = p.colsum_a ? pl.colsum_a_rows(p.N) : pl.colsum_rows(p.M);
     if (rows * (p.colsum_a ? p.M : p.N) > p.colsum_floats) return hipErrorInvalidValue;

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 
 enum GemmTile { TILE_256 = 0, TILE_256x128 = 1, TILE_128 = 2, TILE_64 = 3, TILE_32 = 4, TILE_192x256 = 5 };
 
@@ -108,6 +109,30 @@ inline GemmPlan plan_bf16(long M, long N, long K, bool tn, long z, long room_flo
     }
   }
   return best;
+}
+
+// Few rows of A (a block of 64) over a B of many megabytes: the reading of B is all
+// the time, at the pace of the compute units that take part (about 24 GB/s each), so
+// the reduction is split until whole rounds of them do.  plan_bf16, whose costs are
+// those of operands in the caches, leaves half of them out (1 row over 8192 x 8192,
+// n-contiguous: 42 us, so 25; 134 MB take 27 at the rate of a large copy).
+inline GemmPlan plan_stream(long M, long N, long K, long room_floats, int cus) {
+  const long nk = std::max(1L, (K + 63) / 64), rows = (M + 63) / 64, tiles = rows * ((N + 63) / 64);
+  GemmPlan p{TILE_64, 64, 64, tiles, 1, (int)(nk * 64), 0};
+  double best = 0.0;
+  for (long want = 1; want <= 32; ++want) {
+    const long per = (nk + want - 1) / want;
+    if ((nk + per - 1) / per != want) continue;
+    if (want > 1 && (per < 2 || want * M * N > room_floats)) break;
+    const double load = (double)tiles * want / cus;
+    const double used = load / std::ceil(load) - 0.02 * want;   // of the last round's units; a split costs its partials
+    if (want > 1 && used <= best) continue;
+    best = used;
+    p.splits = (int)want;
+    p.split_k = (int)(per * 64);
+    p.split_floats = want > 1 ? want * M * N : 0;
+  }
+  return p;
 }
 
 // Whether an operand of a 128-row tile spans more bytes than the 2^31 that the

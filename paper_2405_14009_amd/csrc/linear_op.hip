@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "gemm.h"
+#include "gemm_plan.h"
 #include "linear_few.h"
 
 namespace {
@@ -38,10 +39,21 @@ GemmWork work_of(int elt, long m, long n, long k, bool tn) {
   return elt == 2 ? gemm_bf16_work(m, n, 1, k, tn) : gemm_f32_work(m, n, 1, k);
 }
 
+// Whether a product of n columns over k is the reading of its weight (plan_stream).
+// kcontig: weights whose reduced dimension is the contiguous one.  Below 32 MB, with
+// those 64 MB, one unsplit launch is as fast.
+bool streams(int elt, long rows, long n, long k, bool kcontig) {
+  return elt == 2 && rows <= 64 && n * k >= (kcontig ? 32L << 20 : 16L << 20);
+}
+
 // Floats of split workspace for a product over `rows`, sized for operands without
 // gaps between their rows (a call with others runs in more parts, which split
-// within that room).
-long split_floats(int elt, long rows, long n, long k) {
+// within that room).  Small products of few rows are not split: one launch of 32x32
+// tiles takes no longer than two (1 row over 4096 x 1024: 9 and 15 us, of which each
+// launch takes the host 3.5) until its chain of k-tiles is the longer one.
+long split_floats(int elt, long rows, long n, long k, bool kcontig) {
+  if (streams(elt, rows, n, k, kcontig)) return plan_stream(rows, n, k, GEMM_SPLIT_MAX_FLOATS, 256).split_floats;
+  if (elt == 2 && rows <= 32 && (kcontig ? k <= 8192 : k <= 4096 && n <= 2048)) return 0;
   const long each = part_rows(elt, k, 0);
   const long full = std::min(rows, each), rest = rows > each ? rows % each : 0;
   long f = work_of(elt, std::max(1L, full), n, k, false).split_floats;
@@ -92,10 +104,10 @@ WeightWork weight_work(const LinearArgs& a) {
 }  // namespace
 
 size_t linear_forward_work(const LinearArgs& a) {
-  return sizeof(float) * (size_t)split_floats(a.elt, a.rows, a.out, a.in);
+  return sizeof(float) * (size_t)split_floats(a.elt, a.rows, a.out, a.in, a.by_out);
 }
 size_t linear_input_work(const LinearArgs& a) {
-  return sizeof(float) * (size_t)split_floats(a.elt, a.rows, a.in, a.out);
+  return sizeof(float) * (size_t)split_floats(a.elt, a.rows, a.in, a.out, !a.by_out);
 }
 size_t linear_weight_work(const LinearArgs& a) {
   const WeightWork w = weight_work(a);
@@ -106,7 +118,7 @@ hipError_t linear_forward(const LinearArgs& args, hipStream_t s) {
   LinearArgs a = args;
   if (a.rows == 0) return hipSuccess;
   const long each = part_rows(a.elt, a.x.stride, 0);
-  const long split = split_floats(a.elt, a.rows, a.out, a.in);
+  const long split = split_floats(a.elt, a.rows, a.out, a.in, a.by_out);
   return parts(a.rows, each, [&](long r, long m) {
     GemmParams p = params(m, a.out, a.in, EPI_LINEAR);
     p.A = at(a.x, r, a.elt);
@@ -115,6 +127,7 @@ hipError_t linear_forward(const LinearArgs& args, hipStream_t s) {
     p.B = a.w.data;
     p.ldb = a.w.stride;
     p.b_kcontig = a.by_out;
+    p.stream = streams(a.elt, a.rows, p.N, p.K, p.b_kcontig);
     p.C = at(a.y, r, a.elt);
     p.ldc = a.y.stride;
     p.bias = (const float*)a.bias;
@@ -134,7 +147,7 @@ hipError_t linear_backward_input(const LinearArgs& args, hipStream_t s) {
   LinearArgs a = args;
   if (a.rows == 0) return hipSuccess;
   const long each = part_rows(a.elt, a.dy.stride, 0);
-  const long split = split_floats(a.elt, a.rows, a.in, a.out);
+  const long split = split_floats(a.elt, a.rows, a.in, a.out, !a.by_out);
   return parts(a.rows, each, [&](long r, long m) {
     GemmParams p = params(m, a.in, a.out, a.before.data ? EPI_GELU_BWD : EPI_STORE);
     p.A = at(a.dy, r, a.elt);
@@ -143,6 +156,7 @@ hipError_t linear_backward_input(const LinearArgs& args, hipStream_t s) {
     p.B = a.w.data;
     p.ldb = a.w.stride;
     p.b_kcontig = !a.by_out;
+    p.stream = streams(a.elt, a.rows, p.N, p.K, p.b_kcontig);
     p.C = at(a.dx, r, a.elt);
     p.ldc = a.dx.stride;
     p.aux = at(a.before, r, a.elt);

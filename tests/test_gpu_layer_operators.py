@@ -332,6 +332,22 @@ def test_linear_larger_tiles(rows, i, o, kind):
 
 
 @pytest.mark.parametrize("by_out", [False, True])
+@pytest.mark.parametrize("rows,i,o", [(1, 8192, 4104), (3, 1024, 20480), (64, 4104, 8192), (33, 2048, 8200), (65, 4096, 4096),
+                                      (1, 4096, 1024), (32, 1032, 4104), (2, 16384, 2056)])
+def test_linear_of_few_rows_and_a_large_weight(rows, i, o, by_out):
+    """Plans of few rows: the weight streamed by the whole card, or one launch."""
+    x, dy, b = normal(1, rows, i), normal(2, rows, o, std=0.1), normal(3, o, kind=F32)
+    w = normal(4, i, o, std=i ** -0.5)
+    if by_out:
+        w = w.t().contiguous().t()
+    X, W, DY = ref.wide(x), ref.wide(w), ref.wide(dy)
+    y, _ = ops().linear_forward(x, w, b)
+    u, e = ref.product(X, W)
+    ref.close("y", y, u + ref.wide(b), e + ref.U * (np.abs(u) + np.abs(ref.wide(b))))
+    ref.close("dx", ops().linear_backward_input(dy, w), *ref.product(DY, W.T))
+
+
+@pytest.mark.parametrize("by_out", [False, True])
 @pytest.mark.parametrize("rows,i,o", [(1, 4096, 4096), (100, 256, 200), (640, 1024, 1024), (300, 4096, 4096), (1111, 2048, 8192),
                                       (2048, 4096, 12288), (9001, 4096, 12288), (20000, 512, 512), (5000, 1536, 768),
                                       (40, 64, 16384), (3, 16384, 64)])

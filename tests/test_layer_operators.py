@@ -152,13 +152,22 @@ int main() {
         }
       }
     }
+  for (long M : {1L, 16L, 64L}) for (long N : dims) for (long K : depths) for (long room : {0L, 1L << 16, 16L << 20})
+    for (int cus : {64, 256, 304}) {
+      const GemmPlan p = plan_stream(M, N, K, room, cus);
+      if (p.tiles != (M + 63) / 64 * ((N + 63) / 64) || p.split_k % 64 || p.splits * (long)p.split_k < K ||
+          (p.splits - 1) * (long)p.split_k >= K || p.split_floats > room || (p.splits > 1) != (p.split_floats > 0)) {
+        std::printf("stream M %ld N %ld K %ld room %ld cus %d\n", M, N, K, room, cus);
+        return 1;
+      }
+    }
   return 0;
 }
 """
 
 
 def test_plans_leave_room_for_the_left_operand_s_sums(tmp_path):
-    """The choice of tile and split where a product sums its left operand's columns."""
+    """The choice of tile and split where a product sums its left operand's columns, and of few rows."""
     cxx = shutil.which("g++")
     if cxx is None:
         pytest.skip("no host compiler")
