@@ -63,18 +63,25 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& turn, c
   }
 }
 
-// Runs work(row data, row, next row) over the rows of a workgroup; work fetches the
-// next row's data as soon as it has this row's numbers, so that its loads are in
-// flight during the rest.  All threads go through the same number of steps (work
-// has barriers); rows beyond the last are the work's to leave out.
-template <class Row, class Fetch, class Work>
+// Runs work(row data, row, next row) over the rows of a workgroup.  AHEAD: work
+// fetches the next row's data as soon as it has this row's numbers, so that its
+// loads are in flight during the rest.  All threads go through the same number of
+// steps (work has barriers); rows beyond the last are the work's to leave out.
+template <bool AHEAD, class Row, class Fetch, class Work>
 __device__ __forceinline__ void walk_rows(long rows, int slot, int slots, Fetch fetch, Work work) {
   const long step = (long)gridDim.x * slots;
   long k = (long)blockIdx.x * slots;
   Row r;
-  fetch(r, k + slot);
-  for (; k < rows; k += step) work(r, k + slot, k + step + slot);
+  if (AHEAD) fetch(r, k + slot);
+  for (; k < rows; k += step) {
+    if (!AHEAD) fetch(r, k + slot);
+    work(r, k + slot, k + step + slot);
+  }
 }
+// Rows of more than 8192 columns hold two groups a lane in nine to sixteen waves,
+// whose registers have no room for the next row's data (and, backward, the weight,
+// which is read again from the caches): held all the same they spill.
+constexpr bool roomy(int lpr, int cpl) { return lpr > 0 || cpl == 1; }
 
 template <class E, int LPR, int CPL, bool TAIL, int NT>
 __global__ __launch_bounds__(NT) void norm_fwd_k(NormArgs a, int waves) {
@@ -84,23 +91,22 @@ __global__ __launch_bounds__(NT) void norm_fwd_k(NormArgs a, int waves) {
   const bool add = a.total.data != nullptr;
   Philox rng;
   if (a.drop.on) rng.init(a.drop);
-  float ib[CPL][8], wt[CPL][8], sh[CPL][8];
+  // the vectors' values of a group (0 or 1 where there is none)
+  auto vector = [&](const void* p, float none, int g, float(&f)[8]) {
 #pragma unroll
-  for (int q = 0; q < CPL; ++q) {
-    const int g = at.lane + at.lanes * q;
+    for (int e = 0; e < 8; ++e) f[e] = none;
+    if (p && 8 * g < a.cols) param_floats<TAIL>(load_params<TAIL>(p, a.params_f32, g, a.cols), a.params_f32, g, a.cols, f);
+  };
+  constexpr bool KEEP = roomy(LPR, CPL);
+  constexpr int KEPT = KEEP ? CPL : 1;
+  float ib[KEPT][8], wt[KEPT][8], sh[KEPT][8];
+  if constexpr (KEEP) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ib[q][e] = sh[q][e] = 0.f;
-      wt[q][e] = 1.f;
-    }
-    if (8 * g < a.cols) {
-      RawParams b, w, h;
-      if (a.bias) b = load_params<TAIL>(a.bias, a.params_f32, g, a.cols);
-      if (a.weight) w = load_params<TAIL>(a.weight, a.params_f32, g, a.cols);
-      if (a.shift) h = load_params<TAIL>(a.shift, a.params_f32, g, a.cols);
-      if (a.bias) param_floats<TAIL>(b, a.params_f32, g, a.cols, ib[q]);
-      if (a.weight) param_floats<TAIL>(w, a.params_f32, g, a.cols, wt[q]);
-      if (a.shift) param_floats<TAIL>(h, a.params_f32, g, a.cols, sh[q]);
+    for (int q = 0; q < CPL; ++q) {
+      const int g = at.lane + at.lanes * q;
+      vector(a.bias, 0.f, g, ib[q]);
+      vector(a.weight, 1.f, g, wt[q]);
+      vector(a.shift, 0.f, g, sh[q]);
     }
   }
   struct Row {
@@ -129,13 +135,14 @@ __global__ __launch_bounds__(NT) void norm_fwd_k(NormArgs a, int waves) {
       C::floats(r.res[q], g, a.cols, res[q]);
     }
     __builtin_amdgcn_sched_barrier(0);
-    fetch(r, next);
+    if (KEEP) fetch(r, next);
 #pragma unroll
     for (int q = 0; q < CPL; ++q) {
       const int g = at.lane + at.lanes * q;
       if (here && 8 * g < a.cols) {
+        if (!KEEP) vector(a.bias, 0.f, g, ib[0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[q][e] += ib[q][e];
+        for (int e = 0; e < 8; ++e) f[q][e] += ib[q % KEPT][e];
         if (a.drop.on) drop8(rng, a.drop, g, row, f[q]);
         if (a.residual.data) {
 #pragma unroll
@@ -173,8 +180,12 @@ __global__ __launch_bounds__(NT) void norm_fwd_k(NormArgs a, int waves) {
     for (int q = 0; q < CPL; ++q) {
       const int g = at.lane + at.lanes * q;
       if (8 * g < a.cols) {
+        if (!KEEP) {
+          vector(a.weight, 1.f, g, wt[0]);
+          vector(a.shift, 0.f, g, sh[0]);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * rstd * wt[q][e] + sh[q][e];
+        for (int e = 0; e < 8; ++e) f[q][e] = f[q][e] * rstd * wt[q % KEPT][e] + sh[q % KEPT][e];
         C::store((E*)a.y.data + row * a.y.stride, g, a.cols, f[q]);
       }
     }
@@ -183,7 +194,7 @@ __global__ __launch_bounds__(NT) void norm_fwd_k(NormArgs a, int waves) {
       a.stats[a.rows + row] = rstd;
     }
   };
-  walk_rows<Row>(a.rows, at.slot, at.slots, fetch, work);
+  walk_rows<roomy(LPR, CPL), Row>(a.rows, at.slot, at.slots, fetch, work);
 }
 
 template <class E, int LPR, int CPL, bool TAIL, int NT>
@@ -194,17 +205,19 @@ __global__ __launch_bounds__(NT) void norm_bwd_k(NormArgs a, int waves, int stri
   const bool sums = a.dweight || a.dshift || a.dbias, grads = a.dtotal.data || a.dx.data || a.dbias;
   Philox rng;
   if (a.drop.on) rng.init(a.drop);
-  float wt[CPL][8], sw[CPL][8], sh[CPL][8], sb[CPL][8];
+  constexpr int KEPT = roomy(LPR, CPL) ? CPL : 1;
+  float kept[KEPT][8], sw[CPL][8], sh[CPL][8], sb[CPL][8];
+  auto weight = [&](int g, float(&f)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = 1.f;
+    if (a.weight && 8 * g < a.cols)
+      param_floats<TAIL>(load_params<TAIL>(a.weight, a.params_f32, g, a.cols), a.params_f32, g, a.cols, f);
+  };
 #pragma unroll
   for (int q = 0; q < CPL; ++q) {
-    const int g = at.lane + at.lanes * q;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      wt[q][e] = 1.f;
-      sw[q][e] = sh[q][e] = sb[q][e] = 0.f;
-    }
-    if (a.weight && 8 * g < a.cols)
-      param_floats<TAIL>(load_params<TAIL>(a.weight, a.params_f32, g, a.cols), a.params_f32, g, a.cols, wt[q]);
+    for (int e = 0; e < 8; ++e) sw[q][e] = sh[q][e] = sb[q][e] = 0.f;
+    if (roomy(LPR, CPL)) weight(at.lane + at.lanes * q, kept[q % KEPT]);
   }
   struct Row {
     Raw8<E> dy[CPL], t[CPL], in[CPL];
@@ -240,18 +253,20 @@ __global__ __launch_bounds__(NT) void norm_bwd_k(NormArgs a, int waves, int stri
       in[q] = r.in[q];
     }
     __builtin_amdgcn_sched_barrier(0);
-    fetch(r, next);
+    if (roomy(LPR, CPL)) fetch(r, next);
 #pragma unroll
     for (int q = 0; q < CPL; ++q) {
       const int g = at.lane + at.lanes * q;
       if (here && 8 * g < a.cols) {
+        if (!roomy(LPR, CPL)) weight(g, kept[0]);
+        float(&wt)[8] = kept[q % KEPT];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           xh[q][e] = (xh[q][e] - mean) * rstd;
           if (!TAIL || 8 * g + e < a.cols) {
             sw[q][e] += d[q][e] * xh[q][e];
             sh[q][e] += d[q][e];
-            d[q][e] *= wt[q][e];
+            d[q][e] *= wt[e];
             m[0] += d[q][e];
             m[1] += d[q][e] * xh[q][e];
           }
@@ -282,7 +297,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_k(NormArgs a, int waves, int stri
       }
     }
   };
-  walk_rows<Row>(a.rows, at.slot, at.slots, fetch, work);
+  walk_rows<roomy(LPR, CPL), Row>(a.rows, at.slot, at.slots, fetch, work);
   if (!sums) return;
   // The row sets of the workgroup in order: into its row of partial sums, or, of the
   // only workgroup, to where they belong.
