@@ -184,7 +184,8 @@ hipError_t rows_finish(const float* part, int n, int vectors, int stride, int co
 }
 
 size_t dropout_work_bytes(long rows, int cols) {
-  return sizeof(float) * (size_t)grid_of(rows, cols, true).deep * rows_pad(cols);
+  const int deep = grid_of(rows, cols, true).deep;
+  return deep > 1 ? sizeof(float) * (size_t)deep * rows_pad(cols) : 0;
 }
 
 hipError_t dropout_rows(const DropoutArgs& a, int elt, hipStream_t s) {

@@ -41,6 +41,7 @@ struct GemmParams {
   int batch, heads;
   long a_bs, a_hs, b_bs, b_hs, c_bs, c_hs;
   int stream;       // bf16: few rows of A, the plan of a large B that is read once (plan_stream)
+  int wide;         // fp32: tiles of 128x256 as well, and the choice fitted with them
   int causal_skip;  // skip output tiles strictly above the diagonal (n0 > m0 + BM - 1)
   int krange;       // KRange
   int epi;          // EpiKind
@@ -94,7 +95,7 @@ struct GemmWork {
   long split_floats, colsum_floats, colsum_a_floats;
 };
 GemmWork gemm_bf16_work(long M, long N, long nseg, long seg, bool tn);  // tn: A and B m/n-contiguous
-GemmWork gemm_f32_work(long M, long N, long nseg, long seg);
+GemmWork gemm_f32_work(long M, long N, long nseg, long seg, bool wide = false);
 constexpr long GEMM_SPLIT_MAX_FLOATS = 16L << 20;  // most partials of one product
 hipError_t gemm_f32(const GemmParams& p, hipStream_t s);
 

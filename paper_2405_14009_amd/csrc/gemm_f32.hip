@@ -165,7 +165,6 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
   // latency and the copies' addresses would otherwise stand between every
   // barrier and its products.
   constexpr int NG = TK / 8;
-  static_assert(PER_TILE % NG == 0, "copies between the groups");
   float fa[2][NG][WM][4], fb[2][NG][WN][4];
   auto products = [&](int set, int g) {
 #pragma unroll
@@ -214,7 +213,7 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
       __builtin_amdgcn_sched_barrier(0);
       if (refill) {
 #pragma unroll
-        for (int q = 0; q < PER_TILE / NG; ++q) issue(lds + si * STAGE, g * (PER_TILE / NG) + q);
+        for (int q = g * PER_TILE / NG; q < (g + 1) * PER_TILE / NG; ++q) issue(lds + si * STAGE, q);
       }
     }
     if (refill) advance();
@@ -307,6 +306,14 @@ __global__ __launch_bounds__(128 * NWN) void gemm_f32_kernel(GemmParams p) {
 template <bool AK, bool BKC, int EPI>
 hipError_t launch_tiles(const GemmParams& p, const F32Plan& pl, int y, hipStream_t s) {
   const dim3 grid((unsigned)pl.tiles, (unsigned)y);
+  // 128x256 (the linear operator's): four blocks a wave, so half the barriers and
+  // three quarters of the copies a product (4096 cubed: 1000 us, 1075 with 128x128)
+  if constexpr (EPI == EPI_STORE || EPI == EPI_GELU_BWD || EPI == EPI_F32_ACC || EPI == EPI_F32_STORE || EPI == EPI_LINEAR) {
+    if (pl.bn == 256) {
+      hipLaunchKernelGGL((gemm_f32_kernel<2, 2, 4, 3, AK, BKC, EPI>), grid, dim3(512), 0, s, p);
+      return hipGetLastError();
+    }
+  }
   if (pl.bm == 128)
     hipLaunchKernelGGL((gemm_f32_kernel<2, 1, 4, 4, AK, BKC, EPI>), grid, dim3(512), 0, s, p);
   else if (pl.bm == 64)
@@ -342,7 +349,7 @@ hipError_t launch_epi(const GemmParams& p, hipStream_t s) {
   const bool whole = p.batch * p.heads == 1 && p.krange == KR_FULL && !p.causal_skip;
   const F32Plan pl = plan_f32(p.M, p.N, p.kseg_len > 0 ? p.K / p.kseg_len : 1, p.kseg_len > 0 ? p.kseg_len : p.K,
                               (long)p.batch * p.heads, whole && p.split_work ? p.split_floats : 0,
-                              device_compute_units());
+                              device_compute_units(), p.wide);
   switch (p.epi) {
     case EPI_STORE: return launch<AK, BKC, EPI_STORE>(p, pl, s);
     case EPI_BIAS: return launch<AK, BKC, EPI_BIAS>(p, pl, s);
@@ -357,8 +364,8 @@ hipError_t launch_epi(const GemmParams& p, hipStream_t s) {
 
 }  // namespace
 
-GemmWork gemm_f32_work(long M, long N, long nseg, long seg) {
-  return {plan_f32(M, N, nseg, seg, 1, GEMM_SPLIT_MAX_FLOATS, 256).split_floats, 0, 0};
+GemmWork gemm_f32_work(long M, long N, long nseg, long seg, bool wide) {
+  return {plan_f32(M, N, nseg, seg, 1, GEMM_SPLIT_MAX_FLOATS, 256, wide).split_floats, 0, 0};
 }
 
 hipError_t gemm_f32(const GemmParams& p, hipStream_t s) {

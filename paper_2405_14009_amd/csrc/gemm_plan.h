@@ -149,28 +149,36 @@ inline double split_f32_us(int splits, long M, long N) {
 }
 
 struct F32Plan {
-  int bm;               // tiles of bm x bm: 32, 64 or 128
+  int bm;               // tiles of bm x bn: 32, 64 or 128 square, or 128 x 256
   long tiles;
   int splits, split_k;  // split_k: k per split, a multiple of 32
   long split_floats;
+  int bn;
 };
 
 // The same for fp32 products and k-tiles of 32, each segment padded to whole
 // k-tiles.  (A 64x64 k-tile takes 0.72 us alone on its CU, 0.57 beside
 // another, of which the matrix core needs 0.43; a 128x128 one 2.0 of 1.7.)
-inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_floats, int cus) {
+// wide: tiles of 128x256 too (3.8 of 3.4 us a k-tile), and costs fitted to the
+// linear operator's products, of few k-tiles as well (4096 x 4096 over 64 .. 4096).
+inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_floats, int cus, bool wide = false) {
   struct Kind {
-    int b;
+    int b, bn;
     GemmCost c;
   };
-  static const Kind kinds[3] = {{128, {7.0, 0.0, 2.0, 2.4, SHARE_NONE, 0.0}},
-                                {64, {4.7, 0.0, 0.72, 0.57, SHARE_EVEN, 0.0}},
-                                {32, {3.3, 2.4, 0.19, 0.19, SHARE_NONE, 0.0}}};
+  static const Kind kinds[3] = {{128, 128, {7.0, 0.0, 2.0, 2.4, SHARE_NONE, 0.0}},
+                                {64, 64, {4.7, 0.0, 0.72, 0.57, SHARE_EVEN, 0.0}},
+                                {32, 32, {3.3, 2.4, 0.19, 0.19, SHARE_NONE, 0.0}}};
+  static const Kind wides[4] = {{128, 256, {14.0, 14.0, 3.8, 3.8, SHARE_NONE, 0.0}},
+                                {128, 128, {8.4, 8.4, 2.03, 2.03, SHARE_NONE, 0.0}},
+                                {64, 64, {4.7, 2.6, 0.72, 0.545, SHARE_NONE, 0.0}},
+                                {32, 32, {3.3, 2.4, 0.19, 0.19, SHARE_NONE, 0.0}}};
   const long nk = std::max(1L, nseg * ((seg + 31) / 32));
   F32Plan best{};
   double best_us = 1e30;
-  for (const Kind& q : kinds) {
-    const long tiles = ((M + q.b - 1) / q.b) * ((N + q.b - 1) / q.b);
+  for (int i = 0; i < (wide ? 4 : 3); ++i) {
+    const Kind& q = wide ? wides[i] : kinds[i];
+    const long tiles = ((M + q.b - 1) / q.b) * ((N + q.bn - 1) / q.bn);
     for (int want = 1; want <= (q.b == 32 ? 1 : 64); ++want) {
       const long per = (nk + want - 1) / want;
       if ((nk + per - 1) / per != want) continue;
@@ -179,7 +187,7 @@ inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_f
       if (want > 1) us += split_f32_us(want, M, N);
       if (us < best_us) {
         best_us = us;
-        best = F32Plan{q.b, tiles, want, (int)(per * 32), want > 1 ? want * M * N : 0L};
+        best = F32Plan{q.b, tiles, want, (int)(per * 32), want > 1 ? want * M * N : 0L, q.bn};
       }
     }
   }

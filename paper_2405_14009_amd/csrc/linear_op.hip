@@ -36,7 +36,7 @@ void* at(RowsView& v, long row, int elt) { return v.data ? (char*)v.data + row *
 hipError_t gemm(int elt, const GemmParams& p, hipStream_t s) { return elt == 2 ? gemm_bf16(p, s) : gemm_f32(p, s); }
 
 GemmWork work_of(int elt, long m, long n, long k, bool tn) {
-  return elt == 2 ? gemm_bf16_work(m, n, 1, k, tn) : gemm_f32_work(m, n, 1, k);
+  return elt == 2 ? gemm_bf16_work(m, n, 1, k, tn) : gemm_f32_work(m, n, 1, k, true);
 }
 
 // Whether a product of n columns over k is the reading of its weight (plan_stream).
@@ -68,6 +68,7 @@ GemmParams params(long m, int n, long k, int epi) {
   p.K = (int)k;
   p.batch = p.heads = 1;
   p.epi = epi;
+  p.wide = 1;
   return p;
 }
 

@@ -42,7 +42,8 @@ NormPlan plan_of(long rows, int cols, bool sums) {
 }  // namespace
 
 size_t norm_work_bytes(long rows, int cols) {
-  return sizeof(float) * (size_t)plan_of(rows, cols, true).groups * ROWS_MAX_VECTORS * rows_pad(cols);
+  const long groups = plan_of(rows, cols, true).groups;
+  return groups > 1 ? sizeof(float) * (size_t)groups * ROWS_MAX_VECTORS * rows_pad(cols) : 0;
 }
 
 hipError_t norm_forward(const NormArgs& a, int elt, hipStream_t s) {

@@ -243,7 +243,7 @@ def dropout_backward(dy, drop: Dropout, *, derivative=None, bias_grad=False, acc
     dbias = _gradient(bias_grad, "bias_grad", (cols,), dy)
     m = None if derivative is None else _matrix(derivative, "derivative", shape, dtype, device)
     dx, dxm = _output(out, "out", dy, shape, dtype, device)
-    work = None if dbias is None else _work(work_bytes, dy)
+    work = _work(work_bytes, dy) if dbias is not None and work_bytes else None
     _call(L.load().rc_dropout_backward, device, c, d, _ref(_Matrix(dy.data_ptr(), step)), m, dxm, _address(dbias), more,
           _address(work))
     return dx, dbias
@@ -321,7 +321,7 @@ def layer_norm_backward(dy, total, stats, weight=None, *, dtotal=None, drop: Opt
             dx, dxm = _output(None, "dx", dy, shape, dtype, device)
     elif not sums:
         raise ValueError("no gradient is asked for")
-    work = _work(work_bytes, dy) if sums else None
+    work = _work(work_bytes, dy) if sums and work_bytes else None
     _call(L.load().rc_layer_norm_backward, device, c, d, _ref(_Matrix(dy.data_ptr(), step)), din, t, stats.data_ptr(), w,
           dtm, dxm, _address(dw), _address(db), _address(dib), more, _address(work))
     return NormGradients(dx, dt, dw, db, dib)

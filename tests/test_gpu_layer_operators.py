@@ -325,7 +325,8 @@ def test_linear(rows, i, o, kind):
 
 
 @KINDS
-@pytest.mark.parametrize("rows,i,o", [(1, 64, 72), (40, 72, 64), (700, 512, 1536), (2100, 264, 1032), (4100, 1032, 264)])
+@pytest.mark.parametrize("rows,i,o", [(1, 64, 72), (40, 72, 64), (700, 512, 1536), (2100, 264, 1032), (4100, 1032, 264),
+                                      (2100, 1032, 2056), (300, 2056, 2312)])
 def test_linear_larger_tiles(rows, i, o, kind):
     check_linear(rows, i, o, kind, "relu", params=BF16)
     check_linear(rows, i, o, kind, None, by_out=True)

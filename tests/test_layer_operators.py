@@ -120,7 +120,9 @@ def test_rows_memory(r, c):
     pad = 4 * (-(-c // 8) * 8)
     for call, vectors in ((lib.rc_dropout_memory, 1), (lib.rc_layer_norm_memory, 3)):
         assert call(REF(rows(rows=r, cols=c)), REF(n)) == 0
-        assert n.value % (vectors * pad) == 0 and vectors * pad <= n.value <= vectors * pad * 2048
+        assert n.value % (vectors * pad) == 0 and n.value <= vectors * pad * 2048
+        # several workgroups leave partial sums, one (few rows) none
+        assert (n.value > vectors * pad) == (r > 512) or r == 1000
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
@@ -130,8 +132,8 @@ def test_linear_memory(r, i, o, dtype):
     for by_out in (0, 1):
         n = [ctypes.c_size_t() for _ in range(3)]
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o, by_out=by_out)), *map(REF, n)) == 0
-        # a row of the bias gradient's sums at least, but for few tokens, which take none
-        assert n[2].value >= 4 * o or 0 < r <= 32
+        # a row of the bias gradient's sums at least, where they take more than one workgroup
+        assert n[2].value >= 4 * o or (0 < r <= 8 if dtype else r <= 512)
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o)), None, None, None) == 0
 
 
@@ -211,7 +213,7 @@ def test_bad_dropout(kw, word):
 
 def test_dropout_refusals():
     L, lib = lib_or_skip()
-    r, d = REF(rows()), REF(drop())
+    r, d, many = REF(rows()), REF(drop()), REF(rows(rows=600))
     fwd = lambda x=at(0), b=None, res=None, y=at(1): lib.rc_dropout_forward(r, d, x, b, res, y, None)  # noqa: E731
     refused(lib.rc_dropout_forward(None, d, at(0), None, None, at(1), None), "INVALID_ARG", b"null sizes")
     refused(lib.rc_dropout_forward(r, None, at(0), None, None, at(1), None), "INVALID_ARG", b"null dropout")
@@ -234,10 +236,12 @@ def test_dropout_refusals():
         r, d, at(0), s, dx, db, acc, w, None)
     refused(bwd(dx=None), "INVALID_ARG", b"null dx")
     refused(bwd(acc=2), "INVALID_ARG", b"accumulate")
-    refused(bwd(db=place(3), w=None), "INVALID_ARG", b"work")
-    refused(bwd(db=place(3), w=place(5) + 16), "INVALID_ARG", b"work")
+    large = lambda w: lib.rc_dropout_backward(many, d, at(0), None, at(2), place(4), 0, w, None)  # noqa: E731
+    refused(large(None), "INVALID_ARG", b"work")
+    refused(large(place(8) + 16), "INVALID_ARG", b"work")
+    refused(large(place(4)), "INVALID_ARG", b"overlaps")
     refused(bwd(db=place(3) + 2), "INVALID_ARG", b"dbias")
-    refused(bwd(db=place(3), w=place(3)), "INVALID_ARG", b"overlaps")
+    refused(bwd(db=place(1)), "INVALID_ARG", b"overlaps")
     refused(bwd(s=at(1)), "INVALID_ARG", b"dx overlaps derivative")
 
 
@@ -272,7 +276,8 @@ def test_layer_norm_refusals():
     refused(bwd(dt=at(2)), "INVALID_ARG", b"dtotal overlaps total")
     refused(bwd(din=at(4)), "INVALID_ARG", b"overlaps dtotal_in")
     refused(bwd(dw=place(5), db=place(5) + 16), "INVALID_ARG", b"overlaps")
-    refused(bwd(dw=place(5), work=None), "INVALID_ARG", b"work")
+    many = REF(rows(rows=600))
+    refused(bwd(r=many, total=at(2), dt=at(6), stats=place(8), dw=place(20), work=None), "INVALID_ARG", b"work")
     refused(bwd(acc=3), "INVALID_ARG", b"accumulate")
 
 
