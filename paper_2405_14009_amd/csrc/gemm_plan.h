@@ -184,7 +184,7 @@ inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_f
       if ((nk + per - 1) / per != want) continue;
       if (want > 1 && (per < 2 || want * M * N > room_floats)) break;
       double us = q.c.us(tiles * z * want, q.b == 32 ? (per + 3) / 4 * 4 : per, cus);
-      if (want > 1) us += split_f32_us(want, M, N);
+      if (want > 1) us += split_f32_us(want, M, N) + (wide ? 2.0 : 0.0);   // (the host's share of a launch of its own)
       if (us < best_us) {
         best_us = us;
         best = F32Plan{q.b, tiles, want, (int)(per * 32), want > 1 ? want * M * N : 0L, q.bn};

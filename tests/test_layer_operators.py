@@ -163,6 +163,16 @@ int main() {
         return 1;
       }
     }
+  for (long M : dims) for (long N : dims) for (long K : depths) for (long room : {0L, 1L << 20, 16L << 20})
+    for (int cus : {64, 256, 304}) {
+      const F32Plan p = plan_f32(M, N, 1, K, 1, room, cus, true);
+      if (p.tiles != (M + p.bm - 1) / p.bm * ((N + p.bn - 1) / p.bn) || p.split_k % 32 || p.splits * (long)p.split_k < K ||
+          (p.splits - 1) * (long)p.split_k >= K || p.split_floats > room || (p.splits > 1) != (p.split_floats > 0) ||
+          (p.bn != p.bm && (p.bm != 128 || p.bn != 256))) {
+        std::printf("fp32 M %ld N %ld K %ld room %ld cus %d\n", M, N, K, room, cus);
+        return 1;
+      }
+    }
   return 0;
 }
 """
