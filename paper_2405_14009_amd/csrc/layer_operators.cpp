@@ -156,6 +156,8 @@ struct LinearTensors : Tensors {
   LinearTensors(const rc_linear* l, int elt) : l(l), elt(elt) {}
   rc_status at(const rc_matrix* m, const char* name, int64_t cols, bool needed, bool output, RowsView& to) {
     TRY(matrix(m, name, elt, l->rows, cols, needed, output, 16, to));
+    // (the kernels bound their reads by rows of at least a row's length)
+    if (to.data && to.stride < cols) return fail(RC_ERR_INVALID_ARG, std::string(name) + ": rows overlap");
     if (elt == 2 && to.stride >= 1L << 21)
       return fail(RC_ERR_UNSUPPORTED, std::string(name) + ": a row_stride of 2^21 elements or more");
     return RC_OK;

@@ -217,6 +217,22 @@ def test_norm_of_a_large_row_sum_in_bf16():
 
 
 @KINDS
+def test_rows_that_share_their_memory(kind):
+    """Inputs broadcast over rows, as an expanded tensor has them."""
+    x, r = normal(1, 1, 77, kind=kind), normal(2, 9, 77, kind=kind)
+    wide = x.expand(9, 77)
+    drop = ops().Dropout(0.3, SEED, OFFSET)
+    for a, b in ((wide, wide.contiguous()),):
+        one = ops().layer_norm_forward(a, drop=drop, residual=r)
+        two = ops().layer_norm_forward(b, drop=drop, residual=r)
+        assert all(torch.equal(p, q) for p, q in zip(one, two))
+        g = ops().layer_norm_backward(a, one[1], one[2], drop=drop)
+        h = ops().layer_norm_backward(b, one[1], one[2], drop=drop)
+        assert all(torch.equal(p, q) for p, q in zip(g[:4], h[:4]))
+    assert torch.equal(ops().dropout_forward(r, drop, residual=wide), ops().dropout_forward(r, drop, residual=wide.contiguous()))
+
+
+@KINDS
 def test_nan_stays_in_its_row(kind):
     x = normal(1, 6, 100, kind=kind)
     x[2, 50] = float("nan")
@@ -244,8 +260,9 @@ def test_accumulated_gradients():
     assert torch.equal(base, db + 4.0)
 
 
-def test_no_rows():
-    x = torch.empty(0, 40, dtype=BF16, device="cuda")
+@KINDS
+def test_no_rows(kind):
+    x = torch.empty(0, 40, dtype=kind, device="cuda")
     drop = ops().Dropout(0.1, 1)
     assert ops().dropout_forward(x, drop).shape == (0, 40)
     dx, db = ops().dropout_backward(x, drop, bias_grad=True)
@@ -254,10 +271,16 @@ def test_no_rows():
     g = ops().layer_norm_backward(x, total, stats, bias_grad=torch.ones(40, device="cuda"),
                                   weight_grad=torch.ones(40, device="cuda"), accumulate=True)
     assert y.shape == (0, 40) and (g.dweight == 1).all() and (g.dbias == 1).all()
-    w = normal(1, 40, 16)
+    w = normal(1, 40, 16, kind=kind)
     assert ops().linear_forward(x, w)[0].shape == (0, 16)
-    dw, db = ops().linear_backward_weight(x, torch.empty(0, 16, dtype=BF16, device="cuda"))
-    assert dw.shape == (40, 16) and not dw.any() and not db.any()
+    dy = torch.empty(0, 16, dtype=kind, device="cuda")
+    assert ops().linear_backward_input(dy, w).shape == (0, 40)
+    for by_out in (False, True):
+        dw, db = ops().linear_backward_weight(x, dy, by_out=by_out)
+        assert dw.shape == (40, 16) and not dw.any() and not db.any()
+        base, bias = torch.ones_like(dw), torch.ones_like(db)
+        ops().linear_backward_weight(x, dy, by_out=by_out, weight_grad=base, bias_grad=bias, accumulate=True)
+        assert (base == 1).all() and (bias == 1).all()
 
 
 # -- linear ------------------------------------------------------------------------
@@ -618,7 +641,7 @@ def test_refusals_of_device_tensors():
         lambda: o.linear_forward(x, w, activation="tanh"), lambda: o.linear_forward(x, w.float()),
         lambda: o.linear_forward(x, w[:60]), lambda: o.linear_forward(x, w[::2, ::2]),
         lambda: o.linear_forward(x[:, :60], w[:60]), lambda: o.linear_forward(x, w, out=x),
-        lambda: o.linear_forward(x, w, residual=x), lambda: o.linear_backward_input(x, w),
+        lambda: o.linear_forward(x[:1].expand(6, 64), w), lambda: o.linear_forward(x, w, residual=x), lambda: o.linear_backward_input(x, w),
         lambda: o.linear_backward_weight(x, x[:3]), lambda: o.linear_backward_weight(x, x, weight_grad=False),
         lambda: o.linear_backward_weight(x, x, accumulate=True),
         lambda: o.linear_backward_weight(x, x, weight_grad=torch.zeros(64, 32, device="cuda")),

@@ -327,6 +327,8 @@ def test_linear_refusals():
     refused(fwd(y=at(2, stride=56)), "INVALID_ARG", b"rows of the output overlap")
     refused(fwd(x=at(0, stride=1 << 21)), "UNSUPPORTED", b"row_stride")
     refused(fwd(w=at(1, stride=56)), "INVALID_ARG", b"weight: rows overlap")
+    refused(fwd(x=at(0, stride=0)), "INVALID_ARG", b"x: rows overlap")
+    refused(fwd(res=at(3, stride=56)), "INVALID_ARG", b"residual: rows overlap")
     refused(fwd(w=at(1, stride=1 << 24)), "UNSUPPORTED", b"weight: spans")
     refused(fwd(s=at(3)), "INVALID_ARG", b"without an activation")
     refused(fwd(y=at(0)), "INVALID_ARG", b"y overlaps x")
