@@ -126,38 +126,29 @@ struct Copier {
 
 // Column sums over k of the staged m/n-contiguous B tiles ([BK][BN] bf16,
 // 16-byte chunks swizzled by k-row), or A tiles, accumulated over the k-tiles a
-// workgroup takes part for: of `ROWS` columns, thread t (of NTH) owns chunk column
-// t % (ROWS / 8) and k-rows t / (ROWS / 8) + R i of every tile (R row groups), 8
-// fp32 partial sums.  finish() adds the R partials of each column in a fixed order
-// through LDS and stores the workgroup's row of partial sums, so the result is
-// reproducible.  Which operand and whether any is uniform to the launch.
-template <int BM, int BN, int BK, int A_BYTES, int NTH = 512>
+// workgroup takes part for: thread t (of NTH) owns chunk column t % (BN / 8)
+// and k-rows t / (BN / 8) + R i of every tile (R row groups), 8 fp32 partial
+// sums.  finish() adds the R partials of each column in a fixed order through
+// LDS and stores the workgroup's row of partial sums, so the result is
+// reproducible.
+template <int BN, int BK, int NTH = 512>
 struct ColSums {
-  static constexpr int RED_BYTES = NTH * 8 * 4;
+  static constexpr int CC = BN / 8, R = NTH / CC, RPT = BK / R;
+  static_assert(BK % R == 0, "row groups");
+  static constexpr int RED_BYTES = R * BN * 4;
   float s[8];
-  bool on, of_a;
-  int next, every, row, c0, n;   // k-tile to sum, step to the one after, row and first column of the partial sums
-  __device__ __forceinline__ void init(const GemmParams& p, bool first, int tm, int tn, int split, int m0, int n0,
-                                       int tid) {
-    on = p.colsum_work != nullptr && first;
-    of_a = p.colsum_a != 0;
-    next = of_a ? tn : tm;
-    every = of_a ? (p.N + BN - 1) / BN : (p.M + BM - 1) / BM;
-    row = split * every + next;
-    c0 = of_a ? m0 : n0;
-    n = of_a ? p.M : p.N;
+  int cc, rg;
+  __device__ __forceinline__ void init(int tid) {
+    cc = tid % CC;
+    rg = tid / CC;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] = 0.f;
   }
-  template <int ROWS>
-  __device__ __forceinline__ void add(const char* tb) {
-    constexpr int CC = ROWS / 8, R = NTH / CC, RPT = BK / R;
-    static_assert(BK % R == 0, "row groups");
-    const int cc = threadIdx.x % CC, rg = threadIdx.x / CC;
+  __device__ __forceinline__ void tile(const char* tb) {
 #pragma unroll
     for (int i = 0; i < RPT; ++i) {
       const int k = rg + R * i;
-      const uint4 v = *(const uint4*)(tb + k * (ROWS * 2) + ((cc ^ swz_mn<ROWS>(k)) << 4));
+      const uint4 v = *(const uint4*)(tb + k * (BN * 2) + ((cc ^ swz_mn<BN>(k)) << 4));
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -166,41 +157,19 @@ struct ColSums {
       }
     }
   }
-  // st: the stage of k-tile t
-  __device__ __forceinline__ void tile(const char* st, int t) {
-    if (!on || t != next) return;
-    if constexpr (BM == BN) {
-      add<BN>(st + (of_a ? 0 : A_BYTES));
-    } else {
-      if (of_a) add<BM>(st);
-      else add<BN>(st + A_BYTES);
-    }
-    next += every;
-  }
-  template <int ROWS>
-  __device__ __forceinline__ void store(float* red, const GemmParams& p, int tid) {
-    constexpr int CC = ROWS / 8, R = NTH / CC;
+  // red: RED_BYTES of LDS that no wave touches meanwhile; every wave calls it.
+  __device__ __forceinline__ void finish(float* red, const GemmParams& p, int row, int n0, int N, int tid) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) red[(tid / CC) * ROWS + 8 * (tid % CC) + e] = s[e];
+    for (int e = 0; e < 8; ++e) red[rg * BN + 8 * cc + e] = s[e];
     __syncthreads();
-    if (tid < ROWS) {
+    if (tid < BN) {
       float t = 0.f;
 #pragma unroll 8
-      for (int r = 0; r < R; ++r) t += red[r * ROWS + tid];
-      const int c = c0 + tid;
-      if (c < n) p.colsum_work[(long)row * n + c] = t;
+      for (int r = 0; r < R; ++r) t += red[r * BN + tid];
+      const int n = n0 + tid;
+      if (n < N) p.colsum_work[(long)row * N + n] = t;
     }
     __syncthreads();
-  }
-  // red: RED_BYTES of LDS that no wave touches meanwhile; every wave calls it.
-  __device__ __forceinline__ void finish(float* red, const GemmParams& p, int tid) {
-    if (!on) return;
-    if constexpr (BM == BN) {
-      store<BN>(red, p, tid);
-    } else {
-      if (of_a) store<BM>(red, p, tid);
-      else store<BN>(red, p, tid);
-    }
   }
 };
 
@@ -464,7 +433,9 @@ struct KWalk {
   }
 };
 
-template <int BM, int BN, int NW, int KS, int BK, int NST, bool AK, bool BKC, int EPI>
+// CSA: column sums are those of A, not of B (a kernel of its own: which operand,
+// decided at run time, cost the stage's weight passes 2 %).
+template <int BM, int BN, int NW, int KS, int BK, int NST, bool AK, bool BKC, int EPI, bool CSA = false>
 __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
   // the configuration the launcher uses (256 x 128 tiles run the ping-pong
   // kernel, which owns the k-split)
@@ -534,12 +505,15 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // column sums (a workgroup-uniform condition)
+  // column sums of B (a workgroup-uniform condition)
   constexpr bool CS = !AK && !BKC;  // weight-gradient layout only
   // Every tile-row takes part in the column sums for one k-tile in tiles_m, so
   // the extra work spreads evenly over the launch.
-  ColSums<BM, BN, BK, A_BYTES> cs;
-  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
+  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
+  const int cs_tile = CSA ? tn : tm, cs_tiles = CSA ? tiles_n : tiles_m;
+  int cs_next = cs_tile;  // next k-tile this workgroup sums
+  ColSums<(CSA ? BM : BN), BK> cs;
+  if (cs_on) cs.init(threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -582,7 +556,10 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
     if constexpr (CS) {
       // while the tile's MFMAs drain; the stage stays valid until the next barrier
       __builtin_amdgcn_sched_barrier(0);
-      cs.tile(st, t);
+      if (cs_on && t == cs_next) {
+        cs.tile(st + (CSA ? 0 : A_BYTES));
+        cs_next += cs_tiles;
+      }
     }
     sc = sc + 1 == NST ? 0 : sc + 1;
     si = si + 1 == NST ? 0 : si + 1;
@@ -592,9 +569,9 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
   // LDS is free once every wave is past its last k-tile.
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
-  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<(CSA ? BM : BN), BK>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    cs.finish((float*)lds, p, threadIdx.x);
+    if (cs_on) cs.finish((float*)lds, p, split * cs_tiles + cs_tile, CSA ? m0 : n0, CSA ? p.M : p.N, threadIdx.x);
   }
   float* sm = (float*)(lds + wave * EPI_BYTES);
   epilogue<EPI, TN, 0, TM, true, TM>(p, acc, sm, m0 + wm * (BM / 2), n0 + wn * (BN / WN_), lane, c_off);
@@ -611,7 +588,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_bf16_kernel(GemmParams p) {
 // so that copy is in flight while the epilogue computes and stores.  DEFER:
 // each k-tile's last MFMAs are deferred as mma_tile describes.
 // Requirements (checked by the launcher): batch * heads == 1, ntiles % 8 == 0.
-template <int EPI, bool AK, bool BKC, bool DEFER>
+template <int EPI, bool AK, bool BKC, bool DEFER, bool CSA = false>
 __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
   constexpr int BM = 256, BN = 256, NW = 8, BK = 64, NST = 2;
   constexpr int WN_ = 4, TN = 2, NKS = 4;
@@ -621,7 +598,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
   constexpr int EPI_BYTES = 32 * (32 * TN + 8) * 4;
   constexpr int LDS_BYTES = NST * STAGE > STAGE + NW * EPI_BYTES ? NST * STAGE : STAGE + NW * EPI_BYTES;
   static_assert(LDS_BYTES <= 160 * 1024, "LDS");
-  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= NW * EPI_BYTES, "column-sum reduction fits above stage 0");
+  static_assert(ColSums<(CSA ? BM : BN), BK>::RED_BYTES <= NW * EPI_BYTES, "column-sum reduction fits above stage 0");
   __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
 
   const int lane = threadIdx.x & 63;
@@ -657,6 +634,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     wk.next(p, 0, 0);
   };
   constexpr bool CS = !AK && !BKC;
+  const bool cs_on = CS && p.colsum_work != nullptr;
 
   int i = blockIdx.x >> 3;
   if (i >= nx) return;
@@ -673,8 +651,10 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[a][j][r] = 0.f;
   while (true) {
-    ColSums<BM, BN, BK, A_BYTES> cs;
-    if constexpr (CS) cs.init(p, true, tm, n0 / BN, 0, m0, n0, threadIdx.x);
+    const int cs_tile = CSA ? n0 / BN : tm, cs_tiles = CSA ? tiles_n : tiles_m;
+    int cs_next = cs_tile;
+    ColSums<(CSA ? BM : BN), BK> cs;
+    if (cs_on) cs.init(threadIdx.x);
     int sc = 0, si = 1;
     bf16x8 pa[4], pb[TN];  // the deferred last k-step of each k-tile (mma_tile)
     mma_pending_clear<4, TN>(pa, pb);
@@ -694,7 +674,10 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
       if (refill) wk.next(p, 0, 0);
       if constexpr (CS) {
         __builtin_amdgcn_sched_barrier(0);
-        cs.tile(st, t);
+        if (cs_on && t == cs_next) {
+          cs.tile(st + (CSA ? 0 : A_BYTES));
+          cs_next += cs_tiles;
+        }
       }
       sc ^= 1;
       si ^= 1;
@@ -702,7 +685,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     if constexpr (DEFER) mma_flush<4, TN>(acc, pa, pb);
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();  // every wave is past the last k-tile: both stages are free
-    const int cm0 = m0, cn0 = n0;
+    const int cm0 = m0, cn0 = n0, crow = cs_tile;
     const int inext = i + nq;
     if (inext < nx) {
       tile_of(inext, m0, n0, tm);
@@ -712,7 +695,7 @@ __global__ __launch_bounds__(512) void gemm_bf16_persist_kernel(GemmParams p) {
     }
     char* above = lds + STAGE;
     if constexpr (CS) {
-      cs.finish((float*)above, p, threadIdx.x);
+      if (cs_on) cs.finish((float*)above, p, crow, CSA ? cm0 : cn0, CSA ? p.M : p.N, threadIdx.x);
     }
     // (the gradient-accumulating epilogue with its inputs fetched a block-row
     // ahead does not fit the registers next to the next tile's copy state)
@@ -798,7 +781,7 @@ __device__ __forceinline__ void phase_barrier() {
 // issued yet).  The stage being refilled held tile t - 1, whose last fragment
 // reads (group 1's last memory phase of tile t - 1) completed before the
 // barrier that opens group 0's first phase of tile t.
-template <int BN, int KS, int NST, int GM, bool AK, bool BKC, int EPI>
+template <int BN, int KS, int NST, int GM, bool AK, bool BKC, int EPI, bool CSA = false>
 __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
   constexpr int BM = 256, NW = 8, BK = 64;
   // the configuration the launcher uses: 256 x 128 tiles, two k-groups (the
@@ -872,12 +855,15 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // column sums (a workgroup-uniform condition)
+  // column sums of B (a workgroup-uniform condition)
   constexpr bool CS = !AK && !BKC;  // weight-gradient layout only
   // Every tile-row takes part in the column sums for one k-tile in tiles_m, so
   // the extra work spreads evenly over the launch.
-  ColSums<BM, BN, BK, A_BYTES> cs;
-  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
+  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
+  const int cs_tile = CSA ? tn : tm, cs_tiles = CSA ? tiles_n : tiles_m;
+  int cs_next = cs_tile;  // next k-tile this workgroup sums
+  ColSums<(CSA ? BM : BN), BK> cs;
+  if (cs_on) cs.init(threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -924,7 +910,10 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
       load_unit<BM, BN, AK, BKC, TN, NKS, BK>(af, bfr, st, st + A_BYTES, fa, fb, u);
       if (refill) ca.issue(wk.a, dst, wave, p.lda, p.M, wk.k, wk.kend);
       if constexpr (CS) {
-        if (u == 0) cs.tile(st, t);
+        if (u == 0 && cs_on && t == cs_next) {
+          cs.tile(st + (CSA ? 0 : A_BYTES));
+          cs_next += cs_tiles;
+        }
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the unit's fragments are in registers
       if (grp == 1 && u == U - 1) wait_next(t, SPLIT && U == 1);
@@ -944,9 +933,9 @@ __global__ __launch_bounds__(512) void gemm_bf16_pp_kernel(GemmParams p) {
 
   // LDS is free once every wave is past its last k-tile.
   __syncthreads();
-  static_assert(ColSums<BM, BN, BK, A_BYTES>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<(CSA ? BM : BN), BK>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    cs.finish((float*)lds, p, threadIdx.x);
+    if (cs_on) cs.finish((float*)lds, p, split * cs_tiles + cs_tile, CSA ? m0 : n0, CSA ? p.M : p.N, threadIdx.x);
   }
   // The partner's slot is read only by this wave, so after the reduction it
   // serves as this wave's epilogue tile.  (The gradient-accumulating

@@ -5,6 +5,7 @@
 hipError_t gemm_bf16_nt(const GemmParams& p, hipStream_t s);
 hipError_t gemm_bf16_tn(const GemmParams& p, hipStream_t s);
 hipError_t gemm_bf16_linear_nn(const GemmParams& p, hipStream_t s);
+hipError_t gemm_bf16_linear_tn(const GemmParams& p, hipStream_t s);
 
 static hipError_t gemm_bf16_nn(const GemmParams& p, hipStream_t s) {
   switch (p.epi) {
@@ -27,7 +28,7 @@ hipError_t gemm_bf16(const GemmParams& p, hipStream_t s) {
   if (p.colsum_work != nullptr && (p.a_kcontig || p.b_kcontig || p.colsum_rows == nullptr || p.batch * p.heads != 1))
     return hipErrorInvalidValue;
   if (p.a_kcontig && p.b_kcontig) return gemm_bf16_nt(p, s);
-  if (!p.a_kcontig && !p.b_kcontig) return gemm_bf16_tn(p, s);
+  if (!p.a_kcontig && !p.b_kcontig) return p.colsum_a ? gemm_bf16_linear_tn(p, s) : gemm_bf16_tn(p, s);
   return hipErrorInvalidValue;
 }
 

@@ -16,7 +16,7 @@ namespace {
 // before the multiply ran one k-tile behind the reads), so the ring is as deep
 // as two workgroups per CU allow and the launcher splits the reduction until
 // the CUs are filled.
-template <int BM, int BN, int NST, bool AK, bool BKC, int EPI>
+template <int BM, int BN, int NST, bool AK, bool BKC, int EPI, bool CSA = false>
 __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
   static_assert((BM == 128 || BM == 64) && (BN == 128 || BN == 64) && NST >= 2, "tile shapes");
   constexpr int NW = 4, BK = 64, NKS = BK / 16;
@@ -68,11 +68,14 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
     for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  // Column sums (bias gradients): tile-row tm takes the k-tiles t of its split
-  // with t mod tiles_m == tm, into row split * tiles_m + tm.
+  // Column sums of B (bias gradients): tile-row tm takes the k-tiles t of its
+  // split with t mod tiles_m == tm, into row split * tiles_m + tm.
   constexpr bool CS = !AK && !BKC;
-  ColSums<BM, BN, BK, A_BYTES, 256> cs;
-  if constexpr (CS) cs.init(p, z == 0, tm, tn, split, m0, n0, threadIdx.x);
+  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
+  const int cs_tile = CSA ? tn : tm, cs_tiles = CSA ? (p.N + BN - 1) / BN : tiles_m;
+  int cs_next = cs_tile;
+  ColSums<(CSA ? BM : BN), BK, 256> cs;
+  if (cs_on) cs.init(threadIdx.x);
 
   KWalk<AK, BKC, BK> wk;  // the next k-tile to copy
   wk.init(p, a_off, b_off, kb, ke);
@@ -127,7 +130,10 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
     }
     if constexpr (CS) {
       __builtin_amdgcn_sched_barrier(0);
-      cs.tile(st, t);
+      if (cs_on && t == cs_next) {
+        cs.tile(st + (CSA ? 0 : A_BYTES));
+        cs_next += cs_tiles;
+      }
     }
     sc = sc + 1 == NST ? 0 : sc + 1;
     si = si + 1 == NST ? 0 : si + 1;
@@ -149,15 +155,15 @@ __global__ __launch_bounds__(256) void gemm_bf16_tile_kernel(GemmParams p) {
   }
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();
-  static_assert(ColSums<BM, BN, BK, A_BYTES, 256>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
+  static_assert(ColSums<(CSA ? BM : BN), BK, 256>::RED_BYTES <= LDS_BYTES, "column-sum reduction fits LDS");
   if constexpr (CS) {
-    cs.finish((float*)lds, p, threadIdx.x);
+    if (cs_on) cs.finish((float*)lds, p, split * cs_tiles + cs_tile, CSA ? m0 : n0, CSA ? p.M : p.N, threadIdx.x);
   }
   epilogue<EPI, TN, 0, TM, true, TM>(p, acc, (float*)(lds + wave * EPI_BYTES), m0 + wm * (BM / 2),
                                      n0 + wn * (BN / 2), lane, c_off);
 }
 
-template <bool AK, bool BKC, int EPI>
+template <bool AK, bool BKC, int EPI, bool CSA>
 hipError_t launch_bf16_persist(const GemmParams& p, hipStream_t s) {
   const int ntiles = ((p.M + 255) / 256) * ((p.N + 255) / 256);
   const int per_xcd = std::max(1, device_compute_units() / 8);
@@ -166,14 +172,14 @@ hipError_t launch_bf16_persist(const GemmParams& p, hipStream_t s) {
   // batched weight gradients (-2 % batched, -7 % for one-round launches), not
   // on single micro-batch ones (+2.4 % at K = 2048).
   if (p.K >= 8192)
-    hipLaunchKernelGGL((gemm_bf16_persist_kernel<EPI, AK, BKC, true>), dim3(8 * nq), dim3(512), 0, s, p);
+    hipLaunchKernelGGL((gemm_bf16_persist_kernel<EPI, AK, BKC, true, CSA>), dim3(8 * nq), dim3(512), 0, s, p);
   else
-    hipLaunchKernelGGL((gemm_bf16_persist_kernel<EPI, AK, BKC, false>), dim3(8 * nq), dim3(512), 0, s, p);
+    hipLaunchKernelGGL((gemm_bf16_persist_kernel<EPI, AK, BKC, false, CSA>), dim3(8 * nq), dim3(512), 0, s, p);
   return hipGetLastError();
 }
 
 // One launch of plan pl over the whole output: grid (tiles, batch or splits).
-template <bool AK, bool BKC, int EPI>
+template <bool AK, bool BKC, int EPI, bool CSA = false>
 hipError_t launch_tiles(const GemmParams& p, const GemmPlan& pl, hipStream_t s) {
   const unsigned y = p.splits > 1 ? (unsigned)p.splits : (unsigned)(p.batch * p.heads);
   const dim3 grid((unsigned)pl.tiles, y);
@@ -187,9 +193,9 @@ hipError_t launch_tiles(const GemmParams& p, const GemmPlan& pl, hipStream_t s) 
       if constexpr (!AK && !BKC && EPI != EPI_F32_STORE) {
         if (y == 1 && p.krange == KR_FULL && !p.causal_skip && pl.tiles % 8 == 0 &&
             pl.tiles > device_compute_units())
-          return launch_bf16_persist<AK, BKC, EPI>(p, s);
+          return launch_bf16_persist<AK, BKC, EPI, CSA>(p, s);
       }
-      hipLaunchKernelGGL((gemm_bf16_kernel<256, 256, 8, 1, 64, 2, AK, BKC, EPI>), grid, dim3(512), 0, s, p);
+      hipLaunchKernelGGL((gemm_bf16_kernel<256, 256, 8, 1, 64, 2, AK, BKC, EPI, CSA>), grid, dim3(512), 0, s, p);
       break;
     case TILE_192x256:
       if constexpr (AK) {
@@ -198,21 +204,21 @@ hipError_t launch_tiles(const GemmParams& p, const GemmPlan& pl, hipStream_t s) 
       }
       return hipErrorInvalidValue;
     case TILE_256x128:
-      hipLaunchKernelGGL((gemm_bf16_pp_kernel<128, 2, 3, 4, AK, BKC, EPI>), grid, dim3(512), 0, s, p);
+      hipLaunchKernelGGL((gemm_bf16_pp_kernel<128, 2, 3, 4, AK, BKC, EPI, CSA>), grid, dim3(512), 0, s, p);
       break;
     case TILE_128:
-      hipLaunchKernelGGL((gemm_bf16_tile_kernel<128, 128, 2, AK, BKC, EPI>), grid, dim3(256), 0, s, p);
+      hipLaunchKernelGGL((gemm_bf16_tile_kernel<128, 128, 2, AK, BKC, EPI, CSA>), grid, dim3(256), 0, s, p);
       break;
     case TILE_64:
-      hipLaunchKernelGGL((gemm_bf16_tile_kernel<64, 64, 4, AK, BKC, EPI>), grid, dim3(256), 0, s, p);
+      hipLaunchKernelGGL((gemm_bf16_tile_kernel<64, 64, 4, AK, BKC, EPI, CSA>), grid, dim3(256), 0, s, p);
       break;
     default:
-      hipLaunchKernelGGL((gemm_small_kernel<bf16, AK, BKC, EPI>), grid, dim3(256), 0, s, p);
+      hipLaunchKernelGGL((gemm_small_kernel<bf16, AK, BKC, EPI, false, CSA>), grid, dim3(256), 0, s, p);
   }
   return hipGetLastError();
 }
 
-template <bool AK, bool BKC, int EPI>
+template <bool AK, bool BKC, int EPI, bool CSA = false>
 hipError_t launch_bf16(GemmParams p, hipStream_t s) {
   if (p.kseg_len > 0) {  // every segment starts on a k-tile; its last one is padded with zeros
     const int nseg = p.K / p.kseg_len;
@@ -225,20 +231,20 @@ hipError_t launch_bf16(GemmParams p, hipStream_t s) {
   const long room = whole && p.split_work ? p.split_floats : 0;
   const GemmPlan pl = p.stream ? plan_stream(p.M, p.N, p.K, room, cus)
                                : plan_bf16(p.M, p.N, p.K, !AK && !BKC, z, room,
-                                           p.colsum_work != nullptr ? p.colsum_floats : -1, cus, p.colsum_a);
+                                           p.colsum_work != nullptr ? p.colsum_floats : -1, cus, CSA);
   if (p.colsum_work != nullptr) {
-    const long rows = p.colsum_a ? pl.colsum_a_rows(p.N) : pl.colsum_rows(p.M);
-    if (rows * (p.colsum_a ? p.M : p.N) > p.colsum_floats) return hipErrorInvalidValue;
+    const long rows = CSA ? pl.colsum_a_rows(p.N) : pl.colsum_rows(p.M);
+    if (rows * (CSA ? p.M : p.N) > p.colsum_floats) return hipErrorInvalidValue;
     *p.colsum_rows = (int)rows;
   }
   p.splits = 1;
-  if (pl.splits == 1) return launch_tiles<AK, BKC, EPI>(p, pl, s);
+  if (pl.splits == 1) return launch_tiles<AK, BKC, EPI, CSA>(p, pl, s);
   GemmParams q = p;
   q.splits = pl.splits;
   q.split_k = pl.split_k;
   q.C = p.split_work;
   q.ldc = p.N;
-  const hipError_t e = launch_tiles<AK, BKC, EPI_F32_STORE>(q, pl, s);
+  const hipError_t e = launch_tiles<AK, BKC, EPI_F32_STORE, CSA>(q, pl, s);
   if (e != hipSuccess) return e;
   q.C = p.C;
   q.ldc = p.ldc;

@@ -114,7 +114,7 @@ __device__ __forceinline__ void small_products(f32x16 (&acc)[2], const float4 (&
   }
 }
 
-template <class E, bool AK, bool BKC, int EPI, bool WIDE = false>
+template <class E, bool AK, bool BKC, int EPI, bool WIDE = false, bool CSA = false>
 __global__ __launch_bounds__(256) void gemm_small_kernel(GemmParams p) {
   typedef SmallOperand<E, AK> OpA;
   typedef SmallOperand<E, BKC> OpB;
@@ -186,11 +186,11 @@ __global__ __launch_bounds__(256) void gemm_small_kernel(GemmParams p) {
     if (nseg > 0 && k0 >= per_seg * BK) wrap();
   };
 
-  // Column sums of B, or of A (bias gradients, bf16): tile-row tm takes the k-tiles t
-  // with t mod tiles_m == tm (A: tile-column tn, tiles_n).  Lane: chunk lane % 4, k-rows lane / 4 + 16 i.
+  // Column sums of B, or (CSA) of A (bias gradients, bf16): tile-row tm takes the k-tiles t
+  // with t mod tiles_m == tm (CSA: tile-column tn, tiles_n).  Lane: chunk lane % 4, k-rows lane / 4 + 16 i.
   constexpr bool CS = !AK && !BKC && sizeof(E) == 2;
-  const bool cs_on = CS && p.colsum_work != nullptr && z == 0, cs_a = CS && p.colsum_a;
-  const int cs_row = cs_a ? tn : tm, cs_every = cs_a ? (p.N + 31) / 32 : tiles_m;
+  const bool cs_on = CS && p.colsum_work != nullptr && z == 0;
+  const int cs_tile = CSA ? tn : tm, cs_tiles = CSA ? (p.N + 31) / 32 : tiles_m;
   float cs[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) cs[e] = 0.f;
@@ -213,10 +213,10 @@ __global__ __launch_bounds__(256) void gemm_small_kernel(GemmParams p) {
     small_frags<AK>(st, lane, fa[set]);
     small_frags<BKC>(st + 4096, lane, fb[set]);
     if constexpr (CS) {
-      if (cs_on && (wave + 4 * i) % cs_every == cs_row) {
+      if (cs_on && (wave + 4 * i) % cs_tiles == cs_tile) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const uint4 v = *(const uint4*)(st + (cs_a ? 0 : 4096) + (lane / 4 + 16 * u) * 64 + (lane & 3) * 16);
+          const uint4 v = *(const uint4*)(st + (CSA ? 0 : 4096) + (lane / 4 + 16 * u) * 64 + (lane & 3) * 16);
           const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -275,14 +275,14 @@ __global__ __launch_bounds__(256) void gemm_small_kernel(GemmParams p) {
     epi_finish4<EPI, E>(p, C, m, n, v, in, bias);
   }
   if constexpr (CS) {
-    const int c = (cs_a ? m0 : n0) + (int)threadIdx.x, cs_n = cs_a ? p.M : p.N;
-    if (cs_on && threadIdx.x < 32 && c < cs_n) {
+    const int cs_c = (CSA ? m0 : n0) + (int)threadIdx.x, cs_n = CSA ? p.M : p.N;
+    if (cs_on && threadIdx.x < 32 && cs_c < cs_n) {
       float t = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w)
 #pragma unroll
         for (int g = 0; g < 16; ++g) t += ((const float*)(lds + w * NST * STAGE))[CS_OFF + g * 32 + threadIdx.x];
-      p.colsum_work[(long)cs_row * cs_n + c] = t;
+      p.colsum_work[(long)cs_tile * cs_n + cs_c] = t;
     }
   }
 }
