@@ -431,7 +431,7 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
         raise ValueError("weight_grad must be True or an fp32 tensor")
     more = _accumulates(accumulate, weight_grad, bias_grad)
     shape = (fan_out, fan_in) if by_out else (fan_in, fan_out)
-    if weight_grad is not True and by_out:
+    if by_out and isinstance(weight_grad, torch.Tensor) and weight_grad.dim() == 2:
         weight_grad = weight_grad.t()
     dw = _gradient(weight_grad, "weight_grad", shape, x)
     dbias = _gradient(bias_grad, "bias_grad", (fan_out,), x)

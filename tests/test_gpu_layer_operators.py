@@ -644,6 +644,8 @@ def test_refusals_of_device_tensors():
         lambda: o.linear_forward(x[:1].expand(6, 64), w), lambda: o.linear_forward(x, w, residual=x), lambda: o.linear_backward_input(x, w),
         lambda: o.linear_backward_weight(x, x[:3]), lambda: o.linear_backward_weight(x, x, weight_grad=False),
         lambda: o.linear_backward_weight(x, x, accumulate=True),
+        lambda: o.linear_backward_weight(x, x, by_out=True, weight_grad=3),
+        lambda: o.linear_backward_weight(x, x, by_out=True, weight_grad=v),
         lambda: o.linear_backward_weight(x, x, weight_grad=torch.zeros(64, 32, device="cuda")),
     ]
     for i, call in enumerate(bad):
