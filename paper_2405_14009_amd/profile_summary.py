@@ -72,27 +72,34 @@ def sources_digest(d: str = None) -> str:
 
 def kernel_class(name: str) -> str:
     # the one-tile, ping-pong and small-tile bf16 GEMM kernels end their template
-    # arguments with (A k-contiguous, B k-contiguous, epilogue); the persistent
-    # kernel begins with (epilogue, A k-contiguous, B k-contiguous); the sum of a
-    # split product's partials begins with the epilogue
+    # arguments with (A k-contiguous, B k-contiguous, epilogue) and flags; the
+    # persistent kernel begins with (epilogue, A k-contiguous, B k-contiguous); the
+    # sum of a split product's partials begins with the epilogue.  Small tiles in
+    # bf16 keep their mangled name in a profile.
     m = re.search(r"splitk_finish_k(?:<|ILi)(\d+)", name)
     if m:
-        return {1: "gemm_fwd", 2: "gemm_fwd", 3: "gemm_fwd", 5: "gemm_wgrad"}.get(int(m.group(1)), "gemm_dgrad")
+        return {1: "gemm_fwd", 2: "gemm_fwd", 3: "gemm_fwd", 5: "gemm_wgrad", 7: "gemm_fwd"}.get(int(m.group(1)), "gemm_dgrad")
     if re.search(r"gemm_small_kernel<float", name):
         return "gemm_f32"
-    m = re.search(r"gemm_bf16_persist_kernel<(\d+),\s*(true|false),\s*(true|false)(?:,\s*(?:true|false))?>", name)
+    m = re.search(r"gemm_bf16_persist_kernel<(\d+),\s*(true|false),\s*(true|false)(?:,\s*(?:true|false))*>", name)
     if m:
         epi, ak, bk = int(m.group(1)), m.group(2), m.group(3)
     else:
-        m = re.search(r"gemm_(?:bf16(?:_pp|_tile)?|small)_kernel<[^>]*?(true|false),\s*(true|false),\s*(\d+)>", name)
+        m = re.search(r"gemm_(?:bf16(?:_pp|_tile)?|small)_kernel<[^>]*?(true|false),\s*(true|false),\s*(\d+)"
+                      r"(?:,\s*(?:true|false))*>", name)
         if m:
             ak, bk, epi = m.group(1), m.group(2), int(m.group(3))
+        else:
+            m = re.search(r"gemm_small_kernelIDF16bLb([01])ELb([01])ELi(\d+)E", name)
+            if m:
+                ak, bk = ("true" if x == "1" else "false" for x in m.groups()[:2])
+                epi = int(m.group(3))
     if m:
         if (ak, bk) == ("false", "false"):
             return "gemm_wgrad"
-        if epi in (1, 2, 3):          # bias / bias + residual / bias + GeLU: the forward products
+        if epi in (1, 2, 3, 7):       # bias / bias + residual / bias + GeLU / a linear layer's: the forward products
             return "gemm_fwd"
-        if (ak, bk) == ("true", "true") and epi in (0, 4):
+        if epi in (0, 4):             # (a linear layer's weight may be stored either way)
             return "gemm_dgrad"
         return "gemm_other"
     if "gemm_f32" in name:
@@ -107,9 +114,13 @@ def kernel_class(name: str) -> str:
         return "reduce"
     if "attn_op_" in name:            # dq, dk and dv, the sums of shares
         return "attn_bwd"
-    if re.search(r"ln_(fwd|bwd)(_wave)?_k", name):
+    if "few_tokens_k" in name:
+        return "gemm_wgrad"
+    if "dropout_k" in name:
+        return "dropout"
+    if re.search(r"ln_(fwd|bwd)(_wave)?_k|norm_(fwd|bwd)_k", name):
         return "layernorm"
-    if "colsum" in name:
+    if "colsum" in name or "rows_finish_k" in name:
         return "reduce"
     if "adamw" in name:
         return "adamw"

@@ -385,3 +385,25 @@ def test_rows_of_a_view(shape, stride, want):
             _rows(t, "t")
     else:
         assert _rows(t, "t") == want
+
+
+@pytest.mark.parametrize("name,cls", [
+    ("gemm_bf16_persist_kernel<5, false, false, true, false>(GemmParams)", "gemm_wgrad"),
+    ("gemm_bf16_pp_kernel<128, 2, 3, 4, true, true, 0, false>(GemmParams)", "gemm_dgrad"),
+    ("gemm_bf16_pp_kernel<128, 2, 3, 4, true, false, 2, false>(GemmParams)", "gemm_fwd"),
+    ("gemm_bf16_pp_kernel<128, 2, 3, 4, false, false, 5, true>(GemmParams)", "gemm_wgrad"),
+    ("gemm_bf16_tile_kernel<128, 128, 2, true, true, 7, false>(GemmParams)", "gemm_fwd"),
+    ("gemm_bf16_tile_kernel<128, 128, 2, true, false, 4, false>(GemmParams)", "gemm_dgrad"),
+    ("gemm_bf16_kernel<256, 256, 8, 1, 64, 2, true, false, 6, false>(GemmParams)", "gemm_other"),
+    ("gemm_small_kernel<float, true, false, 7, true, false>(GemmParams)", "gemm_f32"),
+    ("_ZN12_GLOBAL__N_117gemm_small_kernelIDF16bLb1ELb0ELi7ELb0ELb0EEEv10GemmParams", "gemm_fwd"),
+    ("_ZN12_GLOBAL__N_117gemm_small_kernelIDF16bLb0ELb0ELi5ELb0ELb1EEEv10GemmParams", "gemm_wgrad"),
+    ("_ZN12_GLOBAL__N_115splitk_finish_kILi7EDF16bEEv10GemmParams", "gemm_fwd"),
+    ("_ZN12_GLOBAL__N_110norm_bwd_kIDF16bLi64ELi1ELb1ELi256EEEv8NormArgsii", "layernorm"),
+    ("_ZN12_GLOBAL__N_19dropout_kIDF16bLb0ELb1EEEv11DropoutArgsili", "dropout"),
+    ("(anonymous namespace)::rows_finish_k(Finish)", "reduce"),
+    ("_ZN12_GLOBAL__N_112few_tokens_kIDF16bLi8EEEv9FewTokens", "gemm_wgrad"),
+])
+def test_profile_classes(name, cls):
+    from paper_2405_14009_amd.profile_summary import kernel_class
+    assert kernel_class(name) == cls
