@@ -349,7 +349,7 @@ hipError_t launch_epi(const GemmParams& p, hipStream_t s) {
   const bool whole = p.batch * p.heads == 1 && p.krange == KR_FULL && !p.causal_skip;
   const F32Plan pl = plan_f32(p.M, p.N, p.kseg_len > 0 ? p.K / p.kseg_len : 1, p.kseg_len > 0 ? p.kseg_len : p.K,
                               (long)p.batch * p.heads, whole && p.split_work ? p.split_floats : 0,
-                              device_compute_units(), p.wide);
+                              device_compute_units(), p.wide, BKC ? p.ldb : 0);
   switch (p.epi) {
     case EPI_STORE: return launch<AK, BKC, EPI_STORE>(p, pl, s);
     case EPI_BIAS: return launch<AK, BKC, EPI_BIAS>(p, pl, s);

@@ -135,11 +135,16 @@ inline GemmPlan plan_stream(long M, long N, long K, long room_floats, int cus) {
   return p;
 }
 
-// Whether an operand of a 128-row tile spans more bytes than the 2^31 that the
-// fp32 kernels' buffer offsets reach (tiles start at their own 64-bit address, so
-// only the rows of one tile count).  The 32x32 kernel then copies through
-// registers; such a stage is bound by its state of tens of GB, not by this.
-inline bool f32_wide(long lda, long ldb) { return 127L * 4 * std::max(lda, ldb) + 512 > 0x7fffffffL; }
+// Whether `rows` rows of a k-contiguous operand, `ld` elements apart, lie within the
+// 2^31 - 1 bytes that the fp32 kernels' buffer offsets reach (tiles start at their
+// own 64-bit address, so only the rows of one tile count; a read beyond gives zeros).
+inline bool f32_reach(long rows, long ld) { return (rows - 1) * 4 * ld + 512 <= 0x7fffffffL; }
+
+// Whether an operand is out of reach of a tile of 128 rows, the most that the choice
+// below takes at any stride (above 4.2 million elements).  The 32x32 kernel then
+// copies through registers; such a stage is bound by its state of tens of GB, not by
+// this.
+inline bool f32_wide(long lda, long ldb) { return !f32_reach(128, std::max(lda, ldb)); }
 
 // Cost of splitting an fp32 reduction: as above, at about 8 TB/s from the caches
 // up to 64 MB and 1.25 beyond.
@@ -161,7 +166,10 @@ struct F32Plan {
 // another, of which the matrix core needs 0.43; a 128x128 one 2.0 of 1.7.)
 // wide: tiles of 128x256 too (3.8 of 3.4 us a k-tile), and costs fitted to the
 // linear operator's products, of few k-tiles as well (4096 x 4096 over 64 .. 4096).
-inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_floats, int cus, bool wide = false) {
+// ldb: the row stride of a k-contiguous right operand (else 0), which has to be in
+// reach over the tile's bn rows: 256 of them up to 2.1 million elements.
+inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_floats, int cus, bool wide = false,
+                        long ldb = 0) {
   struct Kind {
     int b, bn;
     GemmCost c;
@@ -178,6 +186,7 @@ inline F32Plan plan_f32(long M, long N, long nseg, long seg, long z, long room_f
   double best_us = 1e30;
   for (int i = 0; i < (wide ? 4 : 3); ++i) {
     const Kind& q = wide ? wides[i] : kinds[i];
+    if (q.bn > 128 && !f32_reach(q.bn, ldb)) continue;
     const long tiles = ((M + q.b - 1) / q.b) * ((N + q.bn - 1) / q.bn);
     for (int want = 1; want <= (q.b == 32 ? 1 : 64); ++want) {
       const long per = (nk + want - 1) / want;

@@ -450,6 +450,27 @@ def test_linear_beyond_a_buffer_s_reach():
     ref.close("db", db, *ref.column_sums(D, 0.0))
 
 
+@pytest.mark.parametrize("stride", [2200000, 4200000, 4300000])
+def test_linear_fp32_weight_of_rows_far_apart(stride):
+    """Rows of a weight 2^23 bytes and more apart: 256 of them span more than a copy reaches from a tile's start,
+    beyond 4.2 million elements 128 do too."""
+    rows, k, n = 16384, 64, 512
+    wide = torch.empty(n, stride, device="cuda")
+    w = wide[:, 8:8 + k]
+    w.copy_(normal(1, n, k, std=0.1, kind=F32))
+    x, s = normal(2, rows, k, kind=F32), normal(3, rows, n, mean=0.5, kind=F32)
+    W = ref.wide(w)
+    want, e = ref.product(ref.wide(x), W.T)
+    ref.close("y", ops().linear_forward(x, w.t())[0], want, e)              # stored [out, in]
+    ref.close("dx", ops().linear_backward_input(x, w), want, e)             # stored [in, out]
+    ref.close("dx", ops().linear_backward_input(x, w, derivative=s), want * ref.wide(s),
+              (e + ref.U * np.abs(want)) * np.abs(ref.wide(s)))
+    # reduced over the rows far apart
+    want, e = ref.product(ref.wide(s), W)
+    ref.close("y", ops().linear_forward(s, w)[0], want, e)
+    ref.close("dx", ops().linear_backward_input(s, w.t()), want, e)
+
+
 # -- gradients against differences, together, streams and graphs -----------------------
 
 

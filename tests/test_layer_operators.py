@@ -191,6 +191,52 @@ def test_plans_leave_room_for_the_left_operand_s_sums(tmp_path):
     assert r.returncode == 0, r.stdout
 
 
+REACH = r"""
+#include <cstdio>
+#include "gemm_plan.h"
+int main() {
+  const long strides[] = {512, 2100000, 2105372, 2105376, 2105380, 2105384, 2200000, 4194304, 4226948, 4227192, 4227196, 5000000};
+  int wide = 0;
+  for (long M : {64L, 2048L, 4096L, 8192L, 16384L}) for (long N : {256L, 512L, 4096L}) for (long K : {64L, 512L, 4096L})
+    for (long room : {0L, 16L << 20}) for (long lda : strides) for (long ldb : strides) for (bool kcontig : {false, true}) {
+      if (f32_wide(lda, ldb)) continue;   // copied from 64-bit addresses
+      const F32Plan p = plan_f32(M, N, 1, K, 1, room, 256, true, kcontig ? ldb : 0);
+      // the last chunk of a tile's last row, k-contiguous (else its rows are the k-tile's 32)
+      const long a = (p.bm - 1) * 4 * lda + 4 * 32, b = ((kcontig ? p.bn : 32) - 1) * 4 * ldb + 4 * (kcontig ? 32 : p.bn);
+      if (a > 0x7fffffffL || b > 0x7fffffffL) {
+        std::printf("M %ld N %ld K %ld lda %ld ldb %ld: tile %d x %d\n", M, N, K, lda, ldb, p.bm, p.bn);
+        return 1;
+      }
+      wide += p.bn == 256;
+      // no effect where the rows are in reach (255 * 4 * 2105376 + 128 is 2^31)
+      const F32Plan q = plan_f32(M, N, 1, K, 1, room, 256, true);
+      if (ldb < 2105376 && (q.bn != p.bn || q.bm != p.bm || q.splits != p.splits)) return 2;
+    }
+  return wide > 0 ? 0 : 3;
+}
+"""
+
+
+def run_host(tmp_path, text):
+    """The exit status and output of a host program over the launchers' headers."""
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no host compiler")
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2405_14009_amd", "csrc")
+    (tmp_path / "main.cpp").write_text(text)
+    exe = str(tmp_path / "main")
+    subprocess.run([cxx, "-std=c++17", "-O2", "-I", csrc, str(tmp_path / "main.cpp"), "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True)
+    return r.returncode, r.stdout
+
+
+def test_fp32_tiles_stay_in_reach_of_their_copies(tmp_path):
+    """Copies reach 2^31 - 1 bytes from a tile's start (beyond, they deposit zeros): the rows of every tile that
+    the plan takes lie within, whatever the row strides."""
+    status, out = run_host(tmp_path, REACH)
+    assert status == 0, (status, out)
+
+
 # -- refusals ------------------------------------------------------------------------
 
 BAD_ROWS = [(dict(dtype=9), "INVALID_ARG", b"dtype"), (dict(param_dtype=2), "INVALID_ARG", b"param_dtype"),
