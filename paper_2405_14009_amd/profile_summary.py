@@ -99,7 +99,9 @@ def kernel_class(name: str) -> str:
             return "gemm_wgrad"
         if epi in (1, 2, 3, 7):       # bias / bias + residual / bias + GeLU / a linear layer's: the forward products
             return "gemm_fwd"
-        if epi in (0, 4):             # (a linear layer's weight may be stored either way)
+        # a linear layer's weight may be stored either way; without a derivative the product
+        # with one stored [out, in] has the name of materialised attention's P V and dS K
+        if epi == 4 or (epi == 0 and bk == "true"):
             return "gemm_dgrad"
         return "gemm_other"
     if "gemm_f32" in name:

@@ -453,3 +453,14 @@ def test_rows_of_a_view(shape, stride, want):
 def test_profile_classes(name, cls):
     from paper_2405_14009_amd.profile_summary import kernel_class
     assert kernel_class(name) == cls
+
+
+@pytest.mark.parametrize("name", [
+    "gemm_bf16_kernel<256, 256, 8, 1, 64, 2, true, false, 0, false>(GemmParams)",
+    "gemm_bf16_tile_kernel<64, 64, 4, true, false, 0>(GemmParams)",
+    "_ZN12_GLOBAL__N_117gemm_small_kernelIDF16bLb1ELb0ELi0ELb0ELb0EEEv10GemmParams",
+])
+def test_profile_class_of_materialised_attention(name):
+    """P V and dS K, forward and backward, are no input gradient of a linear layer."""
+    from paper_2405_14009_amd.profile_summary import kernel_class
+    assert kernel_class(name) == "gemm_other"
