@@ -10,9 +10,13 @@
 // and 17 us, 16 tokens 18.7 and 17.4 us).
 constexpr int few_tokens_most(int elt) { return elt == 2 ? 8 : 32; }
 
+// Rows of the gradient that a workgroup takes, and the most of them: a grid's second
+// dimension holds 2^16 - 1.
+constexpr int FEW_ROWS = 32, FEW_MOST_ROWS = FEW_ROWS * 0xffff;
+
 // out [m, n] (+)= left^T right over the rows ("tokens") of both
 // operands; sums, where given, (+)= the column sums of right (sums_right) or left.
-// m and n multiples of 8, all rows 16-byte aligned; m / 32 below 2^16.
+// m and n multiples of 8, all rows 16-byte aligned; m at most FEW_MOST_ROWS.
 struct FewTokens {
   int tokens, m, n;
   RowsView left, right;

@@ -15,7 +15,7 @@
 
 namespace {
 
-constexpr int NT = 256, FEW_ROWS = 32;
+constexpr int NT = 256;
 
 template <class E>
 __device__ __forceinline__ void load4(const E* p, float (&f)[4]) {
@@ -119,6 +119,6 @@ hipError_t launch(const FewTokens& a, hipStream_t s) {
 }  // namespace
 
 hipError_t few_tokens(const FewTokens& a, int elt, hipStream_t s) {
-  if (a.tokens > few_tokens_most(elt)) return hipErrorInvalidValue;
+  if (a.tokens > few_tokens_most(elt) || a.m > FEW_MOST_ROWS) return hipErrorInvalidValue;
   return elt == 2 ? launch<bf16>(a, s) : launch<float>(a, s);
 }

@@ -81,9 +81,9 @@ bool sums_in_product(const LinearArgs& a) { return a.dbias && a.elt == 2; }
 struct WeightWork {
   long split, sums;
 };
-// Few tokens: no tiles.  (A grid's second dimension holds 2^16 - 1.)
+// Few tokens: no tiles.
 bool few(const LinearArgs& a) {
-  return a.rows > 0 && a.rows <= few_tokens_most(a.elt) && std::max(a.in, a.out) < 1 << 21;
+  return a.rows > 0 && a.rows <= few_tokens_most(a.elt) && std::max(a.in, a.out) <= FEW_MOST_ROWS;
 }
 WeightWork weight_work(const LinearArgs& a) {
   if (few(a)) return {0, 0};

@@ -450,6 +450,18 @@ def test_linear_beyond_a_buffer_s_reach():
     ref.close("db", db, *ref.column_sums(D, 0.0))
 
 
+@KINDS
+@pytest.mark.parametrize("i,o", [(65535 * 32, 8), ((1 << 21) - 8, 8), (8, (1 << 21) - 8)])
+def test_weight_gradient_of_a_token_and_many_columns(i, o, kind):
+    """At both sides of the most rows that few tokens' outer products take."""
+    for rows in (1, 3):
+        x, dy = normal(1, rows, i, kind=kind), normal(2, rows, o, kind=kind)
+        for by_out in (False, True):
+            dw, db = ops().linear_backward_weight(x, dy, by_out=by_out)
+            ref.close("dw", dw, *ref.product(ref.wide(x).T, ref.wide(dy)))
+            ref.close("db", db, *ref.column_sums(ref.wide(dy), 0.0))
+
+
 @pytest.mark.parametrize("stride", [2200000, 4200000, 4300000])
 def test_linear_fp32_weight_of_rows_far_apart(stride):
     """Rows of a weight 2^23 bytes and more apart: 256 of them span more than a copy reaches from a tile's start,

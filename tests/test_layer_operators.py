@@ -137,6 +137,20 @@ def test_linear_memory(r, i, o, dtype):
         assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=r, in_=i, out=o)), None, None, None) == 0
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("by_out", [0, 1])
+def test_few_tokens_fit_a_grid(dtype, by_out):
+    """Weight gradients of few tokens take no work memory: up to 65535 blocks of 32 rows, which a grid's
+    second dimension holds."""
+    L, lib = lib_or_skip()
+    n = ctypes.c_size_t()
+    for rows_of, few in ((65535 * 32, True), (65535 * 32 + 8, False), ((1 << 21) - 8, False)):
+        i, o = (8, rows_of) if by_out else (rows_of, 8)
+        assert lib.rc_linear_memory(REF(linear(dtype=dtype, rows=1, in_=i, out=o, by_out=by_out)), None, None, REF(n)) == 0
+        # (other products of one token sum dy's columns on their way: bf16)
+        assert n.value == 0 if few else n.value > 0 or dtype == 0, (rows_of, n.value)
+
+
 PLAN = r"""
 #include <cstdio>
 #include "gemm_plan.h"
