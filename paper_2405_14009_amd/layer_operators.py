@@ -6,7 +6,8 @@ Argument marshalling only, as for the attention operator: every step runs in the
 HIP library, on PyTorch's current stream of the tensors' device, with outputs
 and work memory from PyTorch, so the calls may be captured into a graph.
 Autograd does not record them: a forward pass that it would have to record is
-refused, and a backward pass is a call of its own.
+refused, a backward pass is a call of its own, and what one of these calls would
+lose of a tangent or of a second derivative is refused as well.
 
 Matrices are tensors [..., columns] in bf16 or fp32, whose leading dimensions
 have one stride between them; columns are contiguous.  Vectors of parameters are
@@ -20,7 +21,7 @@ from typing import NamedTuple, Optional
 
 from . import _lib as L
 from . import operators as _ops
-from .operators import _kind, _kinds
+from .operators import _kind, _kinds, _no_graph, _no_second_graph
 
 _ACTIVATIONS = {None: L.RC_ACT_NONE, "gelu": L.RC_ACT_GELU, "relu": L.RC_ACT_RELU, "silu": L.RC_ACT_SILU}
 _ref, _Matrix = ctypes.byref, L.RcMatrix
@@ -152,15 +153,6 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
-def _no_graph(*tensors):
-    """Refuses (tensor, name, ...) that autograd would have to record."""
-    if torch.is_grad_enabled():
-        for t, name in zip(tensors[::2], tensors[1::2]):
-            if t is not None and getattr(t, "requires_grad", False):
-                raise RuntimeError(f"{name} requires gradients, which autograd does not pass through this call; "
-                                   "call it under torch.no_grad(), and the operator's backward calls for them")
-
-
 def _dropout(drop, device):
     if not isinstance(drop, Dropout):
         raise TypeError("drop must be a Dropout")
@@ -234,6 +226,7 @@ def dropout_backward(dy, drop: Dropout, *, derivative=None, bias_grad=False, acc
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
+    _no_second_graph(dy, "dy", derivative, "derivative")
     shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
     d = _dropout(drop, device)
     rows, step = _rows(dy, "dy")
@@ -296,6 +289,7 @@ def layer_norm_backward(dy, total, stats, weight=None, *, dtotal=None, drop: Opt
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
+    _no_second_graph(dy, "dy", total, "total", stats, "stats", weight, "weight", dtotal, "dtotal")
     shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
     d = None if drop is None else _dropout(drop, device)
     rows, step = _rows(dy, "dy")
@@ -391,6 +385,7 @@ def linear_backward_input(dy, weight, *, derivative=None, out=None):
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
+    _no_second_graph(dy, "dy", weight, "weight", derivative, "derivative")
     dtype, device = dy.dtype, dy.get_device()
     rows, step = _rows(dy, "dy")
     wm, by_out = _weight(weight, dtype, device)
@@ -418,6 +413,7 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
     if torch is None:
         _import()
     kind = _kind(x, "x")
+    _no_second_graph(x, "x", dy, "dy")
     dtype, device = x.dtype, x.get_device()
     rows, step = _rows(x, "x")
     _tensor(dy, "dy", dtype, device)

@@ -6,7 +6,9 @@ Argument marshalling only: every step runs in the HIP library.  The calls
 enqueue on PyTorch's current stream of the tensors' device and take their
 outputs and scratch memory from PyTorch, so they may be captured into a graph.
 Autograd does not record them: a backward pass is a call of its own, as it is
-for a stage, and a forward pass that autograd would have to record is refused.
+for a stage.  A forward pass that autograd would have to record is refused, and so
+are tangents of forward-mode differentiation and the backward calls of a backward
+pass that is itself recorded (create_graph).
 """
 from __future__ import annotations
 
@@ -20,13 +22,15 @@ from . import _lib as L
 
 
 torch = None   # imported with the first call
+_dual = None   # torch.autograd.forward_ad
 _kinds = {}    # the library's dtype by PyTorch's
 
 
 def _import():
-    global torch
+    global torch, _dual
     if torch is None:
         import torch as module
+        import torch.autograd.forward_ad as _dual
         _kinds.update({module.bfloat16: L.RC_BF16, module.float32: L.RC_FP32})
         torch = module
 
@@ -39,6 +43,36 @@ def _kind(t, name):
     if kind is None:
         raise ValueError(f"{name} must be bfloat16 or float32, not {t.dtype}")
     return kind
+
+
+def _no_graph(*tensors):
+    """Refuses (tensor, name, ...) of a forward call that autograd would have to record."""
+    if torch.is_grad_enabled():
+        for t, name in zip(tensors[::2], tensors[1::2]):
+            if t is not None and getattr(t, "requires_grad", False):
+                raise RuntimeError(f"{name} requires gradients, which autograd does not pass through this call; "
+                                   "call it under torch.no_grad(), and the operator's backward calls for them")
+    if _dual._current_level >= 0:
+        _no_tangent(tensors)
+
+
+def _no_second_graph(*tensors):
+    """Refuses (tensor, name, ...) of a backward call within a backward pass that autograd
+    records (create_graph).  Elsewhere gradients are taken as results, whatever
+    their inputs require (a weight's may be left to a later call)."""
+    if torch.is_grad_enabled() and torch._C._current_graph_task_id() >= 0:
+        for t, name in zip(tensors[::2], tensors[1::2]):
+            if t is not None and getattr(t, "requires_grad", False):
+                raise RuntimeError(f"{name} requires gradients, which a backward pass with create_graph would take "
+                                   "through this call; the operators have no second derivatives")
+    if _dual._current_level >= 0:
+        _no_tangent(tensors)
+
+
+def _no_tangent(tensors):
+    for t, name in zip(tensors[::2], tensors[1::2]):
+        if isinstance(t, torch.Tensor) and _dual.unpack_dual(t).tangent is not None:
+            raise RuntimeError(f"{name} has a tangent, which this call would lose; it has no forward-mode derivative")
 
 
 def _view(t, name, q, shape):
@@ -157,11 +191,7 @@ def attention_forward(q, k, v, *, causal: bool = True, window: int = 0, sinks: i
     Tensors that require gradients are taken where autograd is off (no_grad, or
     the forward of an autograd function): o has no graph."""
     _import()
-    if torch.is_grad_enabled():
-        for name, t in (("q", q), ("k", k), ("v", v), ("rel_bias", rel_bias), ("out", out)):
-            if t is not None and getattr(t, "requires_grad", False):
-                raise RuntimeError(f"{name} requires gradients, which autograd does not pass through this call; "
-                                   "call it under torch.no_grad(), and attention_backward for them")
+    _no_graph(q, "q", k, "k", v, "v", rel_bias, "rel_bias", out, "out")
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
     on, stream = _on(q.device)
     o, ov = _new(q) if out is None else (out, _view(out, "out", q, c.shape))
@@ -179,6 +209,8 @@ def attention_backward(dout, q, k, v, o, saved, *, causal: bool = True, window: 
     a bias and of its type otherwise.  o and saved are attention_forward's for the
     same arguments; dq, dk, dv: tensors for the gradients (all of their elements
     are written)."""
+    _import()
+    _no_second_graph(dout, "dout", q, "q", k, "k", v, "v", rel_bias, "rel_bias", o, "o")
     c = _Call(q, k, v, causal, window, sinks, rel_bias, max_distance, lengths, scale)
     if (not isinstance(saved, torch.Tensor) or saved.numel() != c.saved_bytes or saved.device != q.device
             or saved.dtype is not torch.uint8 or not saved.is_contiguous()):

@@ -685,3 +685,62 @@ def test_refusals_of_device_tensors():
         with pytest.raises((ValueError, TypeError, ops().RcError)):
             call()
             raise AssertionError(f"case {i} was taken")
+
+
+def test_no_tangent_or_second_derivative_is_lost():
+    """Every call refuses tangents, and the backward calls a pass with create_graph; outside of one they take
+    tensors that require gradients, as a deferred weight gradient's."""
+    import torch.autograd.forward_ad as dual
+    o, x, w, g = ops(), normal(1, 6, 64), normal(2, 64, 64), normal(3, 64, kind=F32)
+    drop = ops().Dropout(0.1, 1)
+    _, total, stats = o.layer_norm_forward(x, g)
+    q = normal(4, 1, 8, 2, 32)
+    att, saved = o.attention_forward(q, q, q)
+    bare = torch.ones(6, 64, dtype=BF16, device="cuda")
+    calls = {   # of an input and of a parameter or stored tensor
+        "dropout_backward": [lambda t: o.dropout_backward(t, drop), lambda t: o.dropout_backward(bare, drop, derivative=t)],
+        "layer_norm_backward": [lambda t: o.layer_norm_backward(t, total, stats, g),
+                                lambda t: o.layer_norm_backward(bare, t, stats, g),
+                                lambda t: o.layer_norm_backward(bare, total, stats, g, dtotal=t)],
+        "linear_backward_input": [lambda t: o.linear_backward_input(t, w),
+                                  lambda t: o.linear_backward_input(bare, w, derivative=t)],
+        "linear_backward_weight": [lambda t: o.linear_backward_weight(t, bare), lambda t: o.linear_backward_weight(bare, t)],
+    }
+    forward = [lambda t: o.dropout_forward(t, drop), lambda t: o.dropout_forward(bare, drop, residual=t),
+               lambda t: o.layer_norm_forward(t, g), lambda t: o.layer_norm_forward(bare, residual=t),
+               lambda t: o.linear_forward(t, w), lambda t: o.linear_forward(bare, w, residual=t)]
+    backward = [c for v in calls.values() for c in v]
+    with torch.no_grad(), dual.dual_level():
+        t = dual.make_dual(x, x)
+        for i, call in enumerate(forward + backward):
+            with pytest.raises(RuntimeError, match="tangent"):
+                call(t)
+                raise AssertionError(f"case {i} was taken")
+            call(x)
+        t = dual.make_dual(q, q)
+        for call in (lambda: o.attention_forward(q, t, q), lambda: o.attention_backward(q, q, t, q, att, saved)):
+            with pytest.raises(RuntimeError, match="tangent"):
+                call()
+
+    class Through(torch.autograd.Function):
+        """y = 2 x, whose backward runs a call of x's on the way."""
+
+        @staticmethod
+        def forward(ctx, x, call):
+            ctx.save_for_backward(x)
+            ctx.call = call
+            return 2 * x
+
+        @staticmethod
+        def backward(ctx, g):
+            ctx.call(ctx.saved_tensors[0])
+            return 2 * g, None
+
+    leaf, lq = x.clone().requires_grad_(), q.clone().requires_grad_()
+    some = [(leaf, c) for c in backward] + [(lq, lambda t: o.attention_backward(q, t, q, q, att, saved))]
+    for i, (t, call) in enumerate(some):
+        call(t)
+        torch.autograd.grad(Through.apply(t, call).sum(), t)
+        with pytest.raises(RuntimeError, match="create_graph"):
+            torch.autograd.grad(Through.apply(t, call).sum(), t, create_graph=True)
+            raise AssertionError(f"case {i} was taken")

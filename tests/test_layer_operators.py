@@ -478,3 +478,38 @@ def test_profile_class_of_materialised_attention(name):
     """P V and dS K, forward and backward, are no input gradient of a linear layer."""
     from paper_2405_14009_amd.profile_summary import kernel_class
     assert kernel_class(name) == "gemm_other"
+
+
+def test_what_autograd_would_lose():
+    """The guards that every call goes through: forward calls under autograd, backward calls of a pass with
+    create_graph, tangents in either, whatever the grad mode."""
+    torch = pytest.importorskip("torch")
+    import torch.autograd.forward_ad as dual
+    from paper_2405_14009_amd import operators as o
+    o._import()
+    leaf, plain = torch.ones(2, requires_grad=True), torch.ones(2)
+    with pytest.raises(RuntimeError, match="b requires gradients"):
+        o._no_graph(plain, "a", leaf, "b")
+    with torch.no_grad():
+        o._no_graph(plain, "a", leaf, "b", None, "c")
+    o._no_second_graph(leaf, "a")   # a call of its own, as a deferred weight gradient is
+    for guard in (o._no_graph, o._no_second_graph):
+        with dual.dual_level(), torch.no_grad():
+            guard(plain, "a", leaf, "b", None, "c", True, "d")
+            with pytest.raises(RuntimeError, match="b has a tangent"):
+                guard(plain, "a", dual.make_dual(plain, plain), "b")
+
+    class Twice(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            ctx.save_for_backward(x)
+            return 2 * x
+
+        @staticmethod
+        def backward(ctx, g):
+            o._no_second_graph(g, "g", *ctx.saved_tensors, "x")
+            return 2 * g
+
+    torch.autograd.grad(Twice.apply(leaf).sum(), leaf)
+    with pytest.raises(RuntimeError, match="x requires gradients.*create_graph"):
+        torch.autograd.grad(Twice.apply(leaf).sum(), leaf, create_graph=True)
