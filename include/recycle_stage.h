@@ -633,10 +633,10 @@ enum { RC_ACT_NONE = 0, RC_ACT_GELU = 1, RC_ACT_RELU = 2, RC_ACT_SILU = 3 };
  * calls, as a stage's does: the input's gradient, and the parameters', which may
  * be deferred.
  *
- * Requirements (otherwise RC_ERR_UNSUPPORTED): in and out multiples of 8; bf16: the
- * weight spans less than 2^31 bytes, row strides below 2^21 elements.  data and row
- * strides of all matrices are multiples of 16 bytes, their rows do not overlap,
- * dweight is 16-byte aligned. */
+ * Requirements (otherwise RC_ERR_UNSUPPORTED): in and out multiples of 8, up to 2^30,
+ * their product below 2^40; bf16: the weight spans less than 2^31 bytes, row
+ * strides below 2^21 elements.  data and row strides of all matrices are
+ * multiples of 16 bytes, their rows do not overlap, dweight is 16-byte aligned. */
 typedef struct rc_linear {
   int32_t dtype;        /* rc_dtype of the matrices */
   int32_t bias_dtype;   /* rc_dtype of bias; gradients of weight and bias are fp32 */

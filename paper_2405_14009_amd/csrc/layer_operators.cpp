@@ -16,6 +16,9 @@ namespace {
 static_assert((int)RC_ACT_GELU == ACT_GELU && (int)RC_ACT_RELU == ACT_RELU && (int)RC_ACT_SILU == ACT_SILU, "activations");
 
 constexpr int64_t MAX_ROWS = 0x7fffffff, MAX_COLS = 1 << 29, MAX_ELEMENTS = 1LL << 46;
+// Widths of a linear layer: the products count rows and columns in 32 bits, up to a
+// tile past the last one, and the bias gradient's bytes of a row (fp32) in 32 unsigned.
+constexpr int32_t MAX_WIDTH = 1 << 30;
 
 bool known(int dtype) { return dtype == RC_FP32 || dtype == RC_BF16; }
 
@@ -137,6 +140,7 @@ rc_status linear_args(const rc_linear* l, LinearArgs& a) {
   if (l->activation < RC_ACT_NONE || l->activation > RC_ACT_SILU) return fail(RC_ERR_INVALID_ARG, "unknown activation");
   TRY(flag(l->by_out, "by_out"));
   if (l->in % 8 || l->out % 8) return fail(RC_ERR_UNSUPPORTED, "in and out must be multiples of 8");
+  if (l->in > MAX_WIDTH || l->out > MAX_WIDTH) return fail(RC_ERR_UNSUPPORTED, "in or out above 2^30");
   a.elt = elt_of(l->dtype);
   if (a.elt == 2 && 2LL * l->in * l->out > 0x7fffffffLL)
     return fail(RC_ERR_UNSUPPORTED, "a weight of 2^31 bytes or more");

@@ -371,6 +371,16 @@ def test_bad_linear(kw, st, word):
     refused(lib.rc_linear_backward_weight(l, at(0), at(1), place(4), None, 0, place(5), None), st, word)
 
 
+@pytest.mark.parametrize("kw", [dict(in_=(1 << 30) + 8, out=8), dict(in_=8, out=(1 << 30) + 8),
+                                dict(in_=8, out=(1 << 31) - 8)], ids=str)
+def test_linear_widths_that_32_bits_do_not_count(kw):
+    """fp32 weights of 2^33 elements would fit a card; a tile past the last column, or the bytes of a row, would
+    not fit the kernels' 32 bits."""
+    test_bad_linear(dict(kw, dtype=0), "UNSUPPORTED", b"2^30")
+    L, lib = lib_or_skip()
+    assert lib.rc_linear_memory(REF(linear(dtype=0, in_=8, out=1 << 30)), None, None, None) == 0
+
+
 def test_linear_refusals():
     L, lib = lib_or_skip()
     W = place(9)
