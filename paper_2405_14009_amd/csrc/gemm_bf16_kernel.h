@@ -308,7 +308,9 @@ __device__ __forceinline__ void mma_tile(f32x16 (&acc)[TM][TN], const char* ta, 
 // accumulated) fetch the next block-row's inputs while the current one is
 // finished, so those loads overlap instead of each costing a round trip
 // (LOOK; without it each block-row's inputs are fetched as it is finished,
-// which needs 32 fewer registers).
+// which needs 32 fewer registers).  In the 256 x 128 tile's kernel the linear
+// operator's epilogue spills with it, whether or not there is a residual: 42 registers
+// of weights [in, out], 29 of [out, in] (the stage's bias and residual: 2).
 template <int EPI, int TN, int I0, int I1, bool LOOK = true, int TM = 4>
 __device__ __forceinline__ void epilogue(const GemmParams& p, f32x16 (&acc)[TM][TN], float* sm, int m0,
                                          int n0, int lane, long c_off) {

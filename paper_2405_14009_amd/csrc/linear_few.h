@@ -5,9 +5,11 @@
 
 #include "rows_op.h"
 
-// Most tokens that the kernel takes, by the bytes of an element: where it and the
-// tile kernels meet (4096 x 4096, fp32: 16 tokens 15 and 44 us, bf16: 8 tokens 15
-// and 17 us, 16 tokens 18.7 and 17.4 us).
+// Most tokens that the kernel takes, by the bytes of an element.  bf16: where it and
+// the tile kernels meet (4096 x 4096: 8 tokens 15 and 19 us, 16 tokens 18.7 and 17.4
+// to 19).  fp32: what a thread holds of them in registers (176 of 32 tokens; 4096 x
+// 4096: 16 tokens 15 and 39 us, 32 tokens 22 and 39), which is short of where the two
+// would meet.
 constexpr int few_tokens_most(int elt) { return elt == 2 ? 8 : 32; }
 
 // Rows of the gradient that a workgroup takes, and the most of them: a grid's second

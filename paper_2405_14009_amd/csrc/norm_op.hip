@@ -32,7 +32,13 @@ NormPlan plan_of(long rows, int cols, bool sums) {
     p.threads = 64 * p.waves * p.slots;
   }
   const long sets = std::max(1L, (rows + p.slots - 1) / p.slots);
-  const int room = sums ? 1024 : 1792;   // threads of a compute unit, as registers allow
+  // Threads that a compute unit's share of the grid has: four waves a SIMD with sums,
+  // else seven, what the forward of bf16 rows of 1025 .. 8192 columns, in whole
+  // groups, holds at a time.  The other kernels hold fewer (odd bf16 rows six, fp32 rows five or
+  // four, 513 .. 1024 columns four or three and backward two, a backward pass without
+  // sums four), so that a full grid of theirs walks its rows in a second, partly empty
+  // round of workgroups.
+  const int room = sums ? 1024 : 1792;
   // sums of few rows are one workgroup's, which stores them itself
   if (sums && sets <= 4) p.groups = 1;
   else p.groups = std::min(sets, (long)CUS * std::max(1, room / p.threads));
