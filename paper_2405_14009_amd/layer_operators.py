@@ -25,13 +25,13 @@ from .operators import _kind, _kinds, _no_graph, _no_second_graph
 
 _ACTIVATIONS = {None: L.RC_ACT_NONE, "gelu": L.RC_ACT_GELU, "relu": L.RC_ACT_RELU, "silu": L.RC_ACT_SILU}
 _ref, _Matrix = ctypes.byref, L.RcMatrix
-torch = None   # imported with the first call
+torch = _dual = _task = None   # imported with the first call
 
 
 def _import():
-    global torch
+    global torch, _dual, _task
     _ops._import()
-    torch = _ops.torch
+    _dual, _task, torch = _ops._dual, _ops._task, _ops.torch
 
 
 class Dropout:
@@ -226,7 +226,8 @@ def dropout_backward(dy, drop: Dropout, *, derivative=None, bias_grad=False, acc
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
-    _no_second_graph(dy, "dy", derivative, "derivative")
+    if _task() >= 0 or _dual._current_level >= 0:
+        _no_second_graph(dy, "dy", derivative, "derivative")
     shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
     d = _dropout(drop, device)
     rows, step = _rows(dy, "dy")
@@ -289,7 +290,8 @@ def layer_norm_backward(dy, total, stats, weight=None, *, dtotal=None, drop: Opt
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
-    _no_second_graph(dy, "dy", total, "total", stats, "stats", weight, "weight", dtotal, "dtotal")
+    if _task() >= 0 or _dual._current_level >= 0:
+        _no_second_graph(dy, "dy", total, "total", stats, "stats", weight, "weight", dtotal, "dtotal")
     shape, dtype, device = dy.shape, dy.dtype, dy.get_device()
     d = None if drop is None else _dropout(drop, device)
     rows, step = _rows(dy, "dy")
@@ -385,7 +387,8 @@ def linear_backward_input(dy, weight, *, derivative=None, out=None):
     if torch is None:
         _import()
     kind = _kind(dy, "dy")
-    _no_second_graph(dy, "dy", weight, "weight", derivative, "derivative")
+    if _task() >= 0 or _dual._current_level >= 0:
+        _no_second_graph(dy, "dy", weight, "weight", derivative, "derivative")
     dtype, device = dy.dtype, dy.get_device()
     rows, step = _rows(dy, "dy")
     wm, by_out = _weight(weight, dtype, device)
@@ -413,7 +416,8 @@ def linear_backward_weight(x, dy, *, by_out: bool = False, weight_grad=True, bia
     if torch is None:
         _import()
     kind = _kind(x, "x")
-    _no_second_graph(x, "x", dy, "dy")
+    if _task() >= 0 or _dual._current_level >= 0:
+        _no_second_graph(x, "x", dy, "dy")
     dtype, device = x.dtype, x.get_device()
     rows, step = _rows(x, "x")
     _tensor(dy, "dy", dtype, device)
